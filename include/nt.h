@@ -377,6 +377,65 @@ nt_status nt_op_select_tiled(const float* d_logits, int32_t rows, int32_t V, int
 nt_status nt_op_select_tiled_noalloc(const float* d_logits, int32_t rows, int32_t V, int32_t k, float* d_topv,
                                      int32_t* d_topi, float* d_lse, void* stream);
 
+/* ---- a paged key/value cache -----------------------------------------------------------
+ * A cache for requests whose lengths differ and grow: the keys of every sequence lie in a
+ * pool of pages [n_pages][n_kv_heads][page_len][d_head], the values in another of the same
+ * shape, and position p of sequence b is slot p % page_len of page
+ * d_table[b * max_pages + p / page_len].  The caller hands pages out (a page may appear in
+ * several sequences' rows: a prefix that hypotheses share) and owns pools and table.  An
+ * entry outside [0, n_pages) is a hole: its positions are neither written nor attended to.
+ * This is the step cache of nt_decode_step (Sec. 4.1 "Caching") without its reservation of
+ * every sequence's longest target.
+ *  dtype: type of queries, new keys and values, and outputs.  fp8: 0: the pools hold dtype;
+ *    1 with dtype NT_F16: E4M3 bytes, as for fp8_kv.
+ *  d_head in {32, 64, 128}; page_len in {16, 32, 64, 128, 256}; pools 16-byte aligned. */
+typedef struct {
+  int32_t dtype, fp8, n_kv_heads, d_head, page_len, n_pages, max_pages;
+  void* d_k;
+  void* d_v;
+  const int32_t* d_table;
+} nt_kv_pages;
+
+/* Puts new tokens' keys and values into the cache.  Row i of d_k and d_v (ld elements apart;
+ * head h at h * d_head, so the K and V columns of a QKV projection's output as they are) is
+ * one token of one sequence.  d_off: [n_seqs + 1] non-decreasing device int32, sequence b's
+ * new rows being d_off[b] .. d_off[b+1] - 1; NULL: row b is sequence b's only new token
+ * (n_rows == n_seqs).  d_lens: [n_seqs] device int32, lengths with the new tokens counted:
+ * sequence b's rows go to its last positions, the last row to d_lens[b] - 1.  n_rows: rows of
+ * d_k and d_v (rows of no sequence, positions below 0 or past max_pages pages, and holes are
+ * left out; nothing else of the pools changes).  An fp8 cache takes the E4M3 value nearest to
+ * each element (ties to even, saturating at 448).  Two rows of one call for the same slot of
+ * the same page (sequences that share a page they both extend) leave either in it.
+ * Asynchronous, on the current device.  NT_E_INVALID for a null pointer, a negative size, a
+ * shape the struct does not allow, or rows that are not 16-byte aligned; NT_E_UNSUPPORTED for
+ * fp8 with another dtype than NT_F16. */
+nt_status nt_op_kv_append(const nt_kv_pages* cache, const void* d_k, const void* d_v, int32_t ld,
+                          const int32_t* d_off, const int32_t* d_lens, int32_t n_seqs, int32_t n_rows, void* stream);
+
+/* Attention of one new token a sequence over its cached positions 0 .. d_lens[b] - 1 (the new
+ * token's own key and value among them, where nt_op_kv_append put them first):
+ *   out[b][h] = sum_j p_j V_j,  p = softmax_j(scale * q[b][h] . K_j),
+ * query head h reading key head h / (n_heads / n_kv_heads).  d_q, d_out: dtype, row b at
+ * b * q_ld / b * out_ld, head h at h * d_head within.  d_lens: [n_seqs] device int32.
+ * max_len: at least every length (host; what the work is divided by): positions past it are
+ * not read.  Scores, softmax and sums are fp32; the probabilities enter the second product in
+ * dtype.  Positions in holes are left out; a row with nothing to attend to (length 0 or less)
+ * is zero.  What lies in the pages behind a length is never part of a result, whatever it is.
+ * d_ws: workspace of at least nt_op_attn_paged_workspace bytes (256-byte aligned; may be NULL
+ * when that is 0), in use until the call's work is done: calls that may overlap need their
+ * own.  Results do not depend on the other sequences of a call except through how a length is
+ * divided (a matter of rounding).  Asynchronous, one or two launches, on the current device.
+ * NT_E_INVALID for a null pointer, a negative size, n_heads that n_kv_heads does not divide,
+ * rows that are not 16-byte aligned, or a shape the struct does not allow; NT_E_UNSUPPORTED for
+ * fp8 with another dtype than NT_F16 or more work than one launch takes; NT_E_WORKSPACE if
+ * ws_bytes is too small (the message states the bytes required). */
+nt_status nt_op_attn_paged(const nt_kv_pages* cache, const void* d_q, int32_t q_ld, int32_t n_heads,
+                           const int32_t* d_lens, int32_t n_seqs, int32_t max_len, float scale, void* d_out,
+                           int32_t out_ld, void* d_ws, size_t ws_bytes, void* stream);
+/* Bytes of workspace of such a call; needs no device. */
+nt_status nt_op_attn_paged_workspace(const nt_kv_pages* cache, int32_t n_heads, int32_t n_seqs, int32_t max_len,
+                                     size_t* bytes);
+
 /* Process-wide switch for nt_translate's graph replay of the decoder step (default on;
  * with 0, every step is launched kernel by kernel). */
 nt_status nt_set_graphs(int32_t enable);

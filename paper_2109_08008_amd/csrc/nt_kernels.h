@@ -247,6 +247,46 @@ struct SelfAttnArgs {
 hipError_t self_attn(DT dt, const SelfAttnArgs& a, hipStream_t s);
 
 // ---------------------------------------------------------------------------------
+// Paged key/value cache (nt_paged.hip).
+struct PagedCache {
+  DT dt;                      // type of queries, new keys/values and outputs
+  int fp8;                    // 1: the pools hold E4M3 bytes (DT::F16 only)
+  int n_kv_heads, d_head;
+  int page_shift;             // page_len = 1 << page_shift, at least 16
+  int n_pages, max_pages;     // of the pools; entries of a sequence's table row
+  void *k, *v;                // [n_pages][n_kv_heads][page_len][d_head]
+  const int* table;           // [n_seqs][max_pages]
+};
+struct KvAppendArgs {
+  PagedCache c;
+  const void *k, *v;          // row i at + i * ld, head h at + h * d_head
+  int ld;
+  const int* off;             // [n_seqs + 1] first new row of each sequence (null: row b is
+  const int* lens;            //   sequence b's only one); [n_seqs] lengths, new rows included
+  int n_seqs, rows;
+};
+hipError_t kv_append(const KvAppendArgs& a, hipStream_t s);
+
+struct PagedAttnArgs {
+  PagedCache c;
+  const void* q;              // sequence b's row at + b * q_ld, head h at + h * d_head
+  int q_ld;
+  const int* lens;            // [n_seqs]
+  void* out;                  // like q, rows out_ld apart
+  int out_ld;
+  int n_seqs, n_heads, max_len;
+  float scale_log2;           // scale * log2(e)
+  // the call's cut (paged_attn_plan): query heads to a key head and blocks of 16 of them;
+  // parts of `chunk` keys; waves that share a part
+  int group, qblocks, parts, chunk, waves;
+  float* part_o;              // parts > 1: [parts][n_seqs][n_heads][d_head] and (max, sum) of each
+  float* part_ml;
+};
+// Fills the cut from c, n_seqs, n_heads and max_len.  Host only.
+void paged_attn_plan(PagedAttnArgs* a);
+hipError_t paged_attn(const PagedAttnArgs& a, hipStream_t s);
+
+// ---------------------------------------------------------------------------------
 // Search.
 struct SearchState {
   int B, beam, V, eos, Tcap;

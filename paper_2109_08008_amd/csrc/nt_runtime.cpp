@@ -1267,6 +1267,63 @@ std::vector<int> length_order(const std::vector<int>& lens) {
   return order;
 }
 
+// --------------------------------------------------------------------------------------
+// paged key/value cache (kernel-level entry points)
+
+// The kernels' view of a caller's cache; `used`: the call reads or writes it (a workspace
+// query does not).
+nt_status paged_cache(const nt_kv_pages* c, bool used, nt::PagedCache* out) {
+  if (!c) return fail(NT_E_INVALID, "null nt_kv_pages");
+  if (c->dtype < NT_F32 || c->dtype > NT_BF16) return fail(NT_E_INVALID, "unknown dtype %d", c->dtype);
+  if (c->fp8 != 0 && c->fp8 != 1) return fail(NT_E_INVALID, "fp8 must be 0 or 1");
+  if (c->fp8 && c->dtype != NT_F16) return fail(NT_E_UNSUPPORTED, "an FP8 cache needs dtype NT_F16");
+  if (c->d_head != 32 && c->d_head != 64 && c->d_head != 128)
+    return fail(NT_E_INVALID, "d_head %d not in {32, 64, 128}", c->d_head);
+  if (c->page_len < 16 || c->page_len > 256 || (c->page_len & (c->page_len - 1)))
+    return fail(NT_E_INVALID, "page_len %d not in {16, 32, 64, 128, 256}", c->page_len);
+  if (c->n_kv_heads < 1 || c->n_kv_heads > 4096) return fail(NT_E_INVALID, "n_kv_heads must be in [1, 4096]");
+  if (c->n_pages < 1 || c->max_pages < 1) return fail(NT_E_INVALID, "n_pages and max_pages must be positive");
+  if (used) {
+    if (!c->d_k || !c->d_v || !c->d_table) return fail(NT_E_INVALID, "null pool or table in nt_kv_pages");
+    if ((reinterpret_cast<uintptr_t>(c->d_k) | reinterpret_cast<uintptr_t>(c->d_v)) & 15)
+      return fail(NT_E_INVALID, "pools must be 16-byte aligned");
+  }
+  int shift = 4;
+  while ((1 << shift) < c->page_len) ++shift;
+  *out = nt::PagedCache{static_cast<DT>(c->dtype), c->fp8, c->n_kv_heads, c->d_head, shift, c->n_pages, c->max_pages,
+                        c->d_k, c->d_v, c->d_table};
+  return NT_OK;
+}
+
+// Rows of `heads` heads, ld elements apart, that the kernels read or write in 16-byte pieces.
+nt_status check_rows(const char* name, const void* p, int ld, int heads, const nt::PagedCache& c) {
+  const size_t eb = nt::dt_bytes(c.dt);
+  if (ld < (long long)heads * c.d_head) return fail(NT_E_INVALID, "rows of %s are shorter than their heads", name);
+  if ((reinterpret_cast<uintptr_t>(p) | ((size_t)ld * eb)) & 15)
+    return fail(NT_E_INVALID, "rows of %s must be 16-byte aligned", name);
+  return NT_OK;
+}
+
+nt_status paged_attn_cut(int n_heads, int n_seqs, int max_len, nt::PagedAttnArgs* a) {
+  if (n_seqs < 0 || max_len < 0) return fail(NT_E_INVALID, "n_seqs and max_len must be >= 0");
+  if (n_heads < 1 || n_heads > 65536 || n_heads % a->c.n_kv_heads)
+    return fail(NT_E_INVALID, "n_heads must be a positive multiple of n_kv_heads");
+  const long long reach = (long long)a->c.max_pages << a->c.page_shift;
+  a->max_len = (int)std::min<long long>(std::min<long long>(max_len, reach), 1 << 30);
+  a->n_seqs = n_seqs;
+  a->n_heads = n_heads;
+  // a launch holds less than 2^24 workgroups of 256 threads (and the join has one a head)
+  const long long tasks = (long long)n_seqs * a->c.n_kv_heads * ((n_heads / a->c.n_kv_heads + 15) / 16);
+  if (tasks >= 1 << 23 || (long long)n_seqs * n_heads >= 1 << 23)
+    return fail(NT_E_UNSUPPORTED, "n_seqs * heads of one call must stay below 8388608");
+  nt::paged_attn_plan(a);
+  return NT_OK;
+}
+
+size_t paged_ws_bytes(const nt::PagedAttnArgs& a) {
+  return a.parts > 1 ? align_up((size_t)a.parts * a.n_seqs * a.n_heads * (a.c.d_head + 2) * sizeof(float)) : 0;
+}
+
 }  // namespace
 
 // ======================================================================================
@@ -1964,6 +2021,68 @@ nt_status nt_op_select_tiled_noalloc(const float* d_logits, int32_t rows, int32_
   const hipStream_t s = static_cast<hipStream_t>(stream);
   NT_HIP(nt::tile_records(d_logits, rows, V, part, s));
   NT_HIP(nt::beam_select_tiles(part, n_tiles, d_logits, nullptr, 1, rows, V, k, d_topv, d_topi, d_lse, s));
+  return NT_OK;
+}
+
+nt_status nt_op_kv_append(const nt_kv_pages* cache, const void* d_k, const void* d_v, int32_t ld,
+                          const int32_t* d_off, const int32_t* d_lens, int32_t n_seqs, int32_t n_rows, void* stream) {
+  g_err.clear();
+  nt::KvAppendArgs a{};
+  NT_TRY(paged_cache(cache, true, &a.c));
+  if (!d_k || !d_v || !d_lens) return fail(NT_E_INVALID, "null argument to nt_op_kv_append");
+  if (n_seqs < 0 || n_rows < 0) return fail(NT_E_INVALID, "n_seqs and n_rows must be >= 0");
+  if (!d_off && n_rows != n_seqs) return fail(NT_E_INVALID, "without d_off every sequence has one new row: n_rows == n_seqs");
+  NT_TRY(check_rows("d_k", d_k, ld, a.c.n_kv_heads, a.c));
+  NT_TRY(check_rows("d_v", d_v, ld, a.c.n_kv_heads, a.c));
+  if (n_seqs == 0 || n_rows == 0) return NT_OK;
+  a.k = d_k;
+  a.v = d_v;
+  a.ld = ld;
+  a.off = d_off;
+  a.lens = d_lens;
+  a.n_seqs = n_seqs;
+  a.rows = n_rows;
+  NT_HIP(nt::kv_append(a, static_cast<hipStream_t>(stream)));
+  return NT_OK;
+}
+
+nt_status nt_op_attn_paged_workspace(const nt_kv_pages* cache, int32_t n_heads, int32_t n_seqs, int32_t max_len,
+                                     size_t* bytes) {
+  g_err.clear();
+  if (!bytes) return fail(NT_E_INVALID, "null argument to nt_op_attn_paged_workspace");
+  nt::PagedAttnArgs a{};
+  NT_TRY(paged_cache(cache, false, &a.c));
+  NT_TRY(paged_attn_cut(n_heads, n_seqs, max_len, &a));
+  *bytes = paged_ws_bytes(a);
+  return NT_OK;
+}
+
+nt_status nt_op_attn_paged(const nt_kv_pages* cache, const void* d_q, int32_t q_ld, int32_t n_heads,
+                           const int32_t* d_lens, int32_t n_seqs, int32_t max_len, float scale, void* d_out,
+                           int32_t out_ld, void* d_ws, size_t ws_bytes, void* stream) {
+  g_err.clear();
+  nt::PagedAttnArgs a{};
+  NT_TRY(paged_cache(cache, true, &a.c));
+  if (!d_q || !d_lens || !d_out) return fail(NT_E_INVALID, "null argument to nt_op_attn_paged");
+  NT_TRY(paged_attn_cut(n_heads, n_seqs, max_len, &a));
+  NT_TRY(check_rows("d_q", d_q, q_ld, n_heads, a.c));
+  NT_TRY(check_rows("d_out", d_out, out_ld, n_heads, a.c));
+  const size_t need = paged_ws_bytes(a);
+  if (need > 0) {
+    if (!d_ws || ws_bytes < need)
+      return fail(NT_E_WORKSPACE, "workspace of %zu bytes required, %zu given", need, d_ws ? ws_bytes : (size_t)0);
+    if (reinterpret_cast<uintptr_t>(d_ws) & 255) return fail(NT_E_INVALID, "workspace must be 256-byte aligned");
+  }
+  if (n_seqs == 0) return NT_OK;
+  a.q = d_q;
+  a.q_ld = q_ld;
+  a.lens = d_lens;
+  a.out = d_out;
+  a.out_ld = out_ld;
+  a.scale_log2 = scale * 1.4426950408889634f;
+  a.part_o = static_cast<float*>(d_ws);
+  a.part_ml = a.part_o + (need ? (size_t)a.parts * n_seqs * n_heads * a.c.d_head : 0);
+  NT_HIP(nt::paged_attn(a, static_cast<hipStream_t>(stream)));
   return NT_OK;
 }
 

@@ -31,7 +31,7 @@ EXPORTS = [
     "nt_free_state", "nt_translate", "nt_last_error", "nt_prof_enable", "nt_prof_reset", "nt_prof_get",
     "nt_op_gemm", "nt_op_gemm_ln", "nt_op_gemm_rows", "nt_prof_config", "nt_set_graphs", "nt_set_beam_fused", "nt_set_streams", "nt_prof_units", "nt_op_select",
     "nt_op_select_tiled", "nt_op_select_tiled_noalloc",
-    "nt_ensemble", "nt_quantize_fp8",
+    "nt_ensemble", "nt_quantize_fp8", "nt_op_kv_append", "nt_op_attn_paged", "nt_op_attn_paged_workspace",
 ]
 NT_ENS_MEAN_LOGP, NT_ENS_LOG_MEAN_P = 0, 1
 NT_SELECT_NOALLOC_MAX_RECORDS = 1 << 20   # include/nt.h: records of nt_op_select_tiled_noalloc
@@ -48,6 +48,12 @@ class nt_search_cfg(ctypes.Structure):
     _fields_ = [("beam", c_int32), ("len_penalty", c_float), ("max_len_a", c_float), ("max_len_b", c_int32),
                 ("max_len_cap", c_int32), ("token_budget", c_int32), ("max_batch_sents", c_int32),
                 ("early_stop", c_int32), ("prune", c_int32)]
+
+
+class nt_kv_pages(ctypes.Structure):
+    _fields_ = [("dtype", c_int32), ("fp8", c_int32), ("n_kv_heads", c_int32), ("d_head", c_int32),
+                ("page_len", c_int32), ("n_pages", c_int32), ("max_pages", c_int32), ("d_k", c_void_p),
+                ("d_v", c_void_p), ("d_table", c_void_p)]
 
 
 class NTError(RuntimeError):
@@ -109,6 +115,11 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
         "nt_op_gemm_ln": (c_int32, [c_int32, P, c_int32, P, c_int32, c_int32, c_int32, P, c_float, P, P, c_int32,
                                     c_int32, c_int32, P, P]),
         "nt_op_gemm_rows": (c_int32, [c_int32] * 8),
+        "nt_op_kv_append": (c_int32, [POINTER(nt_kv_pages), P, P, c_int32, P, P, c_int32, c_int32, P]),
+        "nt_op_attn_paged": (c_int32, [POINTER(nt_kv_pages), P, c_int32, c_int32, P, c_int32, c_int32, c_float, P,
+                                       c_int32, P, c_size_t, P]),
+        "nt_op_attn_paged_workspace": (c_int32, [POINTER(nt_kv_pages), c_int32, c_int32, c_int32,
+                                                 POINTER(c_size_t)]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(L, name)
@@ -308,6 +319,30 @@ def nt_op_select_tiled_noalloc(d_logits: int, rows: int, V: int, k: int, d_topv:
                                stream=None):
     _check(load_library().nt_op_select_tiled_noalloc(c_void_p(d_logits), rows, V, k, c_void_p(d_topv),
                                                      c_void_p(d_topi), c_void_p(d_lse), _stream(stream)))
+
+
+def kv_pages(dtype: str, n_kv_heads: int, d_head: int, page_len: int, n_pages: int, max_pages: int, d_k: int, d_v: int,
+             d_table: int, fp8: bool = False) -> nt_kv_pages:
+    """A paged cache over the caller's pools and page table (device addresses; kept alive by the caller)."""
+    return nt_kv_pages(DTYPES[dtype], int(fp8), n_kv_heads, d_head, page_len, n_pages, max_pages, d_k, d_v, d_table)
+
+
+def nt_op_kv_append(cache: nt_kv_pages, d_k: int, d_v: int, ld: int, d_off, d_lens: int, n_seqs: int, n_rows: int,
+                    stream=None):
+    _check(load_library().nt_op_kv_append(ctypes.byref(cache), d_k, d_v, ld, d_off, d_lens, n_seqs, n_rows,
+                                          _stream(stream)))
+
+
+def nt_op_attn_paged_workspace(cache: nt_kv_pages, n_heads: int, n_seqs: int, max_len: int) -> int:
+    b = c_size_t()
+    _check(load_library().nt_op_attn_paged_workspace(ctypes.byref(cache), n_heads, n_seqs, max_len, ctypes.byref(b)))
+    return b.value
+
+
+def nt_op_attn_paged(cache: nt_kv_pages, d_q: int, q_ld: int, n_heads: int, d_lens: int, n_seqs: int, max_len: int,
+                     scale: float, d_out: int, out_ld: int, d_ws=None, ws_bytes: int = 0, stream=None):
+    _check(load_library().nt_op_attn_paged(ctypes.byref(cache), d_q, q_ld, n_heads, d_lens, n_seqs, max_len, scale,
+                                           d_out, out_ld, d_ws, ws_bytes, _stream(stream)))
 
 
 def nt_prof_enable(mask: int):

@@ -1,0 +1,356 @@
+"""GPU: the paged key/value cache, nt_op_kv_append and nt_op_attn_paged, against float64."""
+import numpy as np
+import pytest
+
+from tests.paged_util import Pages, assert_within, attend, torch_dtype
+
+pytestmark = pytest.mark.gpu
+
+TYPES = [("f16", False), ("bf16", False), ("f32", False), ("f16", True)]
+
+
+def _q(n, heads, d_head, dtype, seed, pad=0):
+    import torch
+    g = torch.Generator().manual_seed(seed)
+    wide = torch.full((n, heads * d_head + pad), float("nan"), dtype=torch_dtype(dtype))
+    wide[:, :heads * d_head] = torch.randn(n, heads * d_head, generator=g).to(wide.dtype)
+    return wide.cuda()[:, :heads * d_head].unflatten(1, (heads, d_head))
+
+
+# ---- append ----------------------------------------------------------------------------
+def _append_expected(pages, k, v, off, lens, n_rows):
+    """The pools after the call, from the rows as the documentation places them."""
+    import torch
+    out = []
+    for pool, x in ((pages.k, k), (pages.v, v)):
+        p = pool.cpu().clone()
+        x = x.cpu().view(k.shape[0], pages.kv_heads, pages.d_head)
+        if pages.fp8:
+            x = x.float().clamp(-448, 448).to(torch.float8_e4m3fn).view(torch.uint8)
+        for b in range(len(lens)):
+            lo, hi = (b, b + 1) if off is None else (off[b], off[b + 1])
+            for i in range(lo, min(hi, n_rows)):
+                pos = lens[b] - (hi - i)
+                if pos < 0 or pos >= pages.max_pages * pages.page:
+                    continue
+                pid = int(pages.table_np[b, pos // pages.page])
+                if 0 <= pid < pages.n_pages:
+                    p[pid, :, pos % pages.page] = x[i]
+        out.append(p)
+    return out
+
+
+def _append(pages, x, off, n_rows, lens=None):
+    import torch
+    from paper_2109_08008_amd import nt
+    w = pages.kv_heads * pages.d_head
+    d_off = None if off is None else torch.tensor(off, dtype=torch.int32, device="cuda")
+    eb = x.element_size()
+    nt.nt_op_kv_append(pages.cache, x.data_ptr() + w * eb, x.data_ptr() + 2 * w * eb, x.stride(0),
+                       None if d_off is None else d_off.data_ptr(), (pages.lens if lens is None else lens).data_ptr(),
+                       len(pages.lens_list), n_rows)
+    torch.cuda.synchronize()
+
+
+def _same(a, b):
+    """Bitwise (NaN cells included)."""
+    import torch
+    as_int = {1: torch.uint8, 2: torch.int16, 4: torch.int32}[a.element_size()]
+    return torch.equal(a.cpu().view(as_int), b.cpu().view(as_int))
+
+
+@pytest.mark.parametrize("dtype,fp8", TYPES)
+@pytest.mark.parametrize("kv_heads,d_head,page", [(1, 32, 16), (3, 64, 16), (8, 64, 32), (5, 128, 256), (16, 128, 64)])
+def test_append_places_rows(dtype, fp8, kv_heads, d_head, page):
+    """Ragged new rows (none, one, more than a page), rows before the first and behind the last
+    sequence, and every other cell left as it was, bit for bit."""
+    import torch
+    new = [0, 1, 37, 0, 2, 300, 16, 1]
+    lens = [0, 1, 40, 9, 700, 300, 31, 257]
+    off = np.concatenate([[2], 2 + np.cumsum(new)]).tolist()
+    rows = off[-1] + 3
+    pages = Pages(lens, kv_heads, d_head, page, dtype, fp8, seed=1)
+    g = torch.Generator().manual_seed(5)
+    w = kv_heads * d_head
+    x = (torch.randn(rows, 3 * w + 16, generator=g) * 3).to(torch_dtype(dtype))
+    x[5, :] = 1000.0            # E4M3 saturates
+    x = x.cuda()
+    want = _append_expected(pages, x[:, w:2 * w].contiguous(), x[:, 2 * w:3 * w].contiguous(), off, lens, rows)
+    _append(pages, x, off, rows)
+    assert _same(pages.k, want[0]) and _same(pages.v, want[1])
+
+
+@pytest.mark.parametrize("dtype,fp8", TYPES)
+@pytest.mark.parametrize("n", [1, 3, 64, 129, 5000])
+def test_append_one_token_each(dtype, fp8, n):
+    import torch
+    rng = np.random.default_rng(n)
+    lens = rng.integers(0, 40, n).tolist()
+    pages = Pages(lens, 2, 64, 16, dtype, fp8, seed=n)
+    x = torch.randn(n, 3 * 128, generator=torch.Generator().manual_seed(n)).to(torch_dtype(dtype)).cuda()
+    want = _append_expected(pages, x[:, 128:256].contiguous(), x[:, 256:].contiguous(), None, lens, n)
+    _append(pages, x, None, n)
+    assert _same(pages.k, want[0]) and _same(pages.v, want[1])
+
+
+def test_append_many_sequences_search():
+    """More sequences than two rounds of 64 probes, most without a row."""
+    import torch
+    n = 9000
+    rng = np.random.default_rng(3)
+    new = (rng.random(n) < 0.05).astype(int) * rng.integers(1, 5, n)
+    new[[0, n - 1]] = [2, 3]
+    lens = (new + rng.integers(0, 3, n)).tolist()
+    off = np.concatenate([[0], np.cumsum(new)]).tolist()
+    pages = Pages(lens, 1, 32, 16, "bf16", seed=2)
+    x = torch.randn(off[-1], 96, generator=torch.Generator().manual_seed(1)).to(torch.bfloat16).cuda()
+    want = _append_expected(pages, x[:, 32:64].contiguous(), x[:, 64:].contiguous(), off, lens, off[-1])
+    _append(pages, x, off, off[-1])
+    assert _same(pages.k, want[0]) and _same(pages.v, want[1])
+
+
+def test_append_leaves_out_what_has_no_place():
+    """Holes and page ids out of range, positions past the table and below 0, an inactive slot,
+    offsets that claim more rows than there are."""
+    import torch
+    lens = [20, 33, 16, 5, 64]
+    pages = Pages(lens, 2, 32, 16, "f16", seed=4)
+    table = pages.table_np.copy()
+    table[0, 1] = -1
+    table[1, 2] = pages.n_pages
+    table[1, 0] = 2 ** 31 - 1
+    pages.retable(table)
+    given = [20, 33, 200, -4, 64]      # past max_pages * page_len = 64; below 0
+    pages.lens = torch.tensor(given, dtype=torch.int32, device="cuda")
+    off = [0, 20, 53, 60, 62, 126]
+    rows = 100                         # fewer than off says
+    x = torch.randn(rows, 192, generator=torch.Generator().manual_seed(1)).half().cuda()
+    want = _append_expected(pages, x[:, 64:128].contiguous(), x[:, 128:].contiguous(), off, given, rows)
+    _append(pages, x, off, rows)
+    assert _same(pages.k, want[0]) and _same(pages.v, want[1])
+
+
+# ---- attention -------------------------------------------------------------------------
+EDGE = [1, 15, 16, 17, 31, 32, 33, 0, 64, 65, 127, 128, 129, 191, 255, 256, 257]
+
+
+@pytest.mark.parametrize("dtype,fp8", TYPES)
+@pytest.mark.parametrize("d_head", [32, 64, 128])
+@pytest.mark.parametrize("page", [16, 32, 128])
+def test_attention_at_the_edges(dtype, fp8, d_head, page):
+    """Lengths on both sides of every block, tile and page edge; empty rows; everything that no
+    sequence holds is NaN."""
+    pages = Pages(EDGE, 2, d_head, page, dtype, fp8, seed=d_head + page).fill(1)
+    q = _q(len(EDGE), 4, d_head, dtype, 2, pad=8)
+    got = attend(pages, q, d_head ** -0.5)
+    want, bound = pages.attention(q, d_head ** -0.5)
+    assert_within(got, want, bound)
+    assert (got[EDGE.index(0)] == 0).all()
+
+
+@pytest.mark.parametrize("dtype,fp8", TYPES)
+@pytest.mark.parametrize("kv_heads,group", [(1, 1), (3, 1), (2, 3), (1, 8), (2, 16), (1, 17), (1, 33), (2, 40)])
+def test_attention_shared_heads(dtype, fp8, kv_heads, group):
+    pages = Pages([70, 3, 200], kv_heads, 64, 16, dtype, fp8, seed=group).fill(3)
+    q = _q(3, kv_heads * group, 64, dtype, 4)
+    got = attend(pages, q, 0.125)
+    assert_within(got, *pages.attention(q, 0.125))
+
+
+@pytest.mark.parametrize("dtype,fp8", TYPES)
+@pytest.mark.parametrize("d_head", [32, 64, 128])
+@pytest.mark.parametrize("lens", [[5000], [1, 3000, 0, 769], [2049, 2048, 2047]])
+def test_attention_split_over_the_length(dtype, fp8, d_head, lens):
+    """Few tasks: the length is divided over workgroups and joined."""
+    from paper_2109_08008_amd import nt
+    pages = Pages(lens, 1, d_head, 64, dtype, fp8, seed=sum(lens)).fill(5)
+    assert nt.nt_op_attn_paged_workspace(pages.cache, 2, len(lens), max(lens)) > 0
+    q = _q(len(lens), 2, d_head, dtype, 6)
+    got = attend(pages, q, d_head ** -0.5)
+    assert_within(got, *pages.attention(q, d_head ** -0.5))
+
+
+@pytest.mark.parametrize("n_seqs,max_len", [(1, 130), (1, 4096), (40, 300), (700, 260)])
+def test_attention_lengths_below_the_bound(n_seqs, max_len):
+    """max_len may be far above the lengths (parts with nothing to do), or below the table's
+    reach; lengths above it are cut there."""
+    rng = np.random.default_rng(n_seqs)
+    lens = rng.integers(0, min(max_len, 300), n_seqs).tolist()
+    lens[0] = 129
+    pages = Pages(lens, 2, 32, 32, "f16", seed=9, extra_pages=max_len // 32).fill(7)
+    q = _q(n_seqs, 2, 32, "f16", 8)
+    got = attend(pages, q, 0.2, max_len=max_len)
+    assert_within(got, *pages.attention(q, 0.2))
+    got = attend(pages, q, 0.2, max_len=100)
+    assert_within(got, *pages.attention(q, 0.2, lens=[min(n, 100) for n in lens]))
+
+
+@pytest.mark.parametrize("dtype,fp8", TYPES)
+@pytest.mark.parametrize("lens", [[200, 64, 40, 96], [3000, 64, 40, 2000]])
+def test_attention_over_holes(dtype, fp8, lens):
+    """Entries outside the pool are left out: a first page, a middle one, a last one, all; and
+    lengths past the table's end or below 0."""
+    import torch
+    pages = Pages(lens, 1, 64, 16, dtype, fp8, seed=11).fill(9)
+    table = pages.table_np.copy()
+    table[0, [0, 5, 6, 12]] = [-1, pages.n_pages, -7, 2 ** 31 - 1]
+    table[1] = -1
+    table[2, :2] = -1
+    pages.retable(table)
+    pages.lens_list = [lens[0], 64, 40, -3]
+    pages.lens = torch.tensor([lens[0] + 0, 64, 40, -3], dtype=torch.int32, device="cuda")
+    q = _q(4, 2, 64, dtype, 10)
+    got = attend(pages, q, 0.125, max_len=max(lens))
+    assert_within(got, *pages.attention(q, 0.125))
+    assert (got[1] == 0).all() and (got[3] == 0).all()
+    pages.lens = torch.tensor([2 ** 31 - 1, 64, 40, -2 ** 31], dtype=torch.int32, device="cuda")   # cut at max_len
+    again = attend(pages, q, 0.125, max_len=lens[0])
+    assert torch.equal(again, got) or lens[0] < max(lens)
+
+
+def test_attention_leaves_other_rows():
+    """Rows behind the last sequence, and what lies between the rows, stay as they were."""
+    import torch
+    for lens in ([40, 3], [4000, 3]):
+        pages = Pages(lens, 1, 64, 16, "f16", seed=1).fill(1)
+        q = _q(5, 2, 64, "f16", 1)
+        wide = torch.full((5, 2 * 64 + 24), 7.0, dtype=torch.float16, device="cuda")
+        out = wide[:, :128].unflatten(1, (2, 64))
+        attend(pages, q, 0.125, n_seqs=2, out=out)
+        assert_within(out[:2], *pages.attention(q[:2], 0.125))
+        assert (wide[2:] == 7).all() and (wide[:, 128:] == 7).all()
+
+
+def test_attention_extreme_scores():
+    """Scores far apart (all weight on one key), equal scores, large values, infinite values at
+    positions that are not attended to, and an infinite value that is."""
+    import torch
+    pages = Pages([300, 300, 50], 1, 64, 16, "f16", seed=3).fill(3)
+    for b, j in ((0, 17), (1, 299)):
+        pages.k[int(pages.table_np[b, j // 16]), 0, j % 16] = 60.0
+    pages.k[[int(x) for x in pages.table_np[2, :4]]] = 0.0
+    pages.v[int(pages.table_np[2, 3]), 0, 2:] = float("inf")      # positions 50..: behind the length
+    q = _q(3, 1, 64, "f16", 3).abs()
+    q[0] = 10.0
+    got = attend(pages, q, 1.0)
+    want, bound = pages.attention(q, 1.0)
+    assert_within(got, want, bound)
+    pages.v[int(pages.table_np[2, 0]), 0, 5, 9] = float("inf")
+    got = attend(pages, q, 1.0)
+    assert got[2, 0, 9] == float("inf") and torch.isfinite(got[2, 0, :9]).all() and torch.isfinite(got[2, 0, 10:]).all()
+
+
+def test_attention_over_shared_pages():
+    """Hypotheses whose rows of the table name the same pages for a common prefix."""
+    pages = Pages([90, 90, 90], 2, 32, 16, "bf16", seed=6).fill(6)
+    table = pages.table_np.copy()
+    table[1, :5] = table[0, :5]
+    table[2, :3] = table[0, :3]
+    pages.retable(table)
+    pages.fill(8)
+    q = _q(3, 2, 32, "bf16", 6)
+    got = attend(pages, q, 0.3)
+    assert_within(got, *pages.attention(q, 0.3))
+
+
+def test_attention_past_32_bit_offsets():
+    """Pages beyond 2^32 elements (and 2^33 bytes) of a pool, written and read."""
+    import torch
+    from paper_2109_08008_amd import nt
+    page, hkv, dh = 256, 16, 128
+    n_pages = (1 << 32) // (page * hkv * dh) + 3
+    k = torch.empty(n_pages, hkv, page, dh, dtype=torch.float16, device="cuda")
+    v = torch.empty_like(k)
+    lens = [300, 2]
+    small = Pages(lens, hkv, dh, page, "f16", seed=2)
+    for pool in (k, v):
+        pool[n_pages - 4:] = float("nan")
+    table = np.array([[n_pages - 1, n_pages - 3], [n_pages - 2, -1]], dtype=np.int32)
+    d_table = torch.from_numpy(table).cuda()
+    cache = nt.kv_pages("f16", hkv, dh, page, n_pages, 2, k.data_ptr(), v.data_ptr(), d_table.data_ptr())
+    w = hkv * dh
+    x = torch.randn(302, 3 * w, generator=torch.Generator().manual_seed(2)).half().cuda()
+    off = torch.tensor([0, 300, 302], dtype=torch.int32, device="cuda")
+    nt.nt_op_kv_append(cache, x.data_ptr() + 2 * w, x.data_ptr() + 4 * w, 3 * w, off.data_ptr(), small.lens.data_ptr(), 2, 302)
+    # the same through a small pool
+    _append(small, x, [0, 300, 302], 302)
+    for b, j in ((0, 0), (0, 1), (1, 0)):
+        assert _same(k[int(table[b, j])], small.k[int(small.table_np[b, j])])
+        assert _same(v[int(table[b, j])], small.v[int(small.table_np[b, j])])
+    q = _q(2, hkv, dh, "f16", 1)
+    want = attend(small, q, 0.09)
+    out = torch.empty_like(want)
+    need = nt.nt_op_attn_paged_workspace(cache, hkv, 2, 300)
+    ws = torch.empty(max(need, 256), dtype=torch.uint8, device="cuda")
+    nt.nt_op_attn_paged(cache, q.data_ptr(), w, hkv, small.lens.data_ptr(), 2, 300, 0.09, out.data_ptr(), w, ws.data_ptr(), need)
+    assert _same(out, want)
+
+
+@pytest.mark.parametrize("lens", [[30, 31, 32], [1500, 2, 700]])
+def test_step_captured_and_replayed(lens):
+    """Append and attention captured into one graph and replayed over new rows and lengths; eager
+    work of the same kind between the replays; every replay equals the eager result."""
+    import torch
+    page, hkv, heads, dh, n = 32, 2, 4, 64, 3
+    steps = 4
+    cap = max(lens) + steps
+    pages = Pages([cap] * n, hkv, dh, page, "f16", seed=1)
+    eager = Pages([cap] * n, hkv, dh, page, "f16", seed=1)
+    for p in (pages, eager):
+        p.fill(2)
+    w = hkv * dh
+    x = torch.empty(n, 3 * w, dtype=torch.float16, device="cuda")
+    q = _q(n, heads, dh, "f16", 1)
+    cur = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    out = torch.empty(n, heads, dh, dtype=torch.float16, device="cuda")
+    from paper_2109_08008_amd import nt
+    need = nt.nt_op_attn_paged_workspace(pages.cache, heads, n, cap)
+    ws = torch.empty(max(need, 256), dtype=torch.uint8, device="cuda")
+
+    def step(p, o, work):
+        nt.nt_op_kv_append(p.cache, x.data_ptr() + 2 * w, x.data_ptr() + 4 * w, 3 * w, None, cur.data_ptr(), n, n)
+        nt.nt_op_attn_paged(p.cache, q.data_ptr(), heads * dh, heads, cur.data_ptr(), n, cap, 0.125, o.data_ptr(), heads * dh,
+                            work.data_ptr(), work.numel())
+
+    side = torch.cuda.Stream()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        step(pages, out, ws)
+    for t in range(steps):
+        cur.fill_(0)
+        cur += torch.tensor(lens, dtype=torch.int32, device="cuda") + t
+        x.copy_(torch.randn(n, 3 * w, generator=torch.Generator().manual_seed(t)).half())
+        graph.replay()
+        want = torch.empty_like(out)
+        step(eager, want, torch.empty_like(ws))
+        torch.cuda.synchronize()
+        assert _same(out, want) and _same(pages.k, eager.k) and _same(pages.v, eager.v)
+
+
+def test_two_streams_with_their_own_workspaces():
+    import torch
+    pages = Pages([3000, 800], 2, 64, 32, "bf16", seed=4).fill(4)
+    q = [_q(2, 4, 64, "bf16", s) for s in (1, 2)]
+    want = [attend(pages, x, 0.125) for x in q]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in q]
+    got = [torch.empty_like(want[0]) for _ in range(6)]
+    ws = [torch.empty(1 << 22, dtype=torch.uint8, device="cuda") for _ in q]
+    for i in range(6):
+        attend(pages, q[i % 2], 0.125, out=got[i], ws=ws[i % 2], stream=streams[i % 2].cuda_stream)
+    torch.cuda.synchronize()
+    for i in range(6):
+        assert _same(got[i], want[i % 2])
+
+
+def test_undersized_workspace_is_reported():
+    import torch
+    from paper_2109_08008_amd import nt
+    pages = Pages([4000], 1, 64, 16, "f16", seed=1).fill(1)
+    q = _q(1, 1, 64, "f16", 1)
+    need = nt.nt_op_attn_paged_workspace(pages.cache, 1, 1, 4000)
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    for ptr, size in ((ws.data_ptr(), need - 1), (None, need)):
+        with pytest.raises(nt.NTError) as e:
+            nt.nt_op_attn_paged(pages.cache, q.data_ptr(), 64, 1, pages.lens.data_ptr(), 1, 4000, 0.1, q.data_ptr(), 64, ptr, size)
+        assert e.value.status == nt.NT_E_WORKSPACE and str(need) in e.value.message

@@ -14,6 +14,15 @@
 
 namespace nt {
 namespace {
+typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+
+// E4M3 codes of four values, e4m3_rne's: the hardware's conversion rounds to nearest even and keeps
+// subnormals, but does not saturate (a NaN passes the comparisons and gives 0x7F).
+__device__ __forceinline__ unsigned e4m3_4(float a, float b, float c, float d) {
+  auto sat = [](float x) { return x > 448.f ? 448.f : x < -448.f ? -448.f : x; };
+  const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(sat(a), sat(b), 0, false);
+  return (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(sat(c), sat(d), lo, true);
+}
 
 // ---- append ----------------------------------------------------------------------------
 // One wave a new row: the row's keys and values in 16-byte pieces, each to its head's page.
@@ -33,8 +42,8 @@ __global__ __launch_bounds__(256) void kv_append_kernel(KvAppendArgs a) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int p = min(p0 + u * kWave + lane, pieces - 1);   // (past the last: again, not stored)
-      kq[u] = *reinterpret_cast<const u32x4*>(k + p * VN);
-      vq[u] = *reinterpret_cast<const u32x4*>(v + p * VN);
+      kq[u] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(k + p * VN));
+      vq[u] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(v + p * VN));
     }
   };
   load(0);
@@ -70,13 +79,11 @@ __global__ __launch_bounds__(256) void kv_append_kernel(KvAppendArgs a) {
         static_assert(VN == 8, "E4M3 caches take 16-bit rows");
         auto codes = [](u32x4 q) {
           const half8 e = __builtin_bit_cast(half8, q);
-          unsigned w[2] = {0, 0};
-#pragma unroll
-          for (int i = 0; i < 8; ++i) w[i / 4] |= (unsigned)e4m3_rne((float)e[i]) << (i % 4 * 8);
-          return make_uint2(w[0], w[1]);
+          return u32x2{e4m3_4((float)e[0], (float)e[1], (float)e[2], (float)e[3]),
+                       e4m3_4((float)e[4], (float)e[5], (float)e[6], (float)e[7])};
         };
-        *reinterpret_cast<uint2*>(static_cast<uint8_t*>(a.c.k) + at) = codes(kq[u]);
-        *reinterpret_cast<uint2*>(static_cast<uint8_t*>(a.c.v) + at) = codes(vq[u]);
+        *reinterpret_cast<u32x2*>(static_cast<uint8_t*>(a.c.k) + at) = codes(kq[u]);
+        *reinterpret_cast<u32x2*>(static_cast<uint8_t*>(a.c.v) + at) = codes(vq[u]);
       } else {
         *reinterpret_cast<u32x4*>(static_cast<T*>(a.c.k) + at) = kq[u];
         *reinterpret_cast<u32x4*>(static_cast<T*>(a.c.v) + at) = vq[u];
@@ -105,7 +112,6 @@ __global__ __launch_bounds__(256) void kv_append_kernel(KvAppendArgs a) {
 // take its 32-key tiles in turn and join in LDS at the end.  A length is split into parts of
 // `chunk` keys over workgroups when there are few tasks; the parts' (max, sum, unnormalised
 // output) go to the workspace and paged_join_kernel merges them.
-constexpr int TK = 32;          // keys of a tile
 constexpr float LOG2E = 1.4426950408889634f;
 
 typedef short short4v __attribute__((ext_vector_type(4)));
@@ -115,22 +121,29 @@ __device__ __forceinline__ uint2 lds_column4(const unsigned char* p) {
   return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
                                        (__attribute__((address_space(3))) short4v*)(p)));
 }
+__device__ __forceinline__ void wave_fence() {   // orders a wave's own LDS accesses
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+}
 
 template <typename T, int DH, typename KV, int SW>
 __global__ __launch_bounds__(256) void paged_attn_kernel(PagedAttnArgs a) {
   constexpr int EB = sizeof(T), EC = sizeof(KV);
   constexpr bool F8 = EC == 1;
+  constexpr int TK = EB == 2 ? 32 : 16;               // keys of a tile: one MFMA step of P.V
+  constexpr int NB = TK / 16;                         // 16-key blocks
   constexpr int QK = DH * EB / 64;                    // MFMA steps over the channels
-  constexpr int KB = F8 && DH == 32 ? 8 : 16;         // bytes a lane loads at once of a key
-  constexpr int NKL = DH * EC / (4 * KB);             // such loads a 16-key block
-  constexpr int ROWP = DH * EC / 16;                  // 16-byte pieces of a value
-  constexpr int VPL = TK * ROWP / kWave;              // pieces a lane takes of a tile's values
   constexpr int CB = DH / 16;                         // blocks of 16 channels of the output
-  constexpr int VSTR = DH * EB / 4 + (EB == 2 ? 8 : 4);   // LDS row (dwords): no bank conflicts
-  constexpr int VBYTES = TK * VSTR * 4;
-  static_assert(TK * ROWP % kWave == 0, "a tile's values split evenly over the lanes");
-  static_assert(SW * 16 * DH * 4 <= 4 * VBYTES || SW == 1, "the joined outputs fit in the values' LDS");
-  __shared__ __attribute__((aligned(16))) unsigned char lds[4 * VBYTES];
+  constexpr int RB = DH * EC;                         // bytes of a key
+  constexpr int ROWP = RB / 16;                       // 16-byte pieces of a key
+  constexpr int NP = TK * ROWP / kWave;               // pieces a lane takes of a tile's keys
+  constexpr int RPL = kWave / ROWP;                   // rows that one load of the wave covers
+  // LDS rows, padded against bank conflicts
+  constexpr int KSTR = RB + 16, VSTR = DH * EB + (EB == 2 ? 32 : 16);
+  constexpr int KBYTES = TK * KSTR, WBYTES = KBYTES + TK * VSTR;
+  static_assert(TK * ROWP % kWave == 0, "a tile's rows split evenly over the lanes");
+  static_assert(16 * DH * 4 <= WBYTES || SW == 1, "the outputs to join fit in the tiles' LDS");
+  __shared__ __attribute__((aligned(16))) unsigned char lds[4 * WBYTES];
   __shared__ float jm[4][16], jl[4][16];
 
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
@@ -159,53 +172,42 @@ __global__ __launch_bounds__(256) void paged_attn_kernel(PagedAttnArgs a) {
 
   const int sh = a.c.page_shift, slots = 1 << sh;
   const int* table = a.c.table + (size_t)b * a.c.max_pages;
-  const size_t head_bytes = (size_t)DH * EC << sh;    // a head's share of a page
+  const size_t head_bytes = (size_t)RB << sh;         // a head's share of a page
   const char* Kp = static_cast<const char*>(a.c.k) + hk * head_bytes;
   const char* Vp = static_cast<const char*>(a.c.v) + hk * head_bytes;
   const size_t page_bytes = head_bytes * a.c.n_kv_heads;
 
-  struct Pages { int id[2]; };                        // of a tile's two 16-key blocks; -1: none
+  struct Pages { int id[NB]; };                       // of a tile's 16-key blocks; -1: none
   auto pages_of = [&](int t) {
     Pages p;
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
+    for (int j = 0; j < NB; ++j) {
       const int key = t + 16 * j;
       const int id = table[min(key >> sh, a.c.max_pages - 1)];
       p.id[j] = key < len && (unsigned)id < (unsigned)a.c.n_pages ? id : -1;
     }
     return p;
   };
-  u32x4 kr[2][NKL], vr[VPL];
-  auto load_k = [&](int t, const Pages& p) {          // (of a hole: some page's, masked below)
+  // A tile's rows of a pool, whole lines a load: lane l takes piece l % ROWP of row l / ROWP + RPL u.
+  // Rows behind the length re-read the last one; of a hole, some page's (both masked below).
+  const int row0 = lane / ROWP, col = lane % ROWP * 16;
+  auto load = [&](const char* pool, int t, const Pages& p, u32x4 (&r)[NP]) {
+    const char* at[NB];
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const char* row = Kp + max(p.id[j], 0) * page_bytes + (size_t)(((t + 16 * j) & (slots - 1)) + ln) * (DH * EC);
+    for (int j = 0; j < NB; ++j) at[j] = pool + max(p.id[j], 0) * page_bytes + (size_t)((t + 16 * j) & (slots - 1)) * RB + col;
+    const int last = len - 1 - t;
+    if (last >= TK - 1) {
 #pragma unroll
-      for (int i = 0; i < NKL; ++i) {
-        if constexpr (KB == 16) {
-          kr[j][i] = *reinterpret_cast<const u32x4*>(row + i * 64 + grp * 16);
-        } else {
-          const uint2 w = *reinterpret_cast<const uint2*>(row + i * 32 + grp * 8);
-          kr[j][i] = u32x4{w.x, w.y, 0, 0};
-        }
+      for (int u = 0; u < NP; ++u) {
+        const int row = row0 + u * RPL;
+        r[u] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(
+            (RPL <= 16 ? at[u * RPL / 16] : at[NB > 1 && row >= 16]) + (row & 15) * RB));
       }
-    }
-  };
-  auto load_v = [&](int t, const Pages& p) {
-    const char* at[2];
+    } else {
 #pragma unroll
-    for (int j = 0; j < 2; ++j) at[j] = Vp + max(p.id[j], 0) * page_bytes + (size_t)((t + 16 * j) & (slots - 1)) * (DH * EC);
-#pragma unroll
-    for (int u = 0; u < VPL; ++u) {
-      const int pc = lane + u * kWave, row = pc / ROWP, col = pc % ROWP;
-      vr[u] = *reinterpret_cast<const u32x4*>((row < 16 ? at[0] : at[1]) + (row & 15) * (DH * EC) + col * 16);
-    }
-    // what lies behind the length, or on no page, may be anything: no 0 * NaN from it
-    if (t + TK > len || (p.id[0] | p.id[1]) < 0) {
-#pragma unroll
-      for (int u = 0; u < VPL; ++u) {
-        const int row = (lane + u * kWave) / ROWP;
-        if (t + row >= len || p.id[row >> 4] < 0) vr[u] = u32x4{0, 0, 0, 0};
+      for (int u = 0; u < NP; ++u) {
+        const int row = min(row0 + u * RPL, last);
+        r[u] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(at[NB > 1 && row >= 16] + (row & 15) * RB));
       }
     }
   };
@@ -214,44 +216,58 @@ __global__ __launch_bounds__(256) void paged_attn_kernel(PagedAttnArgs a) {
   floatx4 o[CB];                                      // O[head 4 * grp + r][c * 16 + ln]
 #pragma unroll
   for (int c = 0; c < CB; ++c) o[c] = floatx4{0.f, 0.f, 0.f, 0.f};
-  unsigned char* vs = lds + wave * VBYTES;
+  unsigned char* ks = lds + wave * WBYTES;
+  unsigned char* vs = ks + KBYTES;
 
+  u32x4 kr[NP], vr[NP];
   const int step = SW * TK;
   int t = c0 + (SW == 1 ? 0 : wave * TK);
   if (t < c1) {
     Pages pg = pages_of(t);
-    load_k(t, pg);
-    load_v(t, pg);
+    load(Kp, t, pg, kr);
+    load(Vp, t, pg, vr);
     for (;;) {
       const int tn = t + step;
       const bool more = tn < c1;
       Pages pn = pg;
       if (more) pn = pages_of(tn);
-      floatx4 sc[2];
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
+      for (int u = 0; u < NP; ++u) *reinterpret_cast<u32x4*>(ks + (row0 + u * RPL) * KSTR + col) = kr[u];
+      if (more) load(Kp, tn, pn, kr);
+      wave_fence();
+      floatx4 sc[NB];
+#pragma unroll
+      for (int j = 0; j < NB; ++j) {
+        const unsigned char* krow = ks + (16 * j + ln) * KSTR;
         floatx4 acc = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int st = 0; st < QK; ++st) {
           u32x4 kf;
           if constexpr (!F8) {
-            kf = kr[j][st];
+            kf = *reinterpret_cast<const u32x4*>(krow + st * 64 + grp * 16);
           } else if constexpr (DH == 32) {
-            kf = f8_to_f16x8(kr[j][st].x, kr[j][st].y);
+            const uint2 w = *reinterpret_cast<const uint2*>(krow + grp * 8);
+            kf = f8_to_f16x8(w.x, w.y);
           } else {
-            const u32x4 w = kr[j][st / 2];
-            kf = st % 2 ? f8_to_f16x8(w.z, w.w) : f8_to_f16x8(w.x, w.y);
+            const uint2 w = *reinterpret_cast<const uint2*>(krow + st / 2 * 64 + grp * 16 + st % 2 * 8);
+            kf = f8_to_f16x8(w.x, w.y);
           }
           acc = Mfma<T>::step(kf, qf[st], acc);
         }
         sc[j] = acc;
       }
-      if (more) load_k(tn, pn);
-      // the tile's values to LDS, in the model dtype
+      // the tile's values to LDS, in the model dtype.  What lies behind the length, or on no page,
+      // may be anything: no 0 * NaN from it
+      if (t + TK > len || pg.id[0] < 0 || pg.id[NB - 1] < 0) {
 #pragma unroll
-      for (int u = 0; u < VPL; ++u) {
-        const int pc = lane + u * kWave, row = pc / ROWP, col = pc % ROWP;
-        unsigned char* d = vs + row * (VSTR * 4) + col * (F8 ? 32 : 16);
+        for (int u = 0; u < NP; ++u) {
+          const int row = row0 + u * RPL;
+          if (t + row >= len || (NB > 1 && row >= 16 ? pg.id[NB - 1] : pg.id[0]) < 0) vr[u] = u32x4{0, 0, 0, 0};
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < NP; ++u) {
+        unsigned char* d = vs + (row0 + u * RPL) * VSTR + col * (F8 ? 2 : 1);
         if constexpr (F8) {
           *reinterpret_cast<u32x4*>(d) = f8_to_f16x8(vr[u].x, vr[u].y);
           *reinterpret_cast<u32x4*>(d + 16) = f8_to_f16x8(vr[u].z, vr[u].w);
@@ -259,16 +275,16 @@ __global__ __launch_bounds__(256) void paged_attn_kernel(PagedAttnArgs a) {
           *reinterpret_cast<u32x4*>(d) = vr[u];
         }
       }
+      if (more) load(Vp, tn, pn, vr);
       float cmax = -INFINITY;
 #pragma unroll
-      for (int j = 0; j < 2; ++j)
+      for (int j = 0; j < NB; ++j)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           const int key = t + 16 * j + 4 * grp + r;
           sc[j][r] = key < len && pg.id[j] >= 0 ? sc[j][r] * a.scale_log2 : -INFINITY;
           cmax = fmaxf(cmax, sc[j][r]);
         }
-      if (more) load_v(tn, pn);
       cmax = fmaxf(cmax, __shfl_xor(cmax, 16, kWave));
       cmax = fmaxf(cmax, __shfl_xor(cmax, 32, kWave));
       const float mn = fmaxf(m, cmax);
@@ -276,7 +292,7 @@ __global__ __launch_bounds__(256) void paged_attn_kernel(PagedAttnArgs a) {
       const float alpha = __builtin_amdgcn_exp2f(m - ref);
       float ps = 0.f;
 #pragma unroll
-      for (int j = 0; j < 2; ++j)
+      for (int j = 0; j < NB; ++j)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           sc[j][r] = __builtin_amdgcn_exp2f(sc[j][r] - ref);
@@ -292,8 +308,7 @@ __global__ __launch_bounds__(256) void paged_attn_kernel(PagedAttnArgs a) {
           for (int c = 0; c < CB; ++c) o[c][r] *= ar;
         }
       }
-      __builtin_amdgcn_wave_barrier();
-      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+      wave_fence();
       if constexpr (EB == 2) {
         T pe[8];
 #pragma unroll
@@ -301,28 +316,24 @@ __global__ __launch_bounds__(256) void paged_attn_kernel(PagedAttnArgs a) {
 #pragma unroll
           for (int r = 0; r < 4; ++r) pe[4 * j + r] = from_f32<T>(sc[j][r]);
         const u32x4 pf = __builtin_bit_cast(u32x4, pe);
-        const unsigned char* col = vs + (4 * grp + (ln >> 2)) * (VSTR * 4) + (ln & 3) * 8;
+        const unsigned char* vcol = vs + (4 * grp + (ln >> 2)) * VSTR + (ln & 3) * 8;
 #pragma unroll
         for (int c = 0; c < CB; ++c) {
-          const uint2 lo = lds_column4(col + c * 32), hi = lds_column4(col + 16 * (VSTR * 4) + c * 32);
+          const uint2 lo = lds_column4(vcol + c * 32), hi = lds_column4(vcol + 16 * VSTR + c * 32);
           o[c] = Mfma<T>::step(pf, u32x4{lo.x, lo.y, hi.x, hi.y}, o[c]);
         }
       } else {
-        const unsigned* vw = reinterpret_cast<const unsigned*>(vs);
+        const u32x4 pf = __builtin_bit_cast(u32x4, sc[0]);
+        const unsigned char* vrow = vs + 4 * grp * VSTR + ln * 4;
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const u32x4 pf = __builtin_bit_cast(u32x4, sc[j]);
+        for (int c = 0; c < CB; ++c) {
+          u32x4 vf;
 #pragma unroll
-          for (int c = 0; c < CB; ++c) {
-            u32x4 vf;
-#pragma unroll
-            for (int r = 0; r < 4; ++r) vf[r] = vw[(16 * j + 4 * grp + r) * VSTR + c * 16 + ln];
-            o[c] = Mfma<T>::step(pf, vf, o[c]);
-          }
+          for (int r = 0; r < 4; ++r) vf[r] = *reinterpret_cast<const unsigned*>(vrow + r * VSTR + c * 64);
+          o[c] = Mfma<T>::step(pf, vf, o[c]);
         }
       }
-      __builtin_amdgcn_wave_barrier();
-      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+      wave_fence();
       if (!more) break;
       t = tn;
       pg = pn;
@@ -345,8 +356,10 @@ __global__ __launch_bounds__(256) void paged_attn_kernel(PagedAttnArgs a) {
     }
     return;
   } else {
+    // a wave's outputs lie where its own tiles were
+    constexpr int JW = WBYTES / 4;
     float* jo = reinterpret_cast<float*>(lds);
-    __syncthreads();                                  // every wave is done with its values
+    static_assert(WBYTES % 16 == 0, "16-byte rows");
     if (grp == 0) {
       jm[wave][ln] = m;
       jl[wave][ln] = lsum;
@@ -356,7 +369,7 @@ __global__ __launch_bounds__(256) void paged_attn_kernel(PagedAttnArgs a) {
       const int i = 4 * grp + r;
       if (i < nq)
 #pragma unroll
-        for (int c = 0; c < CB; ++c) jo[(wave * 16 + i) * DH + c * 16 + ln] = o[c][r];
+        for (int c = 0; c < CB; ++c) jo[wave * JW + i * DH + c * 16 + ln] = o[c][r];
     }
     __syncthreads();
     for (int e = threadIdx.x; e < nq * (DH / 4); e += 256) {
@@ -371,7 +384,7 @@ __global__ __launch_bounds__(256) void paged_attn_kernel(PagedAttnArgs a) {
       for (int w = 0; w < SW; ++w) {
         const float f = __builtin_amdgcn_exp2f(jm[w][i] - ref);
         l += f * jl[w][i];
-        s += f * *reinterpret_cast<const floatx4*>(jo + (w * 16 + i) * DH + x);
+        s += f * *reinterpret_cast<const floatx4*>(jo + w * JW + i * DH + x);
       }
       if (a.parts == 1) {
         const float inv = l == 0.f ? 0.f : 1.0f / l;
@@ -387,47 +400,65 @@ __global__ __launch_bounds__(256) void paged_attn_kernel(PagedAttnArgs a) {
 }
 
 // Merges the parts of a (sequence, head): one workgroup, whose DH / 4 columns of threads take
-// four channels each of every (1024 / DH)-th part.
+// four channels each of every (1024 / DH)-th part, U parts' loads in flight (one round trip
+// for up to 64 parts at d_head 128), each with a running maximum of its own.
 template <typename T, int DH>
 __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnArgs a) {
-  constexpr int COLS = DH / 4, ROWS = 256 / COLS;
-  __shared__ float sw[256 / kWave];
+  constexpr int COLS = DH / 4, ROWS = 256 / COLS, U = 8;
   __shared__ __attribute__((aligned(16))) float so[ROWS][DH];
-  __shared__ float sl[ROWS];
+  __shared__ float sm[ROWS], sl[ROWS];
   const int bh = blockIdx.x, b = bh / a.n_heads, h = bh - b * a.n_heads;
-  const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
   const int len = max(0, min(a.lens[b], a.max_len));
   const int n = max(1, (len + a.chunk - 1) / a.chunk);   // (part 0 is written for an empty row too)
   const size_t stride = (size_t)a.n_seqs * a.n_heads;
   const float* ml = a.part_ml + (size_t)bh * 2;
-  float m = -INFINITY;
-  for (int p = threadIdx.x; p < n; p += 256) m = fmaxf(m, ml[p * stride * 2]);
-  m = wave_max(m);
-  if (lane == 0) sw[wave] = m;
-  __syncthreads();
-#pragma unroll
-  for (int w = 0; w < 256 / kWave; ++w) m = fmaxf(m, sw[w]);
-  const float ref = m == -INFINITY ? 0.f : m;
   const int row = threadIdx.x / COLS, x = threadIdx.x % COLS * 4;
+  const float* po = a.part_o + (size_t)bh * DH + x;
   floatx4 s = floatx4{0.f, 0.f, 0.f, 0.f};
-  float l = 0.f;
-#pragma unroll 4
-  for (int p = row; p < n; p += ROWS) {
-    const float2 q = *reinterpret_cast<const float2*>(ml + p * stride * 2);
-    const floatx4 v = *reinterpret_cast<const floatx4*>(a.part_o + (p * stride + bh) * DH + x);
-    const float f = __builtin_amdgcn_exp2f(q.x - ref);
-    l += f * q.y;
-    s += f * v;
+  float m = -INFINITY, l = 0.f;
+  for (int p0 = row; p0 < n; p0 += ROWS * U) {
+    float2 q[U];
+    floatx4 v[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const size_t p = min(p0 + u * ROWS, n - 1);
+      q[u] = *reinterpret_cast<const float2*>(ml + p * stride * 2);
+      v[u] = *reinterpret_cast<const floatx4*>(po + p * stride * DH);
+    }
+    float mn = m;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (p0 + u * ROWS >= n) q[u] = make_float2(-INFINITY, 0.f);
+      mn = fmaxf(mn, q[u].x);
+    }
+    const float ref = mn == -INFINITY ? 0.f : mn, f0 = __builtin_amdgcn_exp2f(m - ref);
+    l *= f0;
+    s *= f0;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const float f = __builtin_amdgcn_exp2f(q[u].x - ref);
+      l += f * q[u].y;
+      // (a part past the last is the last one's again, its weight 0)
+      if (p0 + u * ROWS < n) s += f * v[u];
+    }
+    m = mn;
   }
   *reinterpret_cast<floatx4*>(&so[row][x]) = s;
-  if (x == 0) sl[row] = l;
+  if (x == 0) {
+    sm[row] = m;
+    sl[row] = l;
+  }
   __syncthreads();
   if (threadIdx.x < DH) {
-    float sum = 0.f, z = 0.f;
+    float mm = sm[0], sum = 0.f, z = 0.f;
+#pragma unroll
+    for (int r = 1; r < ROWS; ++r) mm = fmaxf(mm, sm[r]);
+    const float ref = mm == -INFINITY ? 0.f : mm;
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) {
-      sum += so[r][threadIdx.x];
-      z += sl[r];
+      const float f = __builtin_amdgcn_exp2f(sm[r] - ref);
+      sum += f * so[r][threadIdx.x];
+      z += f * sl[r];
     }
     static_cast<T*>(a.out)[(size_t)b * a.out_ld + (size_t)h * DH + threadIdx.x] = from_f32<T>(z == 0.f ? 0.f : sum / z);
   }
@@ -474,17 +505,32 @@ hipError_t kv_append(const KvAppendArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
-// Parts are multiples of 128 keys (four waves' tiles).
+// How a call is cut, by sizes that the host knows.  Parts are multiples of 128 keys (four waves'
+// tiles), as long as 512 workgroups come of it, two a CU, and at most 1024 keys: more and shorter
+// ones only add to the join, longer ones leave CUs idle at the end of ragged batches.  Measured, us,
+// (512, 1024) / half as long / twice: 16 x 8 heads of 2048..32768 keys (d_head 128) 177 / 183 / 185;
+// one sequence, 4 heads, 131001 E4M3 keys 28.8 / 33.5 / 28.9 (one workgroup a CU: 38); 8 x 8 heads of
+// 4000 keys (d_head 64) 15.9 / 17.6 / 18.7; 8 x 8 of 16000 51 / 48 / 46; 32 x 8 of 500..8000 fp32
+// keys 208 / 209 / 230.
+// Where tasks fill the GPU by themselves and are short, a wave takes one alone and nothing is joined
+// (four waves a task / one): 2160 x 16 heads of up to 231 keys 195 / 164, 2048 x 8 of up to 64
+// 62.7 / 34.4, of up to 256 111 / 93; but 256 x 8 of up to 256 16.9 / 16.9, 64 x 8 of up to 48
+// 4.4 / 4.9, 2048 x 8 of up to 768 250 / 266.
 void paged_attn_plan(PagedAttnArgs* a) {
   a->group = a->n_heads / a->c.n_kv_heads;
   a->qblocks = (a->group + 15) / 16;
   const int tasks = a->n_seqs * a->c.n_kv_heads * a->qblocks;
-  const int tiles = (a->max_len + 4 * TK - 1) / (4 * TK);   // of 128 keys
-  const int want = std::max(1, std::min(1024 / std::max(tasks, 1), tiles / 2));
-  const int per = std::max(1, (tiles + want - 1) / want);
-  a->chunk = per * 4 * TK;
+  const int tiles = (a->max_len + 127) / 128;
+  const long long units = (long long)tiles * tasks;
+  const int per = (int)std::max(1ll, std::min(8ll, (units + 511) / 512));
+  a->chunk = per * 128;
   a->parts = std::max(1, (tiles + per - 1) / per);
-  a->waves = 4;
+  // one wave a task instead of four that share it
+  a->waves = a->max_len <= 256 && tasks >= 2048 ? 1 : 4;
+  if (a->waves == 1) {
+    a->parts = 1;
+    a->chunk = 256;
+  }
 }
 
 hipError_t paged_attn(const PagedAttnArgs& a, hipStream_t s) {

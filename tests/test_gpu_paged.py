@@ -93,6 +93,29 @@ def test_append_one_token_each(dtype, fp8, n):
     assert _same(pages.k, want[0]) and _same(pages.v, want[1])
 
 
+def test_append_rounds_every_fp16_value():
+    """All 65536 fp16 codes through an FP8 cache: the library's E4M3 rounding (nearest even,
+    saturating at 448, NaN to 0x7F), restated here on the exact values."""
+    import torch
+    from paper_2109_08008_amd import nt
+    bits = np.arange(65536, dtype=np.uint16)
+    x = bits.view(np.float16).astype(np.float64)
+    nan = np.isnan(x)
+    a = np.minimum(np.where(nan, 0.0, np.abs(x)), 448.0)
+    step = 2.0 ** (np.floor(np.log2(np.maximum(a, 2.0 ** -6))) - 3)
+    a = np.minimum(np.rint(a / step) * step, 448.0)
+    want = torch.from_numpy(np.where(np.signbit(x), -a, a).astype(np.float32)).to(torch.float8_e4m3fn).view(torch.uint8).numpy()
+    want = np.where(nan, 0x7F, want)
+    pages = Pages([512], 1, 128, 256, "f16", fp8=True, seed=1)
+    rows = torch.from_numpy(bits.view(np.int16).reshape(512, 128).copy()).cuda()
+    off = torch.tensor([0, 512], dtype=torch.int32, device="cuda")
+    nt.nt_op_kv_append(pages.cache, rows.data_ptr(), rows.data_ptr(), 128, off.data_ptr(), pages.lens.data_ptr(), 1, 512)
+    for pool in (pages.k, pages.v):
+        got = torch.cat([pool[int(pages.table_np[0, j]), 0] for j in (0, 1)]).cpu().numpy().reshape(-1)
+        got = np.where(nan & (got == 0xFF), 0x7F, got)      # a NaN's sign is no matter
+        np.testing.assert_array_equal(got, want)
+
+
 def test_append_many_sequences_search():
     """More sequences than two rounds of 64 probes, most without a row."""
     import torch

@@ -377,6 +377,34 @@ nt_status nt_op_select_tiled(const float* d_logits, int32_t rows, int32_t V, int
 nt_status nt_op_select_tiled_noalloc(const float* d_logits, int32_t rows, int32_t V, int32_t k, float* d_topv,
                                      int32_t* d_topi, float* d_lse, void* stream);
 
+/* What a row of logits says about given tokens.  For each of `rows` rows of d_logits (dtype, V
+ * values, rows ld elements apart, any alignment):
+ *   d_logp [rows, n_tok]: log-probability x[w] - log sum_v exp x[v] of each of the row's given
+ *     tokens d_tokens [rows, n_tok] (device int32); 0 for a token outside [0, V), so that padding
+ *     adds nothing to a sum;
+ *   d_lse [rows] the log-sum-exp, d_entropy [rows] the entropy -sum_v p_v log p_v in nats;
+ *   d_topi, d_toplp [rows, k]: the k most probable tokens in (logit desc, index asc) order and
+ *     their log-probabilities.  As for nt_op_select, a logit of -inf is never selected: slots
+ *     beyond hold (INT32_MAX, -inf).
+ * Outputs are fp32, as is the arithmetic.  n_tok >= 0, 0 <= k <= 32, k <= V; d_lse and d_entropy
+ * may be NULL, d_tokens and d_logp if n_tok is 0, d_topi and d_toplp if k is 0.  A logit of -inf
+ * (a word that is ruled out) has probability 0; a row of nothing else has log-sum-exp and
+ * log-probabilities -inf and entropy 0.  A row that holds +inf or NaN gives NaN for the
+ * log-sum-exp, the entropy and every log-probability (a NaN is never an alternative).
+ * d_ws: workspace of at least nt_op_token_logp_workspace bytes (256-byte aligned; may be NULL when
+ * that is 0), in use until the call's work is done: calls that may overlap need their own.
+ * Asynchronous, one or two launches, on the current device.  NT_E_INVALID for a null pointer, a
+ * negative size, ld < V, logits not aligned to their type or a misaligned workspace;
+ * NT_E_UNSUPPORTED for k outside [0, min(32, V)] or 2^24 rows and more; NT_E_WORKSPACE if ws_bytes
+ * is too small (the message states the bytes required).
+ * Defined by: log p(w) of Sec. 4.1's search, whose log_softmax Sec. 4.4 drops: one pass here. */
+nt_status nt_op_token_logp(int32_t dtype, const void* d_logits, int32_t ld, int32_t rows, int32_t V,
+                           const int32_t* d_tokens, int32_t n_tok, int32_t k, float* d_logp, float* d_lse,
+                           float* d_entropy, int32_t* d_topi, float* d_toplp, void* d_ws, size_t ws_bytes,
+                           void* stream);
+/* Bytes of workspace of such a call; needs no device. */
+nt_status nt_op_token_logp_workspace(int32_t dtype, int32_t rows, int32_t V, int32_t k, size_t* bytes);
+
 /* ---- a paged key/value cache -----------------------------------------------------------
  * A cache for requests whose lengths differ and grow: the keys of every sequence lie in a
  * pool of pages [n_pages][n_kv_heads][page_len][d_head], the values in another of the same

@@ -287,6 +287,27 @@ void paged_attn_plan(PagedAttnArgs* a);
 hipError_t paged_attn(const PagedAttnArgs& a, hipStream_t s);
 
 // ---------------------------------------------------------------------------------
+// Log-probabilities, entropy and best alternatives of rows of logits (nt_score.hip).
+constexpr int SCORE_PARTS = 32;   // parts of a row at most
+struct TokenLogpArgs {
+  const void* logits;         // [rows][ld]
+  int ld, rows, V;
+  const int* tokens;          // [rows][n_tok]
+  int n_tok, k;               // k <= 32
+  float *logp, *lse, *entropy;   // [rows][n_tok], [rows] or null, [rows] or null
+  int* topi;                  // [rows][k]
+  float* toplp;
+  // the call's cut (token_logp_plan): parts of part_len values a row; with more than one, their
+  // statistics [rows][parts][4] and best values and indices [rows][parts][k]
+  int parts, part_len;
+  float *part_stats, *part_v;
+  int* part_i;
+};
+// Fills the cut from rows and V.  Host only.
+void token_logp_plan(DT dt, TokenLogpArgs* a);
+hipError_t token_logp(DT dt, const TokenLogpArgs& a, hipStream_t s);
+
+// ---------------------------------------------------------------------------------
 // Search.
 struct SearchState {
   int B, beam, V, eos, Tcap;

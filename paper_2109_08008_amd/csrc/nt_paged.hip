@@ -512,6 +512,8 @@ hipError_t kv_append(const KvAppendArgs& a, hipStream_t s) {
 // one sequence, 4 heads, 131001 E4M3 keys 28.8 / 33.5 / 28.9 (one workgroup a CU: 38); 8 x 8 heads of
 // 4000 keys (d_head 64) 15.9 / 17.6 / 18.7; 8 x 8 of 16000 51 / 48 / 46; 32 x 8 of 500..8000 fp32
 // keys 208 / 209 / 230.
+// Never more than 32768 parts in all, however far max_len is above the lengths: empty ones cost a
+// workgroup each, and every one its place in the workspace.
 // Where tasks fill the GPU by themselves and are short, a wave takes one alone and nothing is joined
 // (four waves a task / one): 2160 x 16 heads of up to 231 keys 195 / 164, 2048 x 8 of up to 64
 // 62.7 / 34.4, of up to 256 111 / 93; but 256 x 8 of up to 256 16.9 / 16.9, 64 x 8 of up to 48
@@ -522,7 +524,7 @@ void paged_attn_plan(PagedAttnArgs* a) {
   const int tasks = a->n_seqs * a->c.n_kv_heads * a->qblocks;
   const int tiles = (a->max_len + 127) / 128;
   const long long units = (long long)tiles * tasks;
-  const int per = (int)std::max(1ll, std::min(8ll, (units + 511) / 512));
+  const int per = (int)std::max({1ll, std::min(8ll, (units + 511) / 512), (units + 32767) / 32768});
   a->chunk = per * 128;
   a->parts = std::max(1, (tiles + per - 1) / per);
   // one wave a task instead of four that share it

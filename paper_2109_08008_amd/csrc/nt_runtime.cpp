@@ -1320,6 +1320,20 @@ nt_status paged_attn_cut(int n_heads, int n_seqs, int max_len, nt::PagedAttnArgs
   return NT_OK;
 }
 
+// The cut of a nt_op_token_logp call and the bytes its parts take.
+nt_status token_logp_cut(int dtype, int rows, int V, int k, nt::TokenLogpArgs* a, size_t* bytes) {
+  if (dtype < NT_F32 || dtype > NT_BF16) return fail(NT_E_INVALID, "unknown dtype %d", dtype);
+  if (rows < 0 || V <= 0) return fail(NT_E_INVALID, "rows must be >= 0 and V > 0");
+  if (k < 0 || k > 32 || k > V) return fail(NT_E_UNSUPPORTED, "k must be in [0, min(32, V)]");
+  if (rows >= 1 << 24) return fail(NT_E_UNSUPPORTED, "at most 16777215 rows");
+  a->rows = rows;
+  a->V = V;
+  a->k = k;
+  nt::token_logp_plan(static_cast<DT>(dtype), a);
+  *bytes = a->parts > 1 ? align_up((size_t)rows * a->parts * (4 + 2 * (size_t)k) * sizeof(float)) : 0;
+  return NT_OK;
+}
+
 size_t paged_ws_bytes(const nt::PagedAttnArgs& a) {
   return a.parts > 1 ? align_up((size_t)a.parts * a.n_seqs * a.n_heads * (a.c.d_head + 2) * sizeof(float)) : 0;
 }
@@ -2021,6 +2035,51 @@ nt_status nt_op_select_tiled_noalloc(const float* d_logits, int32_t rows, int32_
   const hipStream_t s = static_cast<hipStream_t>(stream);
   NT_HIP(nt::tile_records(d_logits, rows, V, part, s));
   NT_HIP(nt::beam_select_tiles(part, n_tiles, d_logits, nullptr, 1, rows, V, k, d_topv, d_topi, d_lse, s));
+  return NT_OK;
+}
+
+nt_status nt_op_token_logp_workspace(int32_t dtype, int32_t rows, int32_t V, int32_t k, size_t* bytes) {
+  g_err.clear();
+  if (!bytes) return fail(NT_E_INVALID, "null argument to nt_op_token_logp_workspace");
+  nt::TokenLogpArgs a{};
+  return token_logp_cut(dtype, rows, V, k, &a, bytes);
+}
+
+nt_status nt_op_token_logp(int32_t dtype, const void* d_logits, int32_t ld, int32_t rows, int32_t V,
+                           const int32_t* d_tokens, int32_t n_tok, int32_t k, float* d_logp, float* d_lse,
+                           float* d_entropy, int32_t* d_topi, float* d_toplp, void* d_ws, size_t ws_bytes,
+                           void* stream) {
+  g_err.clear();
+  nt::TokenLogpArgs a{};
+  size_t need = 0;
+  NT_TRY(token_logp_cut(dtype, rows, V, k, &a, &need));
+  if (n_tok < 0) return fail(NT_E_INVALID, "n_tok must be >= 0");
+  if (!d_logits || (n_tok > 0 && (!d_tokens || !d_logp)) || (k > 0 && (!d_topi || !d_toplp)))
+    return fail(NT_E_INVALID, "null argument to nt_op_token_logp");
+  if (ld < V) return fail(NT_E_INVALID, "ld must be >= V");
+  if (reinterpret_cast<uintptr_t>(d_logits) % nt::dt_bytes(static_cast<DT>(dtype)))
+    return fail(NT_E_INVALID, "logits must be aligned to their type");
+  if (need > 0) {
+    if (!d_ws || ws_bytes < need)
+      return fail(NT_E_WORKSPACE, "workspace of %zu bytes required, %zu given", need, d_ws ? ws_bytes : (size_t)0);
+    if (reinterpret_cast<uintptr_t>(d_ws) & 255) return fail(NT_E_INVALID, "workspace must be 256-byte aligned");
+  }
+  if (rows == 0) return NT_OK;
+  a.logits = d_logits;
+  a.ld = ld;
+  a.tokens = d_tokens;
+  a.n_tok = n_tok;
+  a.logp = d_logp;
+  a.lse = d_lse;
+  a.entropy = d_entropy;
+  a.topi = d_topi;
+  a.toplp = d_toplp;
+  if (need > 0) {
+    a.part_stats = static_cast<float*>(d_ws);
+    a.part_v = a.part_stats + (size_t)rows * a.parts * 4;
+    a.part_i = reinterpret_cast<int*>(a.part_v + (size_t)rows * a.parts * k);
+  }
+  NT_HIP(nt::token_logp(static_cast<DT>(dtype), a, static_cast<hipStream_t>(stream)));
   return NT_OK;
 }
 

@@ -1,0 +1,541 @@
+// What a model says about given tokens: from each row of logits, in one pass, the
+// log-sum-exp, the entropy, the log-probabilities of given tokens and the k best
+// alternatives with theirs.
+//
+// With m the row's maximum, s = sum e^{x - m} and t = sum e^{x - m} (x - m):
+//   lse = m + log s,   H = log s - t / s,   log p(w) = (x_w - m) - log s.
+// A thread keeps (m, s, t) of what it has read, all in fp32, and rescales once a batch of
+// loads: with the maximum moving from m to m', t becomes e^{m - m'} (t + s (m - m')).
+//
+// HBM bounds it (V values a row, read once, non-temporal), closely followed in 16 bits by
+// the vector units: ten slots an element, four of them the exponential's.
+//
+// The alternatives are found as in the beam selection (nt_search.hip): the maxima of 64
+// quads of threads give a threshold that the row's k best reach, only the threads whose
+// maximum reaches it look at their values again, and each value found counts the ones
+// before it under (value desc, index asc).  A row with more than SCORE_CAP values at the
+// threshold (ties, above all 16-bit ones) raises it to the k-th best of those collected
+// and collects again, until what is above it fits; then the lowest indices at the
+// threshold fill up.  So the result never depends on the order of arrival.
+//
+// Few rows are cut into parts over workgroups; a part leaves (m, s, t) and its k best, and
+// logp_join_kernel merges them.
+#include <limits.h>
+
+#include <algorithm>
+#include <type_traits>
+
+#include "nt_common.h"
+#include "nt_kernels.h"
+
+namespace nt {
+namespace {
+
+constexpr int SCORE_THREADS = 256;
+constexpr int SCORE_CAP = 528;    // as many as a join keeps at most (32 parts, k = 32)
+constexpr int SCORE_BATCH = 4;    // 16-byte loads of a batch; the next batch's are in flight with it
+constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+
+struct Stats {
+  float m, s, t;
+};
+// (m, s, t) as seen from the maximum `to` >= m.  A part without a finite value (m = -inf) has
+// s = t = 0, or NaN where it held a NaN, and keeps them.
+__device__ __forceinline__ Stats rescale(Stats a, float to) {
+  if (a.m == -INFINITY) return {to, a.s, a.t};
+  const float d = a.m - to, f = __builtin_amdgcn_exp2f(d * LOG2E);
+  return {to, a.s * f, (a.t + a.s * d) * f};
+}
+// The wave's, seen from the largest `best`, which is at least each lane's a.m.
+__device__ __forceinline__ Stats wave_stats(Stats a, float best) {
+  const float m = wave_max(best);
+  a = rescale(a, m);
+  return {m, wave_sum(a.s), wave_sum(a.t)};
+}
+
+// (value desc, index asc)
+__device__ __forceinline__ bool before(float v1, int i1, float v2, int i2) { return v1 > v2 || (v1 == v2 && i1 < i2); }
+
+// The candidates of a workgroup: `n` (value, index) pairs, and how many come before one.
+struct Candidates {
+  __attribute__((aligned(16))) float v[SCORE_CAP + 4];
+  __attribute__((aligned(16))) int i[SCORE_CAP + 4];
+  int count;
+};
+__device__ __forceinline__ void put(Candidates& c, float x, int i) {
+  const int at = atomicAdd(&c.count, 1);
+  if (at < SCORE_CAP) {
+    c.v[at] = x;
+    c.i[at] = i;
+  }
+}
+// Entries up to the next multiple of four behind the last are before none.  Call between two barriers.
+__device__ __forceinline__ void pad(Candidates& c, int n) {
+  if (threadIdx.x < 4) {
+    c.v[n + threadIdx.x] = -INFINITY;
+    c.i[n + threadIdx.x] = INT_MAX;
+  }
+}
+__device__ __forceinline__ int rank_of(const Candidates& c, int n, int e) {
+  const float x = c.v[e];
+  const int i = c.i[e];
+  int at = 0;
+  for (int j = 0; j < n; j += 4) {
+    const float4 v = *reinterpret_cast<const float4*>(c.v + j);
+    const int4 w = *reinterpret_cast<const int4*>(c.i + j);
+    at += before(v.x, w.x, x, i) + before(v.y, w.y, x, i) + before(v.z, w.z, x, i) + before(v.w, w.w, x, i);
+  }
+  return at;
+}
+
+// The values of a 16-byte vector.
+template <typename T>
+__device__ __forceinline__ void widen(u32x4 q, float (&x)[Vec<T>::N]) {
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    if constexpr (sizeof(T) == 4) {
+      x[w] = __uint_as_float(q[w]);
+    } else if constexpr (std::is_same<T, bf16>::value) {
+      x[2 * w] = __uint_as_float(q[w] << 16);
+      x[2 * w + 1] = __uint_as_float(q[w] & 0xffff0000u);
+    } else {
+      const unsigned u = q[w];
+      typedef _Float16 half2v __attribute__((ext_vector_type(2)));
+      const half2v h = __builtin_bit_cast(half2v, u);
+      x[2 * w] = (float)h[0];
+      x[2 * w + 1] = (float)h[1];
+    }
+  }
+}
+template <typename T>
+__device__ __forceinline__ u32x4 minus_infinity() {   // a vector of them
+  const unsigned u = sizeof(T) == 4 ? 0xff800000u : std::is_same<T, bf16>::value ? 0xff80ff80u : 0xfc00fc00u;
+  return u32x4{u, u, u, u};
+}
+
+// The maximum of a thread's vectors.
+template <typename T>
+__device__ __forceinline__ float best_of(const u32x4 (&q)[SCORE_BATCH]) {
+  if constexpr (std::is_same<T, f16>::value) {   // two at a time
+    half8 best = __builtin_bit_cast(half8, q[0]);
+#pragma unroll
+    for (int u = 1; u < SCORE_BATCH; ++u) best = __builtin_elementwise_max(best, __builtin_bit_cast(half8, q[u]));
+    float m = -INFINITY;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) m = fmaxf(m, (float)best[e]);
+    return m;
+  } else {
+    float m = -INFINITY;
+#pragma unroll
+    for (int u = 0; u < SCORE_BATCH; ++u) {
+      float v[Vec<T>::N];
+      widen<T>(q[u], v);
+#pragma unroll
+      for (int e = 0; e < Vec<T>::N; ++e) m = fmaxf(m, v[e]);
+    }
+    return m;
+  }
+}
+
+// Takes a thread's vectors q[0 .. count - 1] (of SCORE_BATCH; the others hold -inf) into acc and
+// returns their maximum.  acc is kept relative to a reference acc.m near the maximum so far, so that
+// one turn over the values is enough; where a batch rises more than 2^64 above it, and in the first
+// batch, the reference moves first.
+// With c = ref log2(e) as rounded and r its rounding error, x log2(e) - c is one operation and
+// equals (x - ref) log2(e) + r: the sums are put right by r once a batch.  What that form cannot
+// take (-inf: 0 * -inf; NaN, and values past 2e38) shows as a NaN in t; the batch is then done by
+// differences, p max(x - ref, -1e30) (a logit of -inf adds nothing, a NaN stays one), and `careful`
+// sends the wave's next batches there at once.
+template <typename T, bool WHOLE>
+__device__ __forceinline__ float take_batch(const u32x4 (&q)[SCORE_BATCH], int count, Stats& acc, bool& careful) {
+  constexpr int VN = Vec<T>::N;
+  if (!careful) {
+    if (__ballot(acc.m == -INFINITY)) {
+      const float m = best_of<T>(q);
+      if (acc.m == -INFINITY) acc.m = m;
+    }
+    const float ref = acc.m == -INFINITY ? 0.f : acc.m;
+    const float c = ref * LOG2E, r = fmaf(ref, LOG2E, -c);
+    float s[2] = {0.f, 0.f}, t[2] = {0.f, 0.f}, best = -INFINITY;
+#pragma unroll
+    for (int u = 0; u < SCORE_BATCH; ++u) {
+      if (!WHOLE && u >= count) break;
+      float v[VN];
+      widen<T>(q[u], v);
+#pragma unroll
+      for (int e = 0; e < VN; ++e) {
+        const float d = fmaf(v[e], LOG2E, -c), p = __builtin_amdgcn_exp2f(d);
+        best = fmaxf(best, v[e]);
+        s[e & 1] += p;
+        t[e & 1] = fmaf(p, d, t[e & 1]);
+      }
+    }
+    const float f = 1.0f - r * LN2;   // 2^-r
+    const float sb = s[0] + s[1], tb = (t[0] + t[1] - r * sb) * (LN2 * f);
+    careful = __ballot(tb != tb) != 0;
+    if (!careful && !__ballot((best - ref) * LOG2E > 64.f)) {
+      acc.s += sb * f;
+      acc.t += tb;
+      return best;
+    }
+  }
+  const float best = best_of<T>(q), mx = fmaxf(acc.m, best);
+  acc = rescale(acc, mx);
+  const float ref = mx == -INFINITY ? 0.f : mx;
+  float sb = 0.f, tb = 0.f;
+#pragma unroll
+  for (int u = 0; u < SCORE_BATCH; ++u) {
+    if (!WHOLE && u >= count) break;
+    float v[VN];
+    widen<T>(q[u], v);
+#pragma unroll
+    for (int e = 0; e < VN; ++e) {
+      const float d = v[e] - ref, p = __builtin_amdgcn_exp2f(d * LOG2E);
+      sb += p;
+      tb = fmaf(p, fmaxf(d, -1e30f), tb);
+    }
+  }
+  acc.s += sb;
+  acc.t += tb;
+  return best;
+}
+
+template <typename T>
+__global__ __launch_bounds__(SCORE_THREADS) void token_logp_kernel(TokenLogpArgs a) {
+  constexpr int NT = SCORE_THREADS, NW = NT / kWave, VN = Vec<T>::N;
+  static_assert(NT == 4 * 64, "groups are quads");
+  __shared__ float sm[NW], ss[NW], st[NW], kth[NW];
+  __shared__ float4 gmax[16];
+  __shared__ Candidates cand;
+  __shared__ float raised;
+  const int row = blockIdx.x / a.parts, part = blockIdx.x - row * a.parts;
+  const int c0 = part * a.part_len, n = min(a.part_len, a.V - c0);
+  const T* x = static_cast<const T*>(a.logits) + (size_t)row * a.ld + c0;
+  const int tid = threadIdx.x, wave = tid / kWave, lane = tid % kWave;
+  // the given tokens' logits, under way with the row
+  float given = 0.f;
+  int token = -1;
+  if (a.parts == 1 && tid < a.n_tok) {
+    token = a.tokens[(size_t)row * a.n_tok + tid];
+    if ((unsigned)token < (unsigned)a.V) given = to_f32(x[token]);
+  }
+  if (tid == 0) cand.count = 0;
+  // `head` single values up to a 128-byte line (a load that straddles lines fetches both: 8192 rows
+  // of 32001 bf16 values 98 us from 16-byte boundaries, of 32000 89), nv vectors and a tail; threads
+  // 0 .. HEAD - 1 take the head's, the next ones the tail's
+  constexpr int HEAD = 128 / (int)sizeof(T);
+  const int head = min(n, (int)((128 - (reinterpret_cast<uintptr_t>(x) & 127)) & 127) / (int)sizeof(T));
+  const int nv = (n - head) / VN, tail = head + nv * VN;
+  const u32x4* xv = reinterpret_cast<const u32x4*>(x + head);
+  const int single = tid < HEAD ? (tid < head ? tid : -1) : tail + tid - HEAD < n ? tail + tid - HEAD : -1;
+  Stats acc{-INFINITY, 0.f, 0.f};
+  float single_value = -INFINITY;
+  if (single >= 0) {
+    const float c = to_f32(x[single]);
+    single_value = acc.m = fmaxf(c, -INFINITY);
+    acc.s = c == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(c - c);   // 1; NaN of an infinity or a NaN
+    acc.t = c == -INFINITY ? 0.f : c - c;
+  }
+  const int batches = (nv + NT * SCORE_BATCH - 1) / (NT * SCORE_BATCH);
+  auto load = [&](u32x4 (&q)[SCORE_BATCH], int batch) {
+#pragma unroll
+    for (int u = 0; u < SCORE_BATCH; ++u) {
+      const int i = tid + (batch * SCORE_BATCH + u) * NT;
+      q[u] = i < nv ? __builtin_nontemporal_load(xv + i) : minus_infinity<T>();
+    }
+  };
+  // the best batch's maximum, which one it is, and the best of all others
+  float first = -INFINITY, second = -INFINITY;
+  int first_batch = 0;
+  bool careful = false;
+  auto take = [&](u32x4 (&q)[SCORE_BATCH], int batch) {
+    const float best = (batch + 1) * SCORE_BATCH * NT <= nv
+                           ? take_batch<T, true>(q, SCORE_BATCH, acc, careful)
+                           : take_batch<T, false>(q, (nv - tid + NT - 1) / NT - batch * SCORE_BATCH, acc, careful);
+    second = fmaxf(second, fminf(first, best));
+    first_batch = best > first ? batch : first_batch;
+    first = fmaxf(first, best);
+  };
+  u32x4 q0[SCORE_BATCH], q1[SCORE_BATCH];
+  load(q0, 0);
+  for (int b = 0; b < batches;) {
+    if (b + 1 < batches) load(q1, b + 1);
+    take(q0, b);
+    if (++b >= batches) break;
+    if (b + 1 < batches) load(q0, b + 1);
+    take(q1, b);
+    ++b;
+  }
+  const float mine = fmaxf(first, single_value);   // acc.m is a reference near it
+  {
+    const Stats w = wave_stats(acc, mine);
+    if (lane == 0) {
+      sm[wave] = w.m;
+      ss[wave] = w.s;
+      st[wave] = w.t;
+    }
+  }
+  if (a.k > 0) {
+    float g = fmaxf(mine, dpp_mov<DPP_XOR1>(mine));
+    g = fmaxf(g, dpp_mov<DPP_XOR2>(g));
+    if (tid % 4 == 0) reinterpret_cast<float*>(gmax)[tid / 4] = g;
+  }
+  __syncthreads();
+  Stats all{fmaxf(fmaxf(sm[0], sm[1]), fmaxf(sm[2], sm[3])), 0.f, 0.f};
+  static_assert(NW == 4, "four waves");
+#pragma unroll
+  for (int w = 0; w < NW; ++w) {
+    const Stats r = rescale(Stats{sm[w], ss[w], st[w]}, all.m);
+    all.s += r.s;
+    all.t += r.t;
+  }
+  const float log_s = logf(all.s);
+  if (a.parts == 1) {
+    if (tid == 0) {
+      const bool none = all.s == 0.f;      // no logit above -inf
+      if (a.lse) a.lse[row] = none ? -INFINITY : all.m + log_s;
+      if (a.entropy) a.entropy[row] = none ? 0.f : log_s - all.t / all.s;
+    }
+    for (int j = tid; j < a.n_tok; j += NT) {
+      if (j >= NT) {
+        token = a.tokens[(size_t)row * a.n_tok + j];
+        if ((unsigned)token < (unsigned)a.V) given = to_f32(x[token]);
+      }
+      const float lp = given == -INFINITY && all.s == all.s ? -INFINITY : (given - all.m) - log_s;
+      a.logp[(size_t)row * a.n_tok + j] = (unsigned)token < (unsigned)a.V ? lp : 0.f;
+    }
+  } else if (tid == 0) {
+    *reinterpret_cast<float4*>(a.part_stats + ((size_t)row * a.parts + part) * 4) = make_float4(all.m, all.s, all.t, 0.f);
+  }
+  if (a.k == 0) return;
+
+  // The k-th largest group maximum: each wave counts the maxima above 16 groups' ones (lane l
+  // group 16 wave + l % 16 against 16 others), the smallest with fewer than k above it is it.
+  float thr;
+  {
+    const float g = reinterpret_cast<const float*>(gmax)[16 * wave + lane % 16];
+    float above = 0.f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float4 o = gmax[lane / 16 * 4 + j];
+      above += (o.x > g ? 1.f : 0.f) + (o.y > g ? 1.f : 0.f) + (o.z > g ? 1.f : 0.f) + (o.w > g ? 1.f : 0.f);
+    }
+    above += __shfl_xor(above, 16, kWave);
+    above += __shfl_xor(above, 32, kWave);
+    const float low = -wave_max(above < (float)a.k ? -g : -INFINITY);
+    if (lane == 0) kth[wave] = low;
+  }
+  __syncthreads();
+  thr = fminf(fminf(kth[0], kth[1]), fminf(kth[2], kth[3]));
+  auto take_values = [&](u32x4 q, int i) {
+    float v[VN];
+    widen<T>(q, v);
+#pragma unroll
+    for (int e = 0; e < VN; ++e)
+      if (v[e] >= thr && v[e] != -INFINITY) put(cand, v[e], head + VN * i + e);
+  };
+  if (single >= 0) {
+    const float c = to_f32(x[single]);
+    if (c >= thr && c != -INFINITY) put(cand, c, single);
+  }
+  if (first >= thr && first != -INFINITY) {
+    u32x4 q[SCORE_BATCH];
+    if (batches <= 1) {   // still at hand
+#pragma unroll
+      for (int u = 0; u < SCORE_BATCH; ++u) q[u] = q0[u];
+    } else {
+      load(q, first_batch);
+    }
+#pragma unroll
+    for (int u = 0; u < SCORE_BATCH; ++u) {
+      const int i = tid + (first_batch * SCORE_BATCH + u) * NT;
+      if (i < nv) take_values(q[u], i);
+    }
+  }
+  // The few threads with a second batch that reaches it: the wave goes through their other vectors,
+  // lane u reading u, u + 64, .. (Reading all of every candidate thread's again, a 128-byte line for
+  // each 16 bytes, took a quarter of a long call: 4000 rows of 32000 fp32 values, k = 8, 102 us
+  // against 82 with k = 0.)
+  unsigned long long who = __ballot(second >= thr && second != -INFINITY);
+  while (who && *(volatile int*)&cand.count <= SCORE_CAP) {
+    const int l = __builtin_ctzll(who), skip = readlane_i(first_batch, l);
+    who &= who - 1;
+    for (int u = lane; u * NT < nv; u += kWave) {
+      const int i = wave * kWave + l + u * NT;
+      if (i < nv && u / SCORE_BATCH != skip) take_values(xv[i], i);
+    }
+  }
+  __syncthreads();
+  int found = cand.count;
+  if (found > SCORE_CAP) {
+    do {
+      // raise the threshold to the k-th best of those collected: k values reach it
+      for (int e = tid; e < SCORE_CAP; e += NT)
+        if (rank_of(cand, SCORE_CAP, e) == a.k - 1) raised = cand.v[e];
+      __syncthreads();
+      thr = raised;
+      if (tid == 0) cand.count = 0;
+      __syncthreads();
+      for (int i = tid; i < n; i += NT) {
+        const float c = to_f32(x[i]);
+        if (c > thr) put(cand, c, i);
+      }
+      __syncthreads();
+      found = cand.count;
+    } while (found > SCORE_CAP);
+    // fewer than k above it: the lowest indices at it, in order
+    for (int i0 = 0; i0 < n && found < a.k; i0 += NT) {
+      const unsigned long long at = __ballot(i0 + tid < n && to_f32(x[min(i0 + tid, n - 1)]) == thr);
+      if (lane == 0) reinterpret_cast<int*>(sm)[wave] = __popcll(at);
+      __syncthreads();
+      int place = found, total = 0;
+#pragma unroll
+      for (int w = 0; w < NW; ++w) {
+        const int c = reinterpret_cast<const int*>(sm)[w];
+        if (w < wave) place += c;
+        total += c;
+      }
+      place += __popcll(at & ((1ull << lane) - 1));
+      if ((at >> lane & 1) && place < a.k) {
+        cand.v[place] = thr;
+        cand.i[place] = i0 + tid;
+      }
+      found = min(a.k, found + total);
+      __syncthreads();
+    }
+  }
+  pad(cand, found);
+  __syncthreads();
+  // each candidate's place is the number of candidates before it
+  const size_t out = ((size_t)row * a.parts + part) * a.k;
+  for (int e = tid; e < found; e += NT) {
+    const int at = rank_of(cand, found, e);
+    if (at >= a.k) continue;
+    if (a.parts == 1) {
+      a.topi[out + at] = cand.i[e];
+      a.toplp[out + at] = (cand.v[e] - all.m) - log_s;
+    } else {
+      a.part_v[out + at] = cand.v[e];
+      a.part_i[out + at] = c0 + cand.i[e];
+    }
+  }
+  for (int e = found + tid; e < a.k; e += NT) {   // fewer logits above -inf than k
+    if (a.parts == 1) {
+      a.topi[out + e] = INT_MAX;
+      a.toplp[out + e] = -INFINITY;
+    } else {
+      a.part_v[out + e] = -INFINITY;
+      a.part_i[out + e] = INT_MAX;
+    }
+  }
+}
+
+// Merges a row's parts: their statistics, and of their k best each the row's.
+template <typename T>
+__global__ __launch_bounds__(SCORE_THREADS) void logp_join_kernel(TokenLogpArgs a) {
+  constexpr int NT = SCORE_THREADS;
+  static_assert(SCORE_PARTS <= kWave && SCORE_PARTS % 4 == 0 && SCORE_PARTS * 32 <= 4 * NT, "four entries a thread");
+  static_assert(SCORE_PARTS == 32 && SCORE_CAP >= 32 * 33 / 2, "what is left of the entries fits");
+  __shared__ __attribute__((aligned(16))) float hv[SCORE_PARTS];   // the parts' best
+  __shared__ Candidates cand;
+  const int row = blockIdx.x, tid = threadIdx.x, lane = tid % kWave;
+  const int n = a.parts * a.k;
+  float ev[4];
+  int ei[4];
+#pragma unroll
+  for (int u = 0; u < 4; ++u) {
+    const int e = tid + u * NT;
+    ev[u] = e < n ? a.part_v[(size_t)row * n + e] : -INFINITY;
+    ei[u] = e < n ? a.part_i[(size_t)row * n + e] : INT_MAX;
+  }
+  if (a.k > 0 && tid < SCORE_PARTS) hv[tid] = tid < a.parts ? a.part_v[(size_t)row * n + tid * a.k] : -INFINITY;
+  if (tid == 0) cand.count = 0;
+  Stats all{-INFINITY, 0.f, 0.f};
+  if (lane < a.parts) {
+    const float4 q = *reinterpret_cast<const float4*>(a.part_stats + ((size_t)row * a.parts + lane) * 4);
+    all = Stats{q.x, q.y, q.z};
+  }
+  all = wave_stats(all, all.m);
+  const float log_s = logf(all.s);
+  if (tid == 0) {
+    const bool none = all.s == 0.f;
+    if (a.lse) a.lse[row] = none ? -INFINITY : all.m + log_s;
+    if (a.entropy) a.entropy[row] = none ? 0.f : log_s - all.t / all.s;
+  }
+  for (int j = tid; j < a.n_tok; j += NT) {
+    const int token = a.tokens[(size_t)row * a.n_tok + j];
+    float lp = 0.f;
+    if ((unsigned)token < (unsigned)a.V) {
+      const float x = to_f32(static_cast<const T*>(a.logits)[(size_t)row * a.ld + token]);
+      lp = x == -INFINITY && all.s == all.s ? -INFINITY : (x - all.m) - log_s;
+    }
+    a.logp[(size_t)row * a.n_tok + j] = lp;
+  }
+  if (a.k == 0) return;
+  __syncthreads();
+  // An entry behind `place` of its own part and behind the best of h other parts (of equal values the
+  // earlier part's) is behind place + h: what is left of all parts' entries where that is below k is a
+  // list of a few k.
+#pragma unroll
+  for (int u = 0; u < 4; ++u) {
+    if (u * NT >= n) break;
+    const int e = tid + u * NT, own = e / a.k, place = e - own * a.k;
+    int heads = 0;
+#pragma unroll
+    for (int j = 0; j < SCORE_PARTS; j += 4) {
+      const float4 v = *reinterpret_cast<const float4*>(hv + j);
+      heads += (j < own ? v.x >= ev[u] : v.x > ev[u]) + (j + 1 < own ? v.y >= ev[u] : v.y > ev[u]) +
+               (j + 2 < own ? v.z >= ev[u] : v.z > ev[u]) + (j + 3 < own ? v.w >= ev[u] : v.w > ev[u]);
+    }
+    // (its own part's best, where that is above it, is one of the `place` already)
+    if (ev[u] < hv[min(own, SCORE_PARTS - 1)]) --heads;
+    if (e < n && ei[u] != INT_MAX && place + heads < a.k) put(cand, ev[u], ei[u]);
+  }
+  __syncthreads();
+  const int found = cand.count;   // at most k + (k - 1) + .. + 1 of them
+  pad(cand, found);
+  __syncthreads();
+  for (int e = tid; e < found; e += NT) {
+    const int at = rank_of(cand, found, e);
+    if (at < a.k) {
+      a.topi[(size_t)row * a.k + at] = cand.i[e];
+      a.toplp[(size_t)row * a.k + at] = (cand.v[e] - all.m) - log_s;
+    }
+  }
+  for (int e = found + tid; e < a.k; e += NT) {   // fewer logits above -inf than k
+    a.topi[(size_t)row * a.k + e] = INT_MAX;
+    a.toplp[(size_t)row * a.k + e] = -INFINITY;
+  }
+}
+
+template <typename T>
+hipError_t logp_launch(const TokenLogpArgs& a, hipStream_t s) {
+  NT_LAUNCH((token_logp_kernel<T>), dim3((unsigned)(a.rows * a.parts)), dim3(SCORE_THREADS), 0, s, a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || a.parts == 1) return e;
+  NT_LAUNCH((logp_join_kernel<T>), dim3((unsigned)a.rows), dim3(SCORE_THREADS), 0, s, a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+void token_logp_plan(DT dt, TokenLogpArgs* a) {
+  const long long row_bytes = (long long)a->V * dt_bytes(dt);
+  long long parts = a->rows > 0 ? 1024 / a->rows : 1;
+  parts = std::min(parts, row_bytes / 16384);
+  parts = std::max(1ll, std::min<long long>(parts, SCORE_PARTS));
+  a->part_len = (int)((a->V + parts - 1) / parts);
+  a->parts = (a->V + a->part_len - 1) / a->part_len;
+}
+
+hipError_t token_logp(DT dt, const TokenLogpArgs& a, hipStream_t s) {
+  if (a.rows <= 0) return hipSuccess;
+  switch (dt) {
+    case DT::F32: return logp_launch<float>(a, s);
+    case DT::F16: return logp_launch<f16>(a, s);
+    case DT::BF16: return logp_launch<bf16>(a, s);
+  }
+  return hipErrorInvalidValue;
+}
+
+}  // namespace nt

@@ -32,6 +32,7 @@ EXPORTS = [
     "nt_op_gemm", "nt_op_gemm_ln", "nt_op_gemm_rows", "nt_prof_config", "nt_set_graphs", "nt_set_beam_fused", "nt_set_streams", "nt_prof_units", "nt_op_select",
     "nt_op_select_tiled", "nt_op_select_tiled_noalloc",
     "nt_ensemble", "nt_quantize_fp8", "nt_op_kv_append", "nt_op_attn_paged", "nt_op_attn_paged_workspace",
+    "nt_op_token_logp", "nt_op_token_logp_workspace",
 ]
 NT_ENS_MEAN_LOGP, NT_ENS_LOG_MEAN_P = 0, 1
 NT_SELECT_NOALLOC_MAX_RECORDS = 1 << 20   # include/nt.h: records of nt_op_select_tiled_noalloc
@@ -115,6 +116,9 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
         "nt_op_gemm_ln": (c_int32, [c_int32, P, c_int32, P, c_int32, c_int32, c_int32, P, c_float, P, P, c_int32,
                                     c_int32, c_int32, P, P]),
         "nt_op_gemm_rows": (c_int32, [c_int32] * 8),
+        "nt_op_token_logp": (c_int32, [c_int32, P, c_int32, c_int32, c_int32, P, c_int32, c_int32, P, P, P, P, P, P,
+                                       c_size_t, P]),
+        "nt_op_token_logp_workspace": (c_int32, [c_int32] * 4 + [POINTER(c_size_t)]),
         "nt_op_kv_append": (c_int32, [POINTER(nt_kv_pages), P, P, c_int32, P, P, c_int32, c_int32, P]),
         "nt_op_attn_paged": (c_int32, [POINTER(nt_kv_pages), P, c_int32, c_int32, P, c_int32, c_int32, c_float, P,
                                        c_int32, P, c_size_t, P]),
@@ -319,6 +323,18 @@ def nt_op_select_tiled_noalloc(d_logits: int, rows: int, V: int, k: int, d_topv:
                                stream=None):
     _check(load_library().nt_op_select_tiled_noalloc(c_void_p(d_logits), rows, V, k, c_void_p(d_topv),
                                                      c_void_p(d_topi), c_void_p(d_lse), _stream(stream)))
+
+
+def nt_op_token_logp_workspace(dtype: str, rows: int, V: int, k: int) -> int:
+    b = c_size_t()
+    _check(load_library().nt_op_token_logp_workspace(DTYPES[dtype], rows, V, k, ctypes.byref(b)))
+    return b.value
+
+
+def nt_op_token_logp(dtype: str, d_logits: int, ld: int, rows: int, V: int, d_tokens, n_tok: int, k: int, d_logp, d_lse,
+                     d_entropy, d_topi=None, d_toplp=None, d_ws=None, ws_bytes: int = 0, stream=None):
+    _check(load_library().nt_op_token_logp(DTYPES[dtype], d_logits, ld, rows, V, d_tokens, n_tok, k, d_logp, d_lse,
+                                           d_entropy, d_topi, d_toplp, d_ws, ws_bytes, _stream(stream)))
 
 
 def kv_pages(dtype: str, n_kv_heads: int, d_head: int, page_len: int, n_pages: int, max_pages: int, d_k: int, d_v: int,

@@ -87,9 +87,10 @@ def test_workspace_sizes(nt):
     lengths reach."""
     c = _cache(nt, max_pages=1 << 20, n_pages=1 << 20)
     size = lambda n, m: nt.nt_op_attn_paged_workspace(c, 4, n, m)   # noqa: E731
-    assert size(0, 100) == 0 and size(5000, 1 << 20) == 0 and size(1, 0) == 0 and size(4, 100) == 0
+    assert size(0, 100) == 0 and size(5000, 250) == 0 and size(1, 0) == 0 and size(4, 100) == 0
     assert size(1, 100000) % 256 == 0 and size(1, 100000) > 0
-    assert size(1, 1 << 24) <= 2048 * 4 * 66 * 4 + 256
+    for n in (1, 7, 5000):      # a part of a task holds two heads' sums; 32768 parts and one a task at most
+        assert size(n, 1 << 24) <= (32768 + 2 * n) * 2 * 66 * 4 + 256
     assert size(1, 2 ** 31 - 1) == size(1, 1 << 24)     # the table's reach
     assert nt.nt_op_attn_paged_workspace(_cache(nt), 4, 1, 1 << 24) == 0     # 64 positions
     for bad in ((3, 1, 10), (4, -1, 10), (4, 1, -1)):

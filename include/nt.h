@@ -326,6 +326,33 @@ nt_status nt_op_gemm_ln(int32_t dtype, const void* d_A, int32_t lda, const void*
                         int32_t K, const float* d_colsum, float ln_eps, const float* d_bias, void* d_out,
                         int32_t ldc, int32_t relu, int32_t tile, const float* d_bscale, void* stream);
 
+/* The input half of a gated feed-forward block in one kernel: both projections, the activation
+ * and the product,
+ *   out[m][n] = act(g) u,   g = A_m . Bt_n + bias[n],   u = A_m . Bt_{N+n} + bias[N+n],
+ * d_Bt [2N][K] holding the gate's N rows, then the up projection's (W [K, 2N], columns gate | up,
+ * transposed as every matrix here).  act: NT_ACT_SILU g / (1 + e^-g), NT_ACT_GELU
+ * g (1 + erf(g / sqrt 2)) / 2, NT_ACT_GELU_TANH g (1 + tanh(sqrt(2/pi) (g + 0.044715 g^3))) / 2,
+ * NT_ACT_RELU max(g, 0).  The block's output half is nt_op_gemm with a residual.
+ *  A, Bt, out in `dtype`; rows of A lda elements apart and 16-byte aligned, rows of out ldc apart
+ *  (any alignment); bias [2N] fp32 or NULL; K % 64 == 0.  d_colsum: NULL, or [2N] fp32: the
+ *  pre-norm LayerNorm of A's rows is folded in, as for nt_op_gemm_ln: A_m . Bt_n becomes
+ *  rstd_m (A_m . Bt_n - mu_m colsum[n]) with K the whole row, colsum[n] = sum_k Bt[n][k].
+ *  Products, activation and product of the two are fp32, rounded once into out; each result is
+ *  the same whatever M and N.  out overlaps no input.  Asynchronous, one launch (A past 2^32
+ *  bytes: one for each 2^32), on the current device.  NT_E_INVALID for a null or misaligned
+ *  pointer, a bad size, act or ln_eps; NT_E_UNSUPPORTED for K % 64 != 0, Bt past 2^32 bytes or rows
+ *  of A past 2^22 bytes.
+ * Defined by: the FFN of Sec. 2.1's Transformer with a gated activation in place of ReLU, a common
+ * variant that the paper does not use. */
+typedef enum { NT_ACT_SILU = 0, NT_ACT_GELU = 1, NT_ACT_GELU_TANH = 2, NT_ACT_RELU = 3 } nt_gate_act;
+nt_status nt_op_gemm_gated(int32_t dtype, const void* d_A, int32_t lda, const void* d_Bt, int32_t M, int32_t N,
+                           int32_t K, int32_t act, const float* d_bias, const float* d_colsum, float ln_eps,
+                           void* d_out, int32_t ldc, void* stream);
+/* The tile that such a product is formed on: 32 (64x32), 64 (64x128; fp32 64x64), 128 (128x128) or
+ * 256 (256x256), over the 2N columns; ln != 0: with d_colsum.  -1 for sizes that the call refuses.
+ * Needs no device; for tests that mean to reach a certain tile. */
+int32_t nt_op_gemm_gated_rows(int32_t dtype, int32_t M, int32_t N, int32_t K, int32_t ln);
+
 /* Which tiles nt_op_gemm (ln == 0) or nt_op_gemm_ln (ln != 0) with tile = 0 forms such a
  * product on: 32 (64x32), 64 (64x128; fp32 64x64), 128 (128x128) or 256 (256x256) for the
  * tiles whose k-loop runs in phases, 0 for one of the tiles 1..4.  f8 != 0: with d_bscale;

@@ -18,6 +18,7 @@ BUILD_DIR = os.path.join(ROOT, "_build")
 LIB_PATH = os.path.join(HERE, "libnt.so")
 
 SOURCES = ["nt_gemm.hip", "nt_gemm_phased_f16.hip", "nt_gemm_phased_bf16.hip", "nt_gemm_phased_f32.hip",
+           "nt_gemm_gated_f16.hip", "nt_gemm_gated_bf16.hip", "nt_gemm_gated_f32.hip",
            "nt_norm.hip", "nt_attn.hip", "nt_paged.hip", "nt_search.hip", "nt_score.hip",
            "nt_runtime.cpp"]
 ARCH = "gfx950"

@@ -819,4 +819,40 @@ hipError_t gemm(DT dt, const void* A, int lda, const void* Bt, int M, int N, int
   return hipErrorInvalidValue;
 }
 
+// Rows of the tile a gated product runs on, counted over its 2N columns.  Measured on MI355X (us a
+// call, one after another; M x N x K of the call):
+//  * Up to 512 tiles of 64x32, two a CU, those: 3x2048x512 5.1 / 7.4 on 64x128, 500x1024x256 with a
+//    folded LayerNorm 5.7 / 6.2; 200x4096x1024 (1024 tiles) 13.3 / 9.5.
+//  * fp32 has 64x64 beside it: 4096x2048x512 148 (64x32 171), 300x1024x512 13.2 (14.2).
+//  * Then 64x128 up to one a CU, 128x128 beyond (800x2048x512, 416 of them: 8.9 / 8.2,
+//    2160x4096x1024 52 / 43).  With a folded LayerNorm, up to the three that share a CU (800x2048x512
+//    10.8 / 11.9, 1200x2048x512, 608, 14.5 / 15.4; 1600x2048x512, 800, 18.5 / 15.8, 2160x4096x1024
+//    58 / 55, 5057x4096x1024 123 / 110): the sums of squares stand between the phases, and another
+//    workgroup's phases cover them.
+//  * 256x256 where its tiles fill 90% of the rounds of CUs that they take, as for gemm_rows
+//    (16384x4096x1024 250 / 290 on 128x128; 16384x2047x512, rows at any alignment, 93 / 99;
+//    2160x4096x1024, 1.1 rounds, 53 / 43).
+int gated_rows(DT dt, int M, int N, bool ln) {
+  const auto tiles = [&](int bm, int bn) { return (long long)((M + bm - 1) / bm) * ((2ll * N + bn - 1) / bn); };
+  if (tiles(64, 32) <= 512) return 32;
+  if (dt == DT::F32) return 64;
+  const long long t64 = tiles(64, 128), t256 = tiles(256, 256);
+  if (ln) return t64 <= 768 ? 64 : 128;
+  if (t64 <= 256) return 64;
+  const long long rounds = (t256 + 255) / 256;
+  return t256 * 10 >= rounds * 256 * 9 ? 256 : 128;
+}
+
+hipError_t gemm_gated(DT dt, const void* A, int lda, const void* Bt, int M, int N, int K, const GemmEpi& epi,
+                      hipStream_t s) {
+  if (M <= 0 || N <= 0) return hipSuccess;
+  const int bm = gated_rows(dt, M, N, epi.lnf_colsum != nullptr);
+  switch (dt) {
+    case DT::F32: return gemm_gated_f32(A, lda, Bt, M, N, K, epi, s, bm);
+    case DT::F16: return gemm_gated_f16(A, lda, Bt, M, N, K, epi, s, bm);
+    case DT::BF16: return gemm_gated_bf16(A, lda, Bt, M, N, K, epi, s, bm);
+  }
+  return hipErrorInvalidValue;
+}
+
 }  // namespace nt

@@ -61,6 +61,59 @@ __device__ __forceinline__ void frag_stats(const u32x4& a, T c, float& s, float&
   }
 }
 
+// The same for a gated projection: s and q sum the values and their squares as they are, by dot
+// products of two (exact products, fp32 sums).  That takes a quarter of the operations, which stand
+// between the matrix phases, but the variance q / K - mean^2 cancels where the mean is large: a row
+// with mean^2 > ROW_RATIO var is read again (row_stats).
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+constexpr float ROW_RATIO = 64.f;
+template <typename T>
+__device__ __forceinline__ void frag_sums(const u32x4& a, float& s, float& q) {
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    const unsigned u = a[w];
+    if constexpr (std::is_same<T, f16>::value) {
+      const half2v x = __builtin_bit_cast(half2v, u);
+      s = __builtin_amdgcn_fdot2(x, half2v{(_Float16)1.0f, (_Float16)1.0f}, s, false);
+      q = __builtin_amdgcn_fdot2(x, x, q, false);
+    } else if constexpr (std::is_same<T, bf16>::value) {
+      const unsigned ones = 0x3f803f80u;
+      const bf16x2 x = __builtin_bit_cast(bf16x2, u);
+      s = __builtin_amdgcn_fdot2_f32_bf16(x, __builtin_bit_cast(bf16x2, ones), s, false);
+      q = __builtin_amdgcn_fdot2_f32_bf16(x, x, q, false);
+    } else {
+      const float x = __uint_as_float(u);
+      s += x;
+      q = fmaf(x, x, q);
+    }
+  }
+}
+// Mean and 1/sqrt(biased variance + eps) of a row of K values from its sums; the second is -1 where
+// the row has to be read again.
+__device__ __forceinline__ float2 sums_stats(float s, float q, float inv_k, float eps) {
+  const float mean = s * inv_k, var = q * inv_k - mean * mean;
+  return make_float2(mean, mean * mean > ROW_RATIO * var ? -1.f : 1.0f / sqrtf(var + eps));
+}
+// The same of the row itself, in two turns by a whole wave: the mean, then the deviations from it.
+template <typename T>
+__device__ __forceinline__ float2 row_stats(const T* row, int K, float inv_k, float eps, int lane) {
+  float s = 0.f, q = 0.f;
+  for (int i = lane * Vec<T>::N; i < K; i += kWave * Vec<T>::N) {
+    float x[Vec<T>::N];
+    load16(row + i, x);
+#pragma unroll
+    for (int e = 0; e < Vec<T>::N; ++e) s += x[e];
+  }
+  const float mean = wave_sum(s) * inv_k;
+  for (int i = lane * Vec<T>::N; i < K; i += kWave * Vec<T>::N) {
+    float x[Vec<T>::N];
+    load16(row + i, x);
+#pragma unroll
+    for (int e = 0; e < Vec<T>::N; ++e) q = fmaf(x[e] - mean, x[e] - mean, q);
+  }
+  return make_float2(mean, 1.0f / sqrtf(wave_sum(q) * inv_k + eps));
+}
+
 // Applies the epilogue MODE to up to 4 consecutive columns n..n+3 of row m (n % 4 == 0).
 // With OPS, it adds the bias (if any) and, for EPI_RESID, the residual itself; without,
 // the caller has added both (an EPI_RESID group is then a plain store).  The mode is a

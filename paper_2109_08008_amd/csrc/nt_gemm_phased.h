@@ -657,6 +657,149 @@ __device__ __forceinline__ void phased_epilogue(floatx4 (&c)[FM][FN], const Gemm
   mode_switch<ROLE>(epi.mode, direct);
 }
 
+// ---- a gated projection -----------------------------------------------------------------------
+// out = act(g) u with g and u two products of the same rows: Bt holds the gate's N rows, then the
+// up projection's N.  A tile takes them 16 rows at a time in turn -- its blocks 2q are 16 gate
+// columns, its blocks 2q + 1 the up columns of the same outputs -- so a lane ends with a gate and
+// its up value in two accumulators, and the activation and the product are all the epilogue adds to
+// a plain product of 2N columns, of whose results it stores half.  Only the rows that the direct
+// loads name differ; the matrix stays as it is.
+constexpr int GATED = 4;   // the kernels' ROLE
+__device__ __forceinline__ int gated_base(int row, int N) { return (row >> 4 & 1) * N; }         // of a tile's row
+__device__ __forceinline__ int gated_column(int row) { return (row >> 5 << 4) + (row & 15); }    //   and its output column
+
+// act(g) by EpiMode.  16-bit outputs take the hardware's exponential and reciprocal (each within an
+// ulp or two of fp32), fp32 ones the library's functions.
+template <typename T, int MODE>
+__device__ __forceinline__ float gate_act(float g) {
+  constexpr bool FAST = sizeof(T) == 2;
+  auto sigmoid = [](float x) {
+    if constexpr (FAST) return __builtin_amdgcn_rcpf(1.0f + __expf(-x));
+    else return 1.0f / (1.0f + expf(-x));
+  };
+  if constexpr (MODE == EPI_GATE_SILU) return g * sigmoid(g);
+  else if constexpr (MODE == EPI_GATE_GELU) return 0.5f * g * (1.0f + erff(g * 0.70710678118654752f));
+  // 0.5 (1 + tanh(z)) = sigmoid(2 z)
+  else if constexpr (MODE == EPI_GATE_GELU_TANH) return g * sigmoid(1.5957691216057308f * (g + 0.044715f * g * g * g));
+  else return g > 0.f ? g : g == g ? 0.f : g;
+}
+
+// Whether a wave's columns are whole and their vectors aligned (N % 4: the up half's too).
+template <bool LNF>
+__device__ __forceinline__ bool gated_whole(const GemmEpi& epi, int nw, int cols, int N) {
+  uintptr_t al = reinterpret_cast<uintptr_t>(epi.bias);
+  if (LNF) al |= reinterpret_cast<uintptr_t>(epi.lnf_colsum);
+  return nw + cols <= N && N % 4 == 0 && (al & 15) == 0;
+}
+template <int FN, bool LNF>
+__device__ __forceinline__ void gated_ahead(EpiAhead<FN>& e, const GemmEpi& epi, int N, int nw, int fc) {
+#pragma unroll
+  for (int j = 0; j < FN; ++j) {
+    const int n = (j & 1) * N + nw + j / 2 * 16 + 4 * fc;
+    if constexpr (LNF) e.colsum[j] = *reinterpret_cast<const floatx4*>(epi.lnf_colsum + n);
+    if (epi.bias) e.bias[j] = *reinterpret_cast<const float4*>(epi.bias + n);
+  }
+}
+
+// The epilogue of a wave's FM x FN blocks: lane (fr, fc) holds, of rows mw + 16 i + fr, the gate
+// (blocks 2q) and up values (2q + 1) of output columns nw + 16 q + 4 fc .. + 3.
+template <typename T, int FM, int FN, bool LNF>
+__device__ __forceinline__ void gated_epilogue(floatx4 (&c)[FM][FN], const GemmEpi& epi, int M, int N, int mw, int nw,
+                                               int fr, int fc, const float (&mu)[FM], const float (&rs)[FM],
+                                               EpiAhead<FN> e) {
+  if (!e.on) {
+    if (gated_whole<LNF>(epi, nw, FN * 8, N)) {
+      gated_ahead<FN, LNF>(e, epi, N, nw, fc);
+    } else {
+#pragma unroll
+      for (int j = 0; j < FN; ++j) {
+        float b[4], s[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int n = (j & 1) * N + min(nw + j / 2 * 16 + 4 * fc + r, N - 1);
+          b[r] = epi.bias ? epi.bias[n] : 0.f;
+          s[r] = LNF ? epi.lnf_colsum[n] : 0.f;
+        }
+        e.bias[j] = make_float4(b[0], b[1], b[2], b[3]);
+        e.colsum[j] = floatx4{s[0], s[1], s[2], s[3]};
+      }
+    }
+  }
+  auto finish = [&](auto mode_c) {
+    constexpr int MODE = decltype(mode_c)::value;
+    constexpr int W = sizeof(T) == 2 && FN >= 4 ? 2 : 1;   // blocks of 16 columns that a store of 16 bytes takes
+#pragma unroll
+    for (int i = 0; i < FM; ++i) {
+      const int m = mw + i * 16 + fr;
+#pragma unroll
+      for (int q0 = 0; q0 < FN / 2; q0 += W) {
+        float y[W][4];
+#pragma unroll
+        for (int w = 0; w < W; ++w) {
+          const int j = 2 * (q0 + w);
+          const float bg[4] = {e.bias[j].x, e.bias[j].y, e.bias[j].z, e.bias[j].w};
+          const float bu[4] = {e.bias[j + 1].x, e.bias[j + 1].y, e.bias[j + 1].z, e.bias[j + 1].w};
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            float g = c[i][j][r], u = c[i][j + 1][r];
+            if constexpr (LNF) {
+              g = (g - mu[i] * e.colsum[j][r]) * rs[i];
+              u = (u - mu[i] * e.colsum[j + 1][r]) * rs[i];
+            }
+            if (epi.bias) {
+              g += bg[r];
+              u += bu[r];
+            }
+            y[w][r] = gate_act<T, MODE>(g) * u;
+          }
+        }
+        T* row = static_cast<T*>(epi.out) + (size_t)m * epi.ldc;
+        // the lane's columns: four of each block, or with two blocks, after their words' exchange,
+        // eight of one
+        int n = nw + q0 * 16 + 4 * fc;
+        if constexpr (W == 2) {
+          uint4 x;
+          x.x = pack2<T>(y[0][0], y[0][1]);
+          x.y = pack2<T>(y[0][2], y[0][3]);
+          x.z = pack2<T>(y[1][0], y[1][1]);
+          x.w = pack2<T>(y[1][2], y[1][3]);
+          row_swap(x.x, x.z);
+          row_swap(x.y, x.w);
+          n = nw + q0 * 16 + (fc & 1) * 16 + (fc >> 1) * 8;
+          if (m >= M) continue;
+          if (n + 8 <= N) {   // (a vector store whatever the row's alignment: global memory takes any)
+            __builtin_memcpy(row + n, &x, 16);
+          } else {
+            const unsigned v[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+            for (int r = 0; r < 8; ++r) {
+              const unsigned short h = (unsigned short)(v[r / 2] >> (r % 2 * 16));
+              if (n + r < N) row[n + r] = __builtin_bit_cast(T, h);
+            }
+          }
+        } else {
+          if (m >= M) continue;
+          T v[4] = {from_f32<T>(y[0][0]), from_f32<T>(y[0][1]), from_f32<T>(y[0][2]), from_f32<T>(y[0][3])};
+          if (n + 4 <= N) {
+            __builtin_memcpy(row + n, v, sizeof(v));
+          } else {
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+              if (n + r < N) row[n + r] = v[r];
+          }
+        }
+      }
+    }
+  };
+  using std::integral_constant;
+  switch (epi.mode) {
+    case EPI_GATE_SILU: finish(integral_constant<int, EPI_GATE_SILU>{}); break;
+    case EPI_GATE_GELU: finish(integral_constant<int, EPI_GATE_GELU>{}); break;
+    case EPI_GATE_GELU_TANH: finish(integral_constant<int, EPI_GATE_GELU_TANH>{}); break;
+    default: finish(integral_constant<int, EPI_GATE_RELU>{}); break;
+  }
+}
+
 // Direct loads of a wave that may be outstanding when phase q of a k-step ends: those of the
 // six halves behind the one the phase after the next multiplies.
 constexpr int phase_vm(int la, int lb) { return 3 * la + 3 * lb; }
@@ -724,10 +867,17 @@ __global__ __launch_bounds__(W::WGM * W::WGN * kWave, 2) void gemm_phased_kernel
   const int ga = wave * LPA * 8, gb = wave * LPB * (F8 ? 16 : 8);   // first region rows of the wave
   const unsigned cha = ((lane & 7) ^ (lane >> 3)) << 4;
   const unsigned chb = F8 ? ((lane & 3) ^ (lane >> 4)) << 4 : cha;
-  const unsigned a_last = (unsigned)(M - 1) * lda_b + cha, b_last = (unsigned)(N - 1) * ldb_b + chb;
+  const unsigned a_last = (unsigned)(M - 1) * lda_b + cha;
+  unsigned b_last = (unsigned)(N - 1) * ldb_b + chb;
   unsigned a_first = (unsigned)(m0 + ga / (FMH * 16) * (FM * 16) + ga % (FMH * 16) + (lane >> 3)) * lda_b + cha;
   unsigned b_first =
       (unsigned)(n0 + gb / (FNH * 16) * (FN * 16) + gb % (FNH * 16) + (F8 ? lane >> 2 : lane >> 3)) * ldb_b + chb;
+  constexpr int HB = ROLE == GATED ? FNH * 8 : FNH * 16;   // matrix rows between a wave's halves
+  if constexpr (ROLE == GATED) {
+    const int row = gb / (FNH * 16) * (FN * 16) + gb % (FNH * 16) + (lane >> 3), base = gated_base(row, N);
+    b_last = (unsigned)(base + N - 1) * ldb_b + chb;
+    b_first = (unsigned)(base + n0 / 2 + gated_column(row)) * ldb_b + chb;
+  }
   const char* Ab = reinterpret_cast<const char*>(A);
   const char* Bb = static_cast<const char*>(Bt);
   auto off_a = [&](int h, unsigned cap, unsigned (&vo)[2]) {
@@ -736,7 +886,7 @@ __global__ __launch_bounds__(W::WGM * W::WGN * kWave, 2) void gemm_phased_kernel
   };
   auto off_b = [&](int h, unsigned cap, unsigned (&vo)[2]) {
 #pragma unroll
-    for (int i = 0; i < LPB; ++i) vo[i] = min(min(b_first + (h * (FNH * 16) + i * 8) * ldb_b, b_last), cap);
+    for (int i = 0; i < LPB; ++i) vo[i] = min(min(b_first + (h * HB + i * 8) * ldb_b, b_last), cap);
   };
   const unsigned lb = (unsigned)(uintptr_t)NT_LDS(lds);
   const unsigned ma = lb + wave * LPA * 1024, mb_ = lb + wave * LPB * 1024;   // the wave's part of a region
@@ -770,14 +920,24 @@ __global__ __launch_bounds__(W::WGM * W::WGN * kWave, 2) void gemm_phased_kernel
   u32x4 ax[FMH][2], ay[FMH][2], az[FMH][2], b0[FNH][2], b1[FNH][2], bq[FNH];
 
   // folded LayerNorm: the row statistics of the wave's rows, A half wn of them in this wave
-  // (both waves of a row hold the same fragments)
+  // (both waves of a row hold the same fragments).  GATED: of all its rows, half wn of every k-step,
+  // so that the two waves have the same to do in every phase: half of a wave's rows in one phase, the
+  // other wave's in the next, keeps each waiting for the other at the phases' barriers.
   static_assert(!LNF || WGN == 2, "two waves share a row's statistics");
-  float lsum[LNF ? FMH : 1], lsq[LNF ? FMH : 1];
-  T lsh[LNF ? FMH : 1];
+  constexpr int NS = !LNF ? 1 : ROLE == GATED ? FM : FMH;
+  float lsum[NS], lsq[NS];
+  T lsh[NS];
 #pragma unroll
-  for (int i = 0; i < (LNF ? FMH : 1); ++i) lsum[i] = lsq[i] = 0.f;
+  for (int i = 0; i < NS; ++i) lsum[i] = lsq[i] = 0.f;
   auto stats = [&](u32x4 (&a)[FMH][2], int h) {
-    if constexpr (LNF) {
+    if constexpr (LNF && ROLE == GATED) {
+#pragma unroll
+      for (int i = 0; i < FMH; ++i) {
+        const int n = h * FMH + i;
+        if (wn) frag_sums<T>(a[i][1], lsum[n], lsq[n]);
+        else frag_sums<T>(a[i][0], lsum[n], lsq[n]);
+      }
+    } else if constexpr (LNF) {
       if (wn == h) {
 #pragma unroll
         for (int k = 0; k < 2; ++k)
@@ -796,23 +956,24 @@ __global__ __launch_bounds__(W::WGM * W::WGN * kWave, 2) void gemm_phased_kernel
     }
   };
 
-  const int nk = (int)((size_t)K * sizeof(T) / ROWB);   // even (checked by the launcher)
+  const int nk = (int)((size_t)K * sizeof(T) / ROWB);   // even (checked by the launcher), or GATED
   // prologue: both slots, in the order the phases read them; A0 and B0 of the first k-step
   // (with a folded LayerNorm also A1, whose rows' first values are the statistics' shifts)
   load_a(0, 0, 0);
   load_b(0, 0, 0);
   load_a(1, 0, 0);
   load_b(1, 0, 0);
-  load_a(0, 1, 1);
-  load_b(0, 1, 1);
-  load_a(1, 1, 1);
-  load_b(1, 1, 1);
+  const int k1 = ROLE == GATED ? min(1, nk - 1) : 1;
+  load_a(0, k1, 1);
+  load_b(0, k1, 1);
+  load_a(1, k1, 1);
+  load_b(1, k1, 1);
   wait_vm<2 * LPA + 3 * LPB>();   // A0, B0 and A1 of the first k-step have landed
   __builtin_amdgcn_s_barrier();
   lds_frags<OA0>(ax, pa, pa ^ XA);
   if constexpr (F8) lds_frags8<OB0>(bq, pb);
   else lds_frags<OB0>(b0, pb, pb ^ XB);
-  if constexpr (LNF) {
+  if constexpr (LNF && ROLE != GATED) {
     lds_frags<OA1>(ay, pa, pa ^ XA);
 #pragma unroll
     for (int i = 0; i < FMH; ++i) {
@@ -872,9 +1033,13 @@ __global__ __launch_bounds__(W::WGM * W::WGN * kWave, 2) void gemm_phased_kernel
     widen(b0);
   };
   using std::integral_constant;
-  for (int kt = 0; kt < nk; kt += 2) {
+  const int pairs = ROLE == GATED ? nk & ~1 : nk;
+  for (int kt = 0; kt < pairs; kt += 2) {
     kstep(integral_constant<int, 0>{}, kt, ax, ay, az);
     kstep(integral_constant<int, 1>{}, kt + 1, az, ay, ax);
+  }
+  if constexpr (ROLE == GATED) {
+    if (nk & 1) kstep(integral_constant<int, 0>{}, nk - 1, ax, ay, az);
   }
   lane = __lane_id();             // formed again: nothing of the lane's is kept through the loop
   asm volatile("" : "+v"(lane));
@@ -887,7 +1052,47 @@ __global__ __launch_bounds__(W::WGM * W::WGN * kWave, 2) void gemm_phased_kernel
   // folded LayerNorm: mean and 1/sqrt(biased variance + eps) per tile row, as in nt_gemm.hip
   float* ln_mu = reinterpret_cast<float*>(lds + CSB);
   float* ln_rs = ln_mu + BM;
-  if constexpr (LNF) {
+  if constexpr (LNF && ROLE == GATED) {
+    const float inv_k = 1.0f / (float)K;
+    float s[FM], q[FM];
+    const int row0 = wm * (FM * 16) + fr;
+#pragma unroll
+    for (int i = 0; i < FM; ++i) {
+      s[i] = lsum[i];
+      q[i] = lsq[i];
+      s[i] += __shfl_xor(s[i], 16, kWave);
+      q[i] += __shfl_xor(q[i], 16, kWave);
+      s[i] += __shfl_xor(s[i], 32, kWave);
+      q[i] += __shfl_xor(q[i], 32, kWave);
+      if (wn == 1 && fc == 0) {
+        ln_mu[row0 + i * 16] = s[i];
+        ln_rs[row0 + i * 16] = q[i];
+      }
+    }
+    __syncthreads();
+    if (wn == 0 && fc == 0) {
+#pragma unroll
+      for (int i = 0; i < FM; ++i) {
+        const int row = row0 + i * 16;
+        const float2 r = sums_stats(s[i] + ln_mu[row], q[i] + ln_rs[row], inv_k, epi.lnf_eps);
+        ln_mu[row] = r.x;
+        ln_rs[row] = r.y;
+      }
+    }
+    __syncthreads();
+    // rows to be read again, BM / NW of them a wave
+    static_assert(BM / NW <= kWave, "a wave's rows in one ballot");
+    unsigned long long again = __ballot(lane < BM / NW && ln_rs[wave * (BM / NW) + lane % (BM / NW)] == -1.f);
+    for (; again; again &= again - 1) {
+      const int row = wave * (BM / NW) + __builtin_ctzll(again);
+      const float2 r = row_stats<T>(A + (size_t)min(m0 + row, M - 1) * lda, K, inv_k, epi.lnf_eps, lane);
+      if (lane == 0) {
+        ln_mu[row] = r.x;
+        ln_rs[row] = r.y;
+      }
+    }
+    __syncthreads();
+  } else if constexpr (LNF) {
     const float inv_k = 1.0f / (float)K;
 #pragma unroll
     for (int i = 0; i < FMH; ++i) {
@@ -913,9 +1118,13 @@ __global__ __launch_bounds__(W::WGM * W::WGN * kWave, 2) void gemm_phased_kernel
     mu[i] = LNF ? ln_mu[wm * (FM * 16) + i * 16 + fr] : 0.f;
     rs[i] = LNF ? ln_rs[wm * (FM * 16) + i * 16 + fr] : 1.f;
   }
-  phased_epilogue<T, FM, FN, ROLE, F8, LNF>(acc, epi, M, N, m0 + wm * (FM * 16), n0 + wn * (FN * 16), t_slot, fr, fc, mu,
-                                            rs, reinterpret_cast<float*>(lds) + wave * (HROWS * CS),
-                                            ln_mu + wm * (FM * 16), ln_rs + wm * (FM * 16), EpiAhead<FN>{});
+  if constexpr (ROLE == GATED)
+    gated_epilogue<T, FM, FN, LNF>(acc, epi, M, N, m0 + wm * (FM * 16), (n0 + wn * (FN * 16)) / 2, fr, fc, mu, rs,
+                                   EpiAhead<FN>{});
+  else
+    phased_epilogue<T, FM, FN, ROLE, F8, LNF>(acc, epi, M, N, m0 + wm * (FM * 16), n0 + wn * (FN * 16), t_slot, fr, fc, mu,
+                                              rs, reinterpret_cast<float*>(lds) + wave * (HROWS * CS),
+                                              ln_mu + wm * (FM * 16), ln_rs + wm * (FM * 16), EpiAhead<FN>{});
 }
 
 // ---- few tiles: 64x32, one phase a k-step ----------------------------------------------------
@@ -1085,7 +1294,10 @@ __global__ __launch_bounds__(256) void gemm_slim_kernel(const T* __restrict__ A,
   for (int i = 0; i < 2; ++i) xa[i] = (unsigned)min(m0 + (wave * 2 + i) * 8 + (lane >> 3), M - 1) * lda_b + ch;
   unsigned xb[LB];
 #pragma unroll
-  for (int i = 0; i < LB; ++i) xb[i] = (unsigned)min(n0 + (wave * LB + i) * 8 + (lane >> 3), N - 1) * ldb_b + ch;
+  for (int i = 0; i < LB; ++i) {
+    const int r = (wave * LB + i) * 8 + (lane >> 3);
+    xb[i] = (unsigned)(ROLE == GATED ? gated_base(r, N) + min(n0 / 2 + gated_column(r), N - 1) : min(n0 + r, N - 1)) * ldb_b + ch;
+  }
   const char* Ab = reinterpret_cast<const char*>(A);
   const char* Bb = static_cast<const char*>(Bt);
   const unsigned lb = (unsigned)(uintptr_t)NT_LDS(lds);
@@ -1115,10 +1327,14 @@ __global__ __launch_bounds__(256) void gemm_slim_kernel(const T* __restrict__ A,
     }
   }
   EpiAhead<FN> ahead{};
-  ahead.on = epi_whole<T, false, LNF>(epi, n0, BN, N);
+  ahead.on = ROLE == GATED ? gated_whole<LNF>(epi, n0 / 2, BN / 2, N) : epi_whole<T, false, LNF>(epi, n0, BN, N);
   // (64x64 tiles have a second workgroup's k-loop to cover the epilogue's loads: 4096x512x512 in
   // fp32 takes 21.6 us with them here, 21.3 behind the loop)
-  if (FN == 2 && ahead.on) epi_ahead<T, FN, ROLE, LNF>(ahead, epi, M, m0 + wave * 16, n0, fr, fc);
+  if constexpr (ROLE == GATED) {
+    if (ahead.on) gated_ahead<FN, LNF>(ahead, epi, N, n0 / 2, fc);
+  } else {
+    if (FN == 2 && ahead.on) epi_ahead<T, FN, ROLE, LNF>(ahead, epi, M, m0 + wave * 16, n0, fr, fc);
+  }
 #pragma unroll
   for (int kt = 2; kt < NS; ++kt) fill(kt);
   floatx4 acc[1][FN];
@@ -1137,8 +1353,9 @@ __global__ __launch_bounds__(256) void gemm_slim_kernel(const T* __restrict__ A,
   }
   __builtin_amdgcn_s_barrier();
   float ls = 0.f, lq = 0.f;
+  float ls1 = 0.f, lq1 = 0.f;   // GATED: the second halves of the k-steps by themselves
   T sh{};
-  if constexpr (LNF) sh = first_value<T>(__shfl(a0[0].x, fr, kWave));
+  if constexpr (LNF && ROLE != GATED) sh = first_value<T>(__shfl(a0[0].x, fr, kWave));
 
   unsigned s0 = 0, s1 = SLOT;   // slots of this k-step and the next
   auto kstep = [&](int kt, u32x4 (&a)[2], u32x4 (&b)[FN][2], u32x4 (&na)[2], u32x4 (&nb)[FN][2]) {
@@ -1146,7 +1363,10 @@ __global__ __launch_bounds__(256) void gemm_slim_kernel(const T* __restrict__ A,
     const unsigned qa = pa + s1, qb = pb + s1;
     SlimPhase<T, FN>::template step<0, VM>(acc, a, b, na, nb, qa, qa ^ 64, qb, qb ^ 64, xa, Ab + at, uniform(ma + s0), xb,
                                        Bb + at, uniform(mb + s0));
-    if constexpr (LNF) {
+    if constexpr (LNF && ROLE == GATED) {
+      frag_sums<T>(a[0], ls, lq);
+      frag_sums<T>(a[1], ls1, lq1);
+    } else if constexpr (LNF) {
       frag_stats<T>(a[0], sh, ls, lq);
       frag_stats<T>(a[1], sh, ls, lq);
     }
@@ -1160,9 +1380,25 @@ __global__ __launch_bounds__(256) void gemm_slim_kernel(const T* __restrict__ A,
     if (++kt >= nk) break;
   }
   mfma_drain(acc);
-  if (FN != 2 && ahead.on) epi_ahead<T, FN, ROLE, LNF>(ahead, epi, M, m0 + wave * 16, n0, fr, fc);
+  if (ROLE != GATED && FN != 2 && ahead.on) epi_ahead<T, FN, ROLE, LNF>(ahead, epi, M, m0 + wave * 16, n0, fr, fc);
   float mu[1] = {0.f}, rs[1] = {1.f};
-  if constexpr (LNF) {   // every lane of a row ends with its sums
+  if constexpr (LNF && ROLE == GATED) {   // (the order of the larger tiles, whose waves take a half each)
+    float* x[4] = {&ls, &lq, &ls1, &lq1};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      *x[i] += __shfl_xor(*x[i], 16, kWave);
+      *x[i] += __shfl_xor(*x[i], 32, kWave);
+    }
+    const float inv_k = 1.0f / (float)K;
+    float2 r = sums_stats(ls + ls1, lq + lq1, inv_k, epi.lnf_eps);
+    for (unsigned long long again = __ballot(fc == 0 && r.y == -1.f); again; again &= again - 1) {
+      const int row = __builtin_ctzll(again);
+      const float2 t = row_stats<T>(A + (size_t)min(m0 + wave * 16 + row, M - 1) * lda, K, inv_k, epi.lnf_eps, lane);
+      if (fr == row) r = t;
+    }
+    mu[0] = r.x;
+    rs[0] = r.y;
+  } else if constexpr (LNF) {   // every lane of a row ends with its sums
     const float inv_k = 1.0f / (float)K;
     ls += __shfl_xor(ls, 16, kWave);
     lq += __shfl_xor(lq, 16, kWave);
@@ -1173,14 +1409,18 @@ __global__ __launch_bounds__(256) void gemm_slim_kernel(const T* __restrict__ A,
     mu[0] = to_f32(sh) + ms;
     rs[0] = 1.0f / sqrtf(var + epi.lnf_eps);
   }
-  phased_epilogue<T, 1, FN, ROLE, false, LNF>(acc, epi, live, N, m0 + wave * 16, n0, t_slot, fr, fc, mu, rs, nullptr,
-                                              nullptr, nullptr, ahead);
+  if constexpr (ROLE == GATED)
+    gated_epilogue<T, 1, FN, LNF>(acc, epi, live, N, m0 + wave * 16, n0 / 2, fr, fc, mu, rs, ahead);
+  else
+    phased_epilogue<T, 1, FN, ROLE, false, LNF>(acc, epi, live, N, m0 + wave * 16, n0, t_slot, fr, fc, mu, rs, nullptr,
+                                                nullptr, nullptr, ahead);
   wait_vm<0>();   // no load into LDS outlives the workgroup
 }
 
 template <typename T, int FN, int NS, int ROLE, bool LNF>
 hipError_t launch_slim(const void* A, int lda, const void* Bt, int M, int N, int K, const GemmEpi& epi, hipStream_t s) {
-  const int tm = (M + 63) / 64, tn = (N + 16 * FN - 1) / (16 * FN);
+  constexpr int BN = ROLE == GATED ? 8 * FN : 16 * FN;   // output columns
+  const int tm = (M + 63) / 64, tn = (N + BN - 1) / BN;
   const dim3 grid = ROLE == 1 ? dim3(tn, tm) : dim3(tm * tn);
   NT_LAUNCH((gemm_slim_kernel<T, FN, NS, ROLE, LNF>), grid, dim3(256), 0, s, static_cast<const T*>(A), lda, Bt, M, N,
             K, epi, tm, tn);
@@ -1190,11 +1430,27 @@ hipError_t launch_slim(const void* A, int lda, const void* Bt, int M, int N, int
 template <typename T, typename W, int ROLE, bool F8, bool LNF>
 hipError_t launch_phased(const void* A, int lda, const void* Bt, int M, int N, int K, const GemmEpi& epi,
                          hipStream_t s) {
-  constexpr int BM = W::WGM * W::FMH * 32, BN = W::WGN * W::FNH * 32;
+  constexpr int BM = W::WGM * W::FMH * 32, BN = W::WGN * W::FNH * (ROLE == GATED ? 16 : 32);
   const int tm = (M + BM - 1) / BM, tn = (N + BN - 1) / BN;
   NT_LAUNCH((gemm_phased_kernel<T, W, ROLE, F8, LNF>), dim3(tm * tn), dim3(W::WGM * W::WGN * kWave), 0, s,
             static_cast<const T*>(A), lda, Bt, M, N, K, epi, tm, tn);
   return hipGetLastError();
+}
+
+// A gated product on the tile that gated_rows names.
+template <typename T, bool LNF>
+hipError_t launch_gated(const void* A, int lda, const void* Bt, int M, int N, int K, const GemmEpi& epi, hipStream_t s,
+                        int bm) {
+  if constexpr (sizeof(T) == 4) {
+    return bm == 64 ? launch_slim<T, 4, 4, GATED, LNF>(A, lda, Bt, M, N, K, epi, s)
+                    : launch_slim<T, 2, 6, GATED, LNF>(A, lda, Bt, M, N, K, epi, s);
+  } else {
+    if (bm == 32) return launch_slim<T, 2, 6, GATED, LNF>(A, lda, Bt, M, N, K, epi, s);
+    if (bm == 64) return launch_phased<T, Tile64, GATED, false, LNF>(A, lda, Bt, M, N, K, epi, s);
+    if constexpr (!LNF)
+      if (bm == 256) return launch_phased<T, Tile256, GATED, false, false>(A, lda, Bt, M, N, K, epi, s);
+    return launch_phased<T, Tile128, GATED, false, LNF>(A, lda, Bt, M, N, K, epi, s);
+  }
 }
 
 template <typename T, int ROLE, bool LNF>

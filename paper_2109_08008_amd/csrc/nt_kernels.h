@@ -59,6 +59,10 @@ enum EpiMode : int {
   EPI_TOPK = 5,       // output projection: per row and 128-column tile, the (max, sum exp,
                       // largest (value, index)) partials -- instead of the logits, or with
                       // out set, as well as the fp32 logits
+  EPI_GATE_SILU = 8,  // gated projections: out = act(gate) * up, bias and lnf_colsum [2N]
+  EPI_GATE_GELU = 9,
+  EPI_GATE_GELU_TANH = 10,
+  EPI_GATE_RELU = 11,
 };
 __host__ __device__ inline int topk_record(int k2) { return 2 + 2 * k2; }   // floats per partial record
 
@@ -131,6 +135,22 @@ hipError_t gemm_phased_bf16(const void* A, int lda, const void* Bt, int M, int N
 // The phased tiles in fp32: 64 x bn, bn = 32, or 64 for encoder launches.
 hipError_t gemm_slim_f32(const void* A, int lda, const void* Bt, int M, int N, int K, const GemmEpi& epi,
                          hipStream_t s, int role, int bn);
+
+// A gated projection: out[M][N] = act(A . Bt[0..N)^T) * (A . Bt[N..2N)^T), each product with its
+// bias and folded LayerNorm as above (epi.mode: one of EPI_GATE_*; bias and lnf_colsum [2N]).
+// K * type size is a multiple of 128 bytes; A and Bt are 16-byte aligned and, with 256 rows more,
+// stay below 2^32 bytes.
+hipError_t gemm_gated(DT dt, const void* A, int lda, const void* Bt, int M, int N, int K, const GemmEpi& epi,
+                      hipStream_t s);
+// The tile it forms them on, by rows: 32 (64x32, of 16 outputs a row), 64 (64x128; fp32 64x64),
+// 128 (128x128) or 256 (256x256).  Host only.
+int gated_rows(DT dt, int M, int N, bool ln);
+hipError_t gemm_gated_f16(const void* A, int lda, const void* Bt, int M, int N, int K, const GemmEpi& epi, hipStream_t s,
+                          int bm);
+hipError_t gemm_gated_bf16(const void* A, int lda, const void* Bt, int M, int N, int K, const GemmEpi& epi, hipStream_t s,
+                           int bm);
+hipError_t gemm_gated_f32(const void* A, int lda, const void* Bt, int M, int N, int K, const GemmEpi& epi, hipStream_t s,
+                          int bm);
 
 // The output projection's logits of chosen (row, 128-column tile) pairs, recomputed: for
 // every block of epi.gblk, the rows of its pairs times the tile's columns of Bt (N = V

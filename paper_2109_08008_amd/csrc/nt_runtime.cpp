@@ -1320,6 +1320,13 @@ nt_status paged_attn_cut(int n_heads, int n_seqs, int max_len, nt::PagedAttnArgs
   return NT_OK;
 }
 
+// Operands of a gated projection within the kernels' 32-bit offsets (tiles name up to 256 rows past
+// the last one before they are bounded).
+constexpr size_t kLim32 = (size_t)1 << 32;
+bool gated_fits(size_t eb, int lda, int N, int K) {
+  return (2 * (size_t)N + 512) * K * eb < kLim32 && (size_t)lda * eb * 1024 < kLim32;
+}
+
 // The cut of a nt_op_token_logp call and the bytes its parts take.
 nt_status token_logp_cut(int dtype, int rows, int V, int k, nt::TokenLogpArgs* a, size_t* bytes) {
   if (dtype < NT_F32 || dtype > NT_BF16) return fail(NT_E_INVALID, "unknown dtype %d", dtype);
@@ -1955,6 +1962,47 @@ nt_status nt_op_gemm_ln(int32_t dtype, const void* d_A, int32_t lda, const void*
   e.lnf_eps = ln_eps;
   NT_HIP(nt::gemm(static_cast<DT>(dtype), d_A, lda, d_Bt, M, N, K, e, static_cast<hipStream_t>(stream), 1, tile));
   return NT_OK;
+}
+
+nt_status nt_op_gemm_gated(int32_t dtype, const void* d_A, int32_t lda, const void* d_Bt, int32_t M, int32_t N,
+                           int32_t K, int32_t act, const float* d_bias, const float* d_colsum, float ln_eps,
+                           void* d_out, int32_t ldc, void* stream) {
+  g_err.clear();
+  if (!d_A || !d_Bt || !d_out) return fail(NT_E_INVALID, "null argument to nt_op_gemm_gated");
+  if (dtype < NT_F32 || dtype > NT_BF16) return fail(NT_E_INVALID, "unknown dtype %d", dtype);
+  if (act < NT_ACT_SILU || act > NT_ACT_RELU) return fail(NT_E_INVALID, "unknown activation %d", act);
+  if (M < 0 || N <= 0 || K <= 0) return fail(NT_E_INVALID, "need M >= 0, N > 0, K > 0");
+  if (K % 64 != 0) return fail(NT_E_UNSUPPORTED, "need K %% 64 == 0");
+  const size_t eb = nt::dt_bytes(static_cast<DT>(dtype));
+  if (lda < K || (lda * eb) % 16 != 0 || ldc < N)
+    return fail(NT_E_INVALID, "lda must be >= K with 16-byte rows, ldc >= N");
+  if ((reinterpret_cast<uintptr_t>(d_A) | reinterpret_cast<uintptr_t>(d_Bt)) & 15)
+    return fail(NT_E_INVALID, "A and Bt must be 16-byte aligned");
+  if (reinterpret_cast<uintptr_t>(d_out) % eb) return fail(NT_E_INVALID, "out must be aligned to its type");
+  if (d_colsum && !(ln_eps > 0.f)) return fail(NT_E_INVALID, "ln_eps must be positive");
+  if (!gated_fits(eb, lda, N, K)) return fail(NT_E_UNSUPPORTED, "Bt must stay below 2^32 bytes, rows of A below 2^22");
+  nt::GemmEpi e{};
+  e.mode = nt::EPI_GATE_SILU + act;
+  e.bias = d_bias;
+  e.ldc = ldc;
+  e.lnf_colsum = d_colsum;
+  e.lnf_eps = ln_eps;
+  // the kernels' offsets into A are 32 bits: the rows of a launch stay below that
+  const int most = (int)std::min<size_t>(M, (kLim32 / (lda * eb) - 256) / 256 * 256);
+  for (int m = 0; m < M; m += most) {
+    e.out = static_cast<char*>(d_out) + (size_t)m * ldc * eb;
+    NT_HIP(nt::gemm_gated(static_cast<DT>(dtype), static_cast<const char*>(d_A) + (size_t)m * lda * eb, lda, d_Bt,
+                          std::min(M - m, most), N, K, e, static_cast<hipStream_t>(stream)));
+  }
+  return NT_OK;
+}
+
+int32_t nt_op_gemm_gated_rows(int32_t dtype, int32_t M, int32_t N, int32_t K, int32_t ln) {
+  if (dtype < NT_F32 || dtype > NT_BF16 || M < 0 || N <= 0 || K <= 0 || K % 64 != 0) return -1;
+  const size_t eb = nt::dt_bytes(static_cast<DT>(dtype));
+  if (!gated_fits(eb, K, N, K)) return -1;
+  const int most = (int)std::min<size_t>(M, (kLim32 / (K * eb) - 256) / 256 * 256);
+  return nt::gated_rows(static_cast<DT>(dtype), most, N, ln != 0);
 }
 
 int32_t nt_op_gemm_rows(int32_t dtype, int32_t lda, int32_t M, int32_t N, int32_t K, int32_t ln, int32_t f8,

@@ -33,8 +33,10 @@ EXPORTS = [
     "nt_op_select_tiled", "nt_op_select_tiled_noalloc",
     "nt_ensemble", "nt_quantize_fp8", "nt_op_kv_append", "nt_op_attn_paged", "nt_op_attn_paged_workspace",
     "nt_op_token_logp", "nt_op_token_logp_workspace",
+    "nt_op_gemm_gated", "nt_op_gemm_gated_rows",
 ]
 NT_ENS_MEAN_LOGP, NT_ENS_LOG_MEAN_P = 0, 1
+GATE_ACTS = {"silu": 0, "gelu": 1, "gelu_tanh": 2, "relu": 3}   # include/nt.h: nt_gate_act
 NT_SELECT_NOALLOC_MAX_RECORDS = 1 << 20   # include/nt.h: records of nt_op_select_tiled_noalloc
 
 
@@ -116,6 +118,9 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
         "nt_op_gemm_ln": (c_int32, [c_int32, P, c_int32, P, c_int32, c_int32, c_int32, P, c_float, P, P, c_int32,
                                     c_int32, c_int32, P, P]),
         "nt_op_gemm_rows": (c_int32, [c_int32] * 8),
+        "nt_op_gemm_gated": (c_int32, [c_int32, P, c_int32, P, c_int32, c_int32, c_int32, c_int32, P, P, c_float, P,
+                                       c_int32, P]),
+        "nt_op_gemm_gated_rows": (c_int32, [c_int32] * 5),
         "nt_op_token_logp": (c_int32, [c_int32, P, c_int32, c_int32, c_int32, P, c_int32, c_int32, P, P, P, P, P, P,
                                        c_size_t, P]),
         "nt_op_token_logp_workspace": (c_int32, [c_int32] * 4 + [POINTER(c_size_t)]),
@@ -295,6 +300,17 @@ def nt_op_gemm_ln(dtype: str, d_A: int, lda: int, d_Bt: int, M: int, N: int, K: 
 def nt_op_gemm_rows(dtype: str, M: int, N: int, K: int, ln: bool = False, f8: bool = False, out_f32: bool = False,
                     lda: int = 0) -> int:
     return load_library().nt_op_gemm_rows(DTYPES[dtype], lda or K, M, N, K, int(ln), int(f8), int(out_f32))
+
+
+def nt_op_gemm_gated(dtype: str, d_A: int, lda: int, d_Bt: int, M: int, N: int, K: int, act: str, d_bias, d_out: int,
+                     ldc: int, d_colsum=None, ln_eps: float = 1e-5, stream=None):
+    """act: a name of GATE_ACTS."""
+    _check(load_library().nt_op_gemm_gated(DTYPES[dtype], d_A, lda, d_Bt, M, N, K, GATE_ACTS[act], d_bias, d_colsum, ln_eps,
+                                           d_out, ldc, _stream(stream)))
+
+
+def nt_op_gemm_gated_rows(dtype: str, M: int, N: int, K: int, ln: bool = False) -> int:
+    return load_library().nt_op_gemm_gated_rows(DTYPES[dtype], M, N, K, int(ln))
 
 
 def nt_quantize_fp8(w: np.ndarray):

@@ -826,8 +826,8 @@ hipError_t gemm(DT dt, const void* A, int lda, const void* Bt, int M, int N, int
 //  * fp32 has 64x64 beside it: 4096x2048x512 148 (64x32 171), 300x1024x512 13.2 (14.2).
 //  * Then 64x128 up to one a CU, 128x128 beyond (800x2048x512, 416 of them: 8.9 / 8.2,
 //    2160x4096x1024 52 / 43).  With a folded LayerNorm, up to the three that share a CU (800x2048x512
-//    10.8 / 11.9, 1200x2048x512, 608, 14.5 / 15.4; 1600x2048x512, 800, 18.5 / 15.8, 2160x4096x1024
-//    58 / 55, 5057x4096x1024 123 / 110): the sums of squares stand between the phases, and another
+//    10.2 / 11.3, 1200x2048x512, 608, 13.9 / 14.8; 1600x2048x512, 800, 17.8 / 15.2, 2160x4096x1024
+//    55 / 51, 5057x4096x1024 118 / 102): the sums of squares stand between the phases, and another
 //    workgroup's phases cover them.
 //  * 256x256 where its tiles fill 90% of the rounds of CUs that they take, as for gemm_rows
 //    (16384x4096x1024 250 / 290 on 128x128; 16384x2047x512, rows at any alignment, 93 / 99;

@@ -930,20 +930,20 @@ __global__ __launch_bounds__(W::WGM * W::WGN * kWave, 2) void gemm_phased_kernel
 #pragma unroll
   for (int i = 0; i < NS; ++i) lsum[i] = lsq[i] = 0.f;
   auto stats = [&](u32x4 (&a)[FMH][2], int h) {
-    if constexpr (LNF && ROLE == GATED) {
-#pragma unroll
-      for (int i = 0; i < FMH; ++i) {
-        const int n = h * FMH + i;
-        if (wn) frag_sums<T>(a[i][1], lsum[n], lsq[n]);
-        else frag_sums<T>(a[i][0], lsum[n], lsq[n]);
-      }
-    } else if constexpr (LNF) {
+    if constexpr (LNF && ROLE != GATED) {
       if (wn == h) {
 #pragma unroll
         for (int k = 0; k < 2; ++k)
 #pragma unroll
           for (int i = 0; i < FMH; ++i) frag_stats<T>(a[i][k], lsh[i], lsum[i], lsq[i]);
       }
+    }
+  };
+  auto sums = [&](auto half_c, u32x4 (&a)[FMH][2], int h) {
+    if constexpr (LNF && ROLE == GATED) {
+#pragma unroll
+      for (int i = 0; i < FMH; ++i)
+        frag_sums<T>(a[i][decltype(half_c)::value], lsum[h * FMH + i], lsq[h * FMH + i]);
     }
   };
   auto widen = [&](u32x4 (&b)[FNH][2]) {
@@ -989,7 +989,7 @@ __global__ __launch_bounds__(W::WGM * W::WGN * kWave, 2) void gemm_phased_kernel
   // One k-step in slot S.  A0 is in a0 and B0 in b0 on entry, the next k-step's in a2 and b0 on
   // return.  Refills past the last k-step read the operand's first line only.
   constexpr int VM = phase_vm(LPA, LPB);
-  auto kstep = [&](auto slot_c, int kt, u32x4 (&a0)[FMH][2], u32x4 (&a1)[FMH][2], u32x4 (&a2)[FMH][2]) {
+  auto kstep = [&](auto half_c, auto slot_c, int kt, u32x4 (&a0)[FMH][2], u32x4 (&a1)[FMH][2], u32x4 (&a2)[FMH][2]) {
     constexpr int S = decltype(slot_c)::value;
     constexpr int SO = S * SLOT, SN = (1 - S) * SLOT;
     const bool in2 = kt + 2 < nk, in3 = kt + 3 < nk;
@@ -1008,6 +1008,7 @@ __global__ __launch_bounds__(W::WGM * W::WGN * kWave, 2) void gemm_phased_kernel
       Ph::template read_a<0, 0, OA1, LPB, VM>(acc, a0, b0, a1, p, p ^ XA, vo, B2, mb_ + SO + OB0);
     }
     stats(a0, 0);
+    sums(half_c, a0, 0);
     // (A1, B0); reads B1, refills A1
     {
       off_a(1, cap2, vo);
@@ -1016,6 +1017,7 @@ __global__ __launch_bounds__(W::WGM * W::WGN * kWave, 2) void gemm_phased_kernel
       else Ph::template read_b<FMH, 0, OB1, LPA, VM>(acc, a1, b0, b1, p, p ^ XB, vo, A2, ma + SO + OA1);
     }
     stats(a1, 1);
+    sums(half_c, a1, 1);
     widen(b1);
     // (A1, B1); reads the next A0, refills B1
     {
@@ -1033,13 +1035,23 @@ __global__ __launch_bounds__(W::WGM * W::WGN * kWave, 2) void gemm_phased_kernel
     widen(b0);
   };
   using std::integral_constant;
-  const int pairs = ROLE == GATED ? nk & ~1 : nk;
-  for (int kt = 0; kt < pairs; kt += 2) {
-    kstep(integral_constant<int, 0>{}, kt, ax, ay, az);
-    kstep(integral_constant<int, 1>{}, kt + 1, az, ay, ax);
-  }
-  if constexpr (ROLE == GATED) {
-    if (nk & 1) kstep(integral_constant<int, 0>{}, nk - 1, ax, ay, az);
+  constexpr integral_constant<int, 0> lower{};
+  if constexpr (ROLE != GATED) {
+    for (int kt = 0; kt < nk; kt += 2) {
+      kstep(lower, integral_constant<int, 0>{}, kt, ax, ay, az);
+      kstep(lower, integral_constant<int, 1>{}, kt + 1, az, ay, ax);
+    }
+  } else {
+    auto ksteps = [&](auto half_c) {
+      for (int kt = 0; kt < (nk & ~1); kt += 2) {
+        kstep(half_c, integral_constant<int, 0>{}, kt, ax, ay, az);
+        kstep(half_c, integral_constant<int, 1>{}, kt + 1, az, ay, ax);
+      }
+      if (nk & 1) kstep(half_c, integral_constant<int, 0>{}, nk - 1, ax, ay, az);
+    };
+    // (a loop for each half of the row sums: chosen inside, it would take a select a word)
+    if (LNF && wn) ksteps(integral_constant<int, 1>{});
+    else ksteps(lower);
   }
   lane = __lane_id();             // formed again: nothing of the lane's is kept through the loop
   asm volatile("" : "+v"(lane));

@@ -14,12 +14,17 @@
 // quads of threads give a threshold that the row's k best reach, only the threads whose
 // maximum reaches it look at their values again, and each value found counts the ones
 // before it under (value desc, index asc).  A row with more than SCORE_CAP values at the
-// threshold (ties, above all 16-bit ones) raises it to the k-th best of those collected
-// and collects again, until what is above it fits; then the lowest indices at the
+// threshold (ties, above all 16-bit ones) raises it to the k-th best of some of those
+// collected and collects again, until what is above it fits; then the lowest indices at the
 // threshold fill up.  So the result never depends on the order of arrival.
 //
-// Few rows are cut into parts over workgroups; a part leaves (m, s, t) and its k best, and
-// logp_join_kernel merges them.
+// Few long rows are cut into parts over workgroups; a part leaves (m, s, t) and its k best, and
+// logp_join_kernel merges them.  Short rows are a wave's each (short_logp_kernel).
+//
+// Measured, us (GB/s): 4000 rows of 32000 fp32 values, k = 8, 86 (5960; k = 0 82); 8192 of 32001
+// bf16, k = 5, 100 (5240; k = 0 87); 1300 of 32000 fp32 36 (4600: every row is in flight at once, and
+// nothing covers their ends); 8192 of 1000 bf16 14; 2 of 131072 fp32, k = 20, 12.7 in two launches.
+// Reads alone reach 6200 GB/s on this card, 7000 non-temporal.
 #include <limits.h>
 
 #include <algorithm>
@@ -53,15 +58,26 @@ __device__ __forceinline__ Stats wave_stats(Stats a, float best) {
   return {m, wave_sum(a.s), wave_sum(a.t)};
 }
 
+__device__ __forceinline__ void wave_fence() {   // orders a wave's own LDS accesses
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+}
 // (value desc, index asc)
 __device__ __forceinline__ bool before(float v1, int i1, float v2, int i2) { return v1 > v2 || (v1 == v2 && i1 < i2); }
 
 // The candidates of a workgroup: `n` (value, index) pairs, and how many come before one.
 struct Candidates {
-  __attribute__((aligned(16))) float v[SCORE_CAP + 4];
-  __attribute__((aligned(16))) int i[SCORE_CAP + 4];
+  __attribute__((aligned(16))) float v[SCORE_CAP + 8];   // (-inf, INT_MAX) behind the last
+  __attribute__((aligned(16))) int i[SCORE_CAP + 8];
   int count;
 };
+__device__ __forceinline__ void clear(Candidates& c) {   // by the workgroup; a barrier before the first put
+  for (int e = threadIdx.x; e < SCORE_CAP + 8; e += SCORE_THREADS) {
+    c.v[e] = -INFINITY;
+    c.i[e] = INT_MAX;
+  }
+  if (threadIdx.x == 0) c.count = 0;
+}
 __device__ __forceinline__ void put(Candidates& c, float x, int i) {
   const int at = atomicAdd(&c.count, 1);
   if (at < SCORE_CAP) {
@@ -69,21 +85,17 @@ __device__ __forceinline__ void put(Candidates& c, float x, int i) {
     c.i[at] = i;
   }
 }
-// Entries up to the next multiple of four behind the last are before none.  Call between two barriers.
-__device__ __forceinline__ void pad(Candidates& c, int n) {
-  if (threadIdx.x < 4) {
-    c.v[n + threadIdx.x] = -INFINITY;
-    c.i[n + threadIdx.x] = INT_MAX;
-  }
-}
-__device__ __forceinline__ int rank_of(const Candidates& c, int n, int e) {
-  const float x = c.v[e];
-  const int i = c.i[e];
+// How many of the first n come before entry e (what lies behind them, up to a multiple of eight, is
+// before none).
+__device__ __forceinline__ int rank_of(const float* cv, const int* ci, int n, int e) {
+  const float x = cv[e];
+  const int i = ci[e];
   int at = 0;
-  for (int j = 0; j < n; j += 4) {
-    const float4 v = *reinterpret_cast<const float4*>(c.v + j);
-    const int4 w = *reinterpret_cast<const int4*>(c.i + j);
-    at += before(v.x, w.x, x, i) + before(v.y, w.y, x, i) + before(v.z, w.z, x, i) + before(v.w, w.w, x, i);
+  for (int j = 0; j < n; j += 8) {
+    const float4 v0 = *reinterpret_cast<const float4*>(cv + j), v1 = *reinterpret_cast<const float4*>(cv + j + 4);
+    const int4 w0 = *reinterpret_cast<const int4*>(ci + j), w1 = *reinterpret_cast<const int4*>(ci + j + 4);
+    at += before(v0.x, w0.x, x, i) + before(v0.y, w0.y, x, i) + before(v0.z, w0.z, x, i) + before(v0.w, w0.w, x, i) +
+          before(v1.x, w1.x, x, i) + before(v1.y, w1.y, x, i) + before(v1.z, w1.z, x, i) + before(v1.w, w1.w, x, i);
   }
   return at;
 }
@@ -219,7 +231,7 @@ __global__ __launch_bounds__(SCORE_THREADS) void token_logp_kernel(TokenLogpArgs
     token = a.tokens[(size_t)row * a.n_tok + tid];
     if ((unsigned)token < (unsigned)a.V) given = to_f32(x[token]);
   }
-  if (tid == 0) cand.count = 0;
+  if (a.k > 0) clear(cand);
   // `head` single values up to a 128-byte line (a load that straddles lines fetches both: 8192 rows
   // of 32001 bf16 values 98 us from 16-byte boundaries, of 32000 89), nv vectors and a tail; threads
   // 0 .. HEAD - 1 take the head's, the next ones the tail's
@@ -338,25 +350,43 @@ __global__ __launch_bounds__(SCORE_THREADS) void token_logp_kernel(TokenLogpArgs
     const float c = to_f32(x[single]);
     if (c >= thr && c != -INFINITY) put(cand, c, single);
   }
-  if (first >= thr && first != -INFINITY) {
-    u32x4 q[SCORE_BATCH];
-    if (batches <= 1) {   // still at hand
+  // The wave's candidate threads, G at a time: a lane for each value of their best batches.  (Each
+  // thread going through its own values took 350 instructions of every wave for the few that have
+  // any: a third of what a row of 32000 16-bit values takes in all.)
+  unsigned long long who = __ballot(first >= thr && first != -INFINITY);
+  constexpr int PER = SCORE_BATCH * VN, G = kWave / PER;
+  while (who && *(volatile int*)&cand.count <= SCORE_CAP) {
+    int l = -1, batch = 0;
 #pragma unroll
-      for (int u = 0; u < SCORE_BATCH; ++u) q[u] = q0[u];
-    } else {
-      load(q, first_batch);
+    for (int g = 0; g < G; ++g) {
+      const int next = who ? __builtin_ctzll(who) : -1;
+      who &= who - 1;   // (0 stays 0)
+      if (lane / PER == g) {
+        l = next;
+        batch = readlane_i(first_batch, max(next, 0));
+      }
     }
-#pragma unroll
-    for (int u = 0; u < SCORE_BATCH; ++u) {
-      const int i = tid + (first_batch * SCORE_BATCH + u) * NT;
-      if (i < nv) take_values(q[u], i);
+    const int e = lane % PER, i = wave * kWave + l + (batch * SCORE_BATCH + e / VN) * NT;
+    const bool in = l >= 0 && i < nv;
+    const int at = in ? head + VN * i + e % VN : 0;
+    const float c = in ? to_f32(x[at]) : -INFINITY;
+    const bool hit = c >= thr && c != -INFINITY;
+    const unsigned long long hits = __ballot(hit);
+    if (!hits) continue;
+    int base = 0;
+    if (lane == 0) base = atomicAdd(&cand.count, __popcll(hits));
+    const int place = __builtin_amdgcn_readfirstlane(base) +
+                      __builtin_amdgcn_mbcnt_hi((unsigned)(hits >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)hits, 0));
+    if (hit && place < SCORE_CAP) {
+      cand.v[place] = c;
+      cand.i[place] = at;
     }
   }
   // The few threads with a second batch that reaches it: the wave goes through their other vectors,
   // lane u reading u, u + 64, .. (Reading all of every candidate thread's again, a 128-byte line for
   // each 16 bytes, took a quarter of a long call: 4000 rows of 32000 fp32 values, k = 8, 102 us
   // against 82 with k = 0.)
-  unsigned long long who = __ballot(second >= thr && second != -INFINITY);
+  who = __ballot(second >= thr && second != -INFINITY);
   while (who && *(volatile int*)&cand.count <= SCORE_CAP) {
     const int l = __builtin_ctzll(who), skip = readlane_i(first_batch, l);
     who &= who - 1;
@@ -369,16 +399,22 @@ __global__ __launch_bounds__(SCORE_THREADS) void token_logp_kernel(TokenLogpArgs
   int found = cand.count;
   if (found > SCORE_CAP) {
     do {
-      // raise the threshold to the k-th best of those collected: k values reach it
-      for (int e = tid; e < SCORE_CAP; e += NT)
-        if (rank_of(cand, SCORE_CAP, e) == a.k - 1) raised = cand.v[e];
+      // raise the threshold to the k-th best of some of those collected: k values reach it
+      constexpr int SAMPLE = 128;
+      static_assert(SAMPLE <= SCORE_CAP && SAMPLE <= NT, "an entry a thread");
+      if (tid < SAMPLE && rank_of(cand.v, cand.i, SAMPLE, tid) == a.k - 1) raised = cand.v[tid];
       __syncthreads();
       thr = raised;
-      if (tid == 0) cand.count = 0;
       __syncthreads();
-      for (int i = tid; i < n; i += NT) {
-        const float c = to_f32(x[i]);
-        if (c > thr) put(cand, c, i);
+      clear(cand);
+      __syncthreads();
+      for (int i0 = tid; i0 < n; i0 += 16 * NT) {
+        T c[16];
+#pragma unroll
+        for (int u = 0; u < 16; ++u) c[u] = x[min(i0 + u * NT, n - 1)];
+#pragma unroll
+        for (int u = 0; u < 16; ++u)
+          if (i0 + u * NT < n && to_f32(c[u]) > thr) put(cand, to_f32(c[u]), i0 + u * NT);
       }
       __syncthreads();
       found = cand.count;
@@ -404,12 +440,10 @@ __global__ __launch_bounds__(SCORE_THREADS) void token_logp_kernel(TokenLogpArgs
       __syncthreads();
     }
   }
-  pad(cand, found);
-  __syncthreads();
   // each candidate's place is the number of candidates before it
   const size_t out = ((size_t)row * a.parts + part) * a.k;
   for (int e = tid; e < found; e += NT) {
-    const int at = rank_of(cand, found, e);
+    const int at = rank_of(cand.v, cand.i, found, e);
     if (at >= a.k) continue;
     if (a.parts == 1) {
       a.topi[out + at] = cand.i[e];
@@ -430,26 +464,164 @@ __global__ __launch_bounds__(SCORE_THREADS) void token_logp_kernel(TokenLogpArgs
   }
 }
 
+// Rows of up to SHORT values: a wave a row, its values in registers, and everything within the wave.
+// The threshold is the k-th largest of the lanes' maxima.  Past SHORT_CAP values at it (ties), k turns
+// of a wave-wide search for the next one.
+// (A workgroup a row has most of its threads idle and half its groups empty: 8192 rows of 1000 bf16
+// values, k = 5, took 38 us, with k = 32, where no threshold came of them, 566.)
+constexpr int SHORT = 2048, SHORT_CAP = 192;
+template <typename T>
+__global__ __launch_bounds__(256) void short_logp_kernel(TokenLogpArgs a) {
+  constexpr int NJ = SHORT / kWave;
+  __shared__ __attribute__((aligned(16))) float cv[4][SHORT_CAP + 8];
+  __shared__ __attribute__((aligned(16))) int ci[4][SHORT_CAP + 8];
+  __shared__ __attribute__((aligned(16))) float best[4][kWave];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
+  const int row = blockIdx.x * 4 + wave;
+  if (row >= a.rows) return;            // whole wave; no workgroup barrier below
+  const T* x = static_cast<const T*>(a.logits) + (size_t)row * a.ld;
+  T raw[NJ];                            // (all under way together: nothing looks at one before)
+#pragma unroll
+  for (int j = 0; j < NJ; ++j) raw[j] = x[min(j * kWave + lane, a.V - 1)];
+  int token = -1;
+  float given = 0.f;
+  if (lane < a.n_tok) {
+    token = a.tokens[(size_t)row * a.n_tok + lane];
+    if ((unsigned)token < (unsigned)a.V) given = to_f32(x[token]);
+  }
+  float v[NJ], mine = -INFINITY;
+#pragma unroll
+  for (int j = 0; j < NJ; ++j) {
+    v[j] = j * kWave + lane < a.V ? to_f32(raw[j]) : -INFINITY;
+    mine = fmaxf(mine, v[j]);
+  }
+  const float m = wave_max(mine), ref = m == -INFINITY ? 0.f : m;
+  float s = 0.f, t = 0.f;
+#pragma unroll
+  for (int j = 0; j < NJ; ++j) {
+    if (j * kWave >= a.V) break;
+    const float d = v[j] - ref, p = __builtin_amdgcn_exp2f(d * LOG2E);
+    s += p;
+    t = fmaf(p, fmaxf(d, -1e30f), t);   // 0, not NaN, of a logit of -inf
+  }
+  s = wave_sum(s);
+  t = wave_sum(t);
+  const float log_s = logf(s);
+  if (lane == 0) {
+    const bool none = s == 0.f;           // no logit above -inf
+    if (a.lse) a.lse[row] = none ? -INFINITY : m + log_s;
+    if (a.entropy) a.entropy[row] = none ? 0.f : log_s - t / s;
+  }
+  for (int j = lane; j < a.n_tok; j += kWave) {
+    if (j >= kWave) {
+      token = a.tokens[(size_t)row * a.n_tok + j];
+      if ((unsigned)token < (unsigned)a.V) given = to_f32(x[token]);
+    }
+    const float lp = given == -INFINITY && s == s ? -INFINITY : (given - m) - log_s;
+    a.logp[(size_t)row * a.n_tok + j] = (unsigned)token < (unsigned)a.V ? lp : 0.f;
+  }
+  if (a.k == 0) return;
+  best[wave][lane] = mine;
+  wave_fence();
+  int above = 0;
+#pragma unroll
+  for (int j = 0; j < kWave; j += 4) {
+    const float4 o = *reinterpret_cast<const float4*>(&best[wave][j]);
+    above += (o.x > mine) + (o.y > mine) + (o.z > mine) + (o.w > mine);
+  }
+  const float thr = -wave_max(above < a.k ? -mine : -INFINITY);
+  int found = 0;
+#pragma unroll
+  for (int j = 0; j < NJ; ++j) {
+    if (j * kWave >= a.V) break;
+    const bool hit = v[j] >= thr && v[j] != -INFINITY;
+    const unsigned long long hits = __ballot(hit);
+    if (!hits) continue;
+    const int place = found + __builtin_amdgcn_mbcnt_hi((unsigned)(hits >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)hits, 0));
+    if (hit && place < SHORT_CAP) {
+      cv[wave][place] = v[j];
+      ci[wave][place] = j * kWave + lane;
+    }
+    found += __popcll(hits);
+  }
+  const size_t out = (size_t)row * a.k;
+  if (found <= SHORT_CAP) {
+    if (lane < 8) {
+      cv[wave][found + lane] = -INFINITY;
+      ci[wave][found + lane] = INT_MAX;
+    }
+    wave_fence();
+    for (int e = lane; e < found; e += kWave) {
+      const int at = rank_of(cv[wave], ci[wave], found, e);
+      if (at < a.k) {
+        a.topi[out + at] = ci[wave][e];
+        a.toplp[out + at] = (cv[wave][e] - m) - log_s;
+      }
+    }
+  } else {
+    float pv = INFINITY;
+    int pi = -1;
+    for (found = 0; found < a.k; ++found) {   // the best behind (pv, pi)
+      float bv = -INFINITY;
+      int bi = INT_MAX;
+#pragma unroll
+      for (int j = NJ - 1; j >= 0; --j) {
+        const int i = j * kWave + lane;
+        if (before(pv, pi, v[j], i) && v[j] >= bv && v[j] != -INFINITY) {
+          bv = v[j];
+          bi = i;
+        }
+      }
+#pragma unroll
+      for (int o = 1; o < kWave; o <<= 1) {
+        const float ov = __shfl_xor(bv, o, kWave);
+        const int oi = __shfl_xor(bi, o, kWave);
+        if (before(ov, oi, bv, bi)) {
+          bv = ov;
+          bi = oi;
+        }
+      }
+      if (bi == INT_MAX) break;
+      if (lane == 0) {
+        a.topi[out + found] = bi;
+        a.toplp[out + found] = (bv - m) - log_s;
+      }
+      pv = bv;
+      pi = bi;
+    }
+  }
+  for (int e = found + lane; e < a.k; e += kWave) {   // fewer logits above -inf than k
+    a.topi[out + e] = INT_MAX;
+    a.toplp[out + e] = -INFINITY;
+  }
+}
+
 // Merges a row's parts: their statistics, and of their k best each the row's.
 template <typename T>
 __global__ __launch_bounds__(SCORE_THREADS) void logp_join_kernel(TokenLogpArgs a) {
   constexpr int NT = SCORE_THREADS;
-  static_assert(SCORE_PARTS <= kWave && SCORE_PARTS % 4 == 0 && SCORE_PARTS * 32 <= 4 * NT, "four entries a thread");
+  static_assert(SCORE_PARTS <= kWave && SCORE_PARTS % 4 == 0, "a part a lane");
   static_assert(SCORE_PARTS == 32 && SCORE_CAP >= 32 * 33 / 2, "what is left of the entries fits");
   __shared__ __attribute__((aligned(16))) float hv[SCORE_PARTS];   // the parts' best
   __shared__ Candidates cand;
   const int row = blockIdx.x, tid = threadIdx.x, lane = tid % kWave;
   const int n = a.parts * a.k;
+  // thread t takes places t % 8, t % 8 + 8, .. of part t / 8
+  static_assert(NT == 8 * SCORE_PARTS, "eight threads a part");
+  const int own = tid / 8;
   float ev[4];
   int ei[4];
 #pragma unroll
   for (int u = 0; u < 4; ++u) {
-    const int e = tid + u * NT;
-    ev[u] = e < n ? a.part_v[(size_t)row * n + e] : -INFINITY;
-    ei[u] = e < n ? a.part_i[(size_t)row * n + e] : INT_MAX;
+    const int place = tid % 8 + 8 * u;
+    const bool in = own < a.parts && place < a.k;
+    const size_t e = (size_t)row * n + (in ? own * a.k + place : 0);
+    ev[u] = a.k > 8 * u ? a.part_v[e] : 0.f;
+    ei[u] = a.k > 8 * u ? a.part_i[e] : INT_MAX;
+    if (!in) ei[u] = INT_MAX;
   }
   if (a.k > 0 && tid < SCORE_PARTS) hv[tid] = tid < a.parts ? a.part_v[(size_t)row * n + tid * a.k] : -INFINITY;
-  if (tid == 0) cand.count = 0;
+  if (a.k > 0) clear(cand);
   Stats all{-INFINITY, 0.f, 0.f};
   if (lane < a.parts) {
     const float4 q = *reinterpret_cast<const float4*>(a.part_stats + ((size_t)row * a.parts + lane) * 4);
@@ -478,8 +650,8 @@ __global__ __launch_bounds__(SCORE_THREADS) void logp_join_kernel(TokenLogpArgs 
   // list of a few k.
 #pragma unroll
   for (int u = 0; u < 4; ++u) {
-    if (u * NT >= n) break;
-    const int e = tid + u * NT, own = e / a.k, place = e - own * a.k;
+    if (8 * u >= a.k) break;
+    const int place = tid % 8 + 8 * u;
     int heads = 0;
 #pragma unroll
     for (int j = 0; j < SCORE_PARTS; j += 4) {
@@ -488,15 +660,13 @@ __global__ __launch_bounds__(SCORE_THREADS) void logp_join_kernel(TokenLogpArgs 
                (j + 2 < own ? v.z >= ev[u] : v.z > ev[u]) + (j + 3 < own ? v.w >= ev[u] : v.w > ev[u]);
     }
     // (its own part's best, where that is above it, is one of the `place` already)
-    if (ev[u] < hv[min(own, SCORE_PARTS - 1)]) --heads;
-    if (e < n && ei[u] != INT_MAX && place + heads < a.k) put(cand, ev[u], ei[u]);
+    if (ev[u] < hv[own]) --heads;
+    if (ei[u] != INT_MAX && place + heads < a.k) put(cand, ev[u], ei[u]);
   }
   __syncthreads();
   const int found = cand.count;   // at most k + (k - 1) + .. + 1 of them
-  pad(cand, found);
-  __syncthreads();
   for (int e = tid; e < found; e += NT) {
-    const int at = rank_of(cand, found, e);
+    const int at = rank_of(cand.v, cand.i, found, e);
     if (at < a.k) {
       a.topi[(size_t)row * a.k + at] = cand.i[e];
       a.toplp[(size_t)row * a.k + at] = (cand.v[e] - all.m) - log_s;
@@ -510,6 +680,10 @@ __global__ __launch_bounds__(SCORE_THREADS) void logp_join_kernel(TokenLogpArgs 
 
 template <typename T>
 hipError_t logp_launch(const TokenLogpArgs& a, hipStream_t s) {
+  if (a.V <= SHORT) {
+    NT_LAUNCH((short_logp_kernel<T>), dim3((unsigned)((a.rows + 3) / 4)), dim3(256), 0, s, a);
+    return hipGetLastError();
+  }
   NT_LAUNCH((token_logp_kernel<T>), dim3((unsigned)(a.rows * a.parts)), dim3(SCORE_THREADS), 0, s, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.parts == 1) return e;
@@ -519,11 +693,15 @@ hipError_t logp_launch(const TokenLogpArgs& a, hipStream_t s) {
 
 }  // namespace
 
+// A row of fewer than 160 KB is one workgroup's: the join costs what the parts save (fp32, k = 8, us
+// whole / in parts of 8 KB: 1 row of 32000 9.4 / 9.3, 100 rows 13.3 / 12.6; k = 20, 2 rows of 131072
+// 22.4 / 12.4, 64 rows of 131072 bf16 values 27 / 19).  Longer ones are cut while that makes no more
+// than 1024 workgroups.
 void token_logp_plan(DT dt, TokenLogpArgs* a) {
   const long long row_bytes = (long long)a->V * dt_bytes(dt);
-  long long parts = a->rows > 0 ? 1024 / a->rows : 1;
-  parts = std::min(parts, row_bytes / 16384);
-  parts = std::max(1ll, std::min<long long>(parts, SCORE_PARTS));
+  long long parts = 1;
+  if (row_bytes >= 160 << 10 && a->rows > 0)
+    parts = std::max(1ll, std::min<long long>({1024 / a->rows, row_bytes / 8192, SCORE_PARTS}));
   a->part_len = (int)((a->V + parts - 1) / parts);
   a->parts = (a->V + a->part_len - 1) / a->part_len;
 }

@@ -28,7 +28,7 @@ def test_refusals(nt, kw, code):   # noqa: F811
 
 def test_workspace_sizes(nt):   # noqa: F811
     size = nt.nt_op_token_logp_workspace
-    assert size("f32", 5000, 32000, 8) == 0 and size("f32", 1, 1000, 8) == 0 and size("bf16", 0, 100000, 8) == 0
+    assert size("f32", 5000, 32000, 8) == 0 and size("f32", 1, 1000, 8) == 0 and size("f32", 1, 32000, 8) == 0 and size("bf16", 0, 100000, 8) == 0
     assert 0 < size("f32", 1, 1 << 30, 32) <= 32 * (4 + 64) * 4 + 256
     assert size("f32", 1, 100000, 32) % 256 == 0
     lib = nt.load_library()

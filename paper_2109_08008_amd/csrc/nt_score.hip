@@ -91,6 +91,7 @@ __device__ __forceinline__ int rank_of(const float* cv, const int* ci, int n, in
   const float x = cv[e];
   const int i = ci[e];
   int at = 0;
+#pragma unroll 1
   for (int j = 0; j < n; j += 8) {
     const float4 v0 = *reinterpret_cast<const float4*>(cv + j), v1 = *reinterpret_cast<const float4*>(cv + j + 4);
     const int4 w0 = *reinterpret_cast<const int4*>(ci + j), w1 = *reinterpret_cast<const int4*>(ci + j + 4);

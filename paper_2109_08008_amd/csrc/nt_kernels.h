@@ -284,6 +284,7 @@ struct KvAppendArgs {
   const int* off;             // [n_seqs + 1] first new row of each sequence (null: row b is
   const int* lens;            //   sequence b's only one); [n_seqs] lengths, new rows included
   int n_seqs, rows;
+  int piece_shift, wave_rows;   // lanes a row (1 << piece_shift), rows a wave; set by kv_append
 };
 hipError_t kv_append(const KvAppendArgs& a, hipStream_t s);
 

@@ -25,56 +25,93 @@ __device__ __forceinline__ unsigned e4m3_4(float a, float b, float c, float d) {
 }
 
 // ---- append ----------------------------------------------------------------------------
-// One wave a new row: the row's keys and values in 16-byte pieces, each to its head's page.
-// A move of rows, so HBM and the launch bound it; the row's sequence is found by a search of
-// 64 probes at a time (off is sorted), under way together with the row's own loads.
-template <typename T, bool F8>
+// A move of rows: HBM and the launch bound it.  A wave takes a.wave_rows rows in turns of `across`
+// at a time, 1 << piece_shift lanes (16-byte pieces) a row, U turns' loads of keys and values under
+// way together, and each lane finds one of the rows' places meanwhile: its sequence (off is sorted) by
+// 64 probes that the lanes share and a search between two of them.  Measured, us (GB/s): 19.8k rows of
+// 16 x 64 fp16 values to E4M3 26.5 (4680; a copy reaches 4940), of 8 x 128 bf16 26.3 (6140); 73k rows
+// of 4 x 32 bf16 14.9 (5050; one row a wave took 36); 96 rows of 8 x 64 3.9.  Eight turns for rows of
+// more than one turn, four for the others (the second case with four 30; 200k rows of 32 fp32 values,
+// with eight 23.5, four 19.7).
+template <typename T, bool F8, int U>
 __global__ __launch_bounds__(256) void kv_append_kernel(KvAppendArgs a) {
-  constexpr int VN = Vec<T>::N, U = 4;   // pieces of keys and of values a lane has in flight
+  constexpr int VN = Vec<T>::N;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
-  const int row = blockIdx.x * 4 + wave;
-  if (row >= a.rows) return;
+  const int first = (blockIdx.x * 4 + wave) * a.wave_rows;
+  if (first >= a.rows) return;
   const int width = a.c.n_kv_heads * a.c.d_head, pieces = width / VN;
-  const T* k = static_cast<const T*>(a.k) + (size_t)row * a.ld;
-  const T* v = static_cast<const T*>(a.v) + (size_t)row * a.ld;
-  u32x4 kq[U], vq[U];
-  auto load = [&](int p0) {
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int p = min(p0 + u * kWave + lane, pieces - 1);   // (past the last: again, not stored)
-      kq[u] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(k + p * VN));
-      vq[u] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(v + p * VN));
+  const int lanes = 1 << a.piece_shift, across = kWave >> a.piece_shift;
+  const int r = lane >> a.piece_shift, p = lane & (lanes - 1);
+  const int chunks = (pieces + lanes - 1) >> a.piece_shift;   // turns a row
+  const int turns = a.wave_rows / across * chunks;
+  const T* k = static_cast<const T*>(a.k);
+  const T* v = static_cast<const T*>(a.v);
+  struct Turn { int t, row, piece; };   // of the lane, rows counted from `first`
+  auto next = [&](Turn& n) {
+    ++n.t;
+    n.piece += lanes;
+    if (n.piece - p >= chunks * lanes) {
+      n.piece = p;
+      n.row += across;
     }
   };
-  load(0);
-  // the row's sequence b and its position: the sequence's last new row is its last position
-  int b = row, behind = 1;
-  if (a.off) {
-    int lo = 0, hi = a.n_seqs;   // entries off[1..n_seqs] at or below the row: lo..hi of them
-    while (lo < hi) {
-      const int step = (hi - lo + kWave - 1) / kWave, at = lo + (lane + 1) * step;
-      const int n = __popcll(__ballot(at <= hi && a.off[min(at, hi)] <= row));
-      hi = min(hi, lo + (n + 1) * step - 1);
-      lo += n * step;
-      if (step == 1) break;
-    }
-    b = lo;
-    if (b >= a.n_seqs || a.off[b] > row) return;   // not a row of any sequence
-    behind = a.off[b + 1] - row;
-  }
-  const int pos = a.lens[b] - behind;
-  if (pos < 0 || (pos >> a.c.page_shift) >= a.c.max_pages) return;
-  const int page = a.c.table[(size_t)b * a.c.max_pages + (pos >> a.c.page_shift)];
-  if ((unsigned)page >= (unsigned)a.c.n_pages) return;
-  const int slot = pos & ((1 << a.c.page_shift) - 1);
-  const size_t cell = ((size_t)page * a.c.n_kv_heads << a.c.page_shift) + slot;
-  for (int p0 = 0;;) {
+  u32x4 kq[U], vq[U];
+  Turn ahead{0, r, p};
+  auto load = [&] {                     // (past the rows' or the row's end: the last again, not stored)
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int p = p0 + u * kWave + lane;
-      if (p >= pieces) continue;
-      const int h = p * VN / a.c.d_head, x = p * VN - h * a.c.d_head;
-      const size_t at = (cell + ((size_t)h << a.c.page_shift)) * a.c.d_head + x;
+      if (ahead.t >= turns) break;
+      const size_t at = (size_t)min(first + ahead.row, a.rows - 1) * a.ld + min(ahead.piece, pieces - 1) * VN;
+      kq[u] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(k + at));
+      vq[u] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(v + at));
+      next(ahead);
+    }
+  };
+  load();
+  // lane l: the cell of row first + l, -1 if it has none
+  long long cell = -1;
+  {
+    const int row = first + min(lane, a.wave_rows - 1);
+    int b = row, behind = 1;            // the sequence's last new row is its last position
+    if (a.off) {
+      // entries off[1 .. n_seqs] at or below the row: lo of them
+      const int step = (a.n_seqs + kWave - 1) / kWave;
+      const int probe = a.off[min((lane + 1) * step, a.n_seqs)];
+      int lo = 0;
+#pragma unroll
+      for (int s = kWave / 2; s; s >>= 1)
+        if (__shfl(probe, lo + s - 1, kWave) <= row) lo += s;
+      if (lo == kWave - 1 && __shfl(probe, kWave - 1, kWave) <= row) lo = kWave;
+      int hi = min((lo + 1) * step - 1, a.n_seqs);
+      lo = min(lo * step, a.n_seqs);
+      while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (a.off[mid] <= row) lo = mid;
+        else hi = mid - 1;
+      }
+      b = lo;
+      behind = b < a.n_seqs && a.off[b] <= row ? a.off[b + 1] - row : 0;   // 0: not a row of any sequence
+    }
+    if (lane < a.wave_rows && row < a.rows && behind > 0) {
+      const int pos = a.lens[b] - behind;
+      if (pos >= 0 && (pos >> a.c.page_shift) < a.c.max_pages) {
+        const int page = a.c.table[(size_t)b * a.c.max_pages + (pos >> a.c.page_shift)];
+        if ((unsigned)page < (unsigned)a.c.n_pages)
+          cell = (((long long)page * a.c.n_kv_heads) << a.c.page_shift) + (pos & ((1 << a.c.page_shift) - 1));
+      }
+    }
+  }
+  const int dsh = 31 - __builtin_clz(a.c.d_head);   // 32, 64 or 128
+  for (Turn now{0, r, p};;) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (now.t >= turns) break;
+      const long long at0 = __shfl(cell, now.row, kWave);
+      const int e = now.piece * VN, h = e >> dsh, x = e & (a.c.d_head - 1);
+      const bool has = now.piece < pieces && at0 >= 0;
+      next(now);
+      if (!has) continue;
+      const size_t at = ((size_t)at0 + ((size_t)h << a.c.page_shift)) * a.c.d_head + x;
       if constexpr (F8) {
         static_assert(VN == 8, "E4M3 caches take 16-bit rows");
         auto codes = [](u32x4 q) {
@@ -89,9 +126,8 @@ __global__ __launch_bounds__(256) void kv_append_kernel(KvAppendArgs a) {
         *reinterpret_cast<u32x4*>(static_cast<T*>(a.c.v) + at) = vq[u];
       }
     }
-    p0 += U * kWave;
-    if (p0 >= pieces) break;
-    load(p0);
+    if (now.t >= turns) break;
+    load();
   }
 }
 
@@ -126,12 +162,30 @@ __device__ __forceinline__ void wave_fence() {   // orders a wave's own LDS acce
   __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
 }
 
-template <typename T, int DH, typename KV, int SW>
+typedef int int2v __attribute__((ext_vector_type(2)));
+// Eight bytes of one column likewise: each lane of 16 names the 8 bytes at row r + lane / 2 (any
+// eight rows), columns 8 (lane % 2).., and receives column lane.
+__device__ __forceinline__ uint2 lds_column8(const unsigned char* p) {
+  return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr8_b64_v2i32(
+                                       (__attribute__((address_space(3))) int2v*)(p)));
+}
+
+// Keys of a tile: those of a P.V step, and twice that for the short rows of E4M3 keys, so that they
+// too have bytes enough under way (us with 32 / 64 keys: E4M3, d_head 64, 79 x 3 heads of 76..7691
+// keys 34.2 / 33.2; but d_head 128, 2184 x 16 of 9 keys 43 / 65, fp16, d_head 32, 33 x 3 of 72423
+// 208 / 220).
+template <typename T, int DH, typename KV>
+constexpr int tile_keys() {
+  return sizeof(T) == 4 ? (DH == 32 ? 32 : 16) : sizeof(KV) == 1 && DH <= 64 ? 64 : 32;
+}
+
+template <typename T, int DH, typename KV, int SW, bool ONCE>
 __global__ __launch_bounds__(256) void paged_attn_kernel(PagedAttnArgs a) {
   constexpr int EB = sizeof(T), EC = sizeof(KV);
   constexpr bool F8 = EC == 1;
-  constexpr int TK = EB == 2 ? 32 : 16;               // keys of a tile: one MFMA step of P.V
-  constexpr int NB = TK / 16;                         // 16-key blocks
+  constexpr int TK = tile_keys<T, DH, KV>();
+  constexpr int NB = TK / 16;                         // 16-key blocks of a tile
+  constexpr int SB = EB == 2 ? 2 : 1;                 // of them in an MFMA step of P.V
   constexpr int QK = DH * EB / 64;                    // MFMA steps over the channels
   constexpr int CB = DH / 16;                         // blocks of 16 channels of the output
   constexpr int RB = DH * EC;                         // bytes of a key
@@ -139,20 +193,31 @@ __global__ __launch_bounds__(256) void paged_attn_kernel(PagedAttnArgs a) {
   constexpr int NP = TK * ROWP / kWave;               // pieces a lane takes of a tile's keys
   constexpr int RPL = kWave / ROWP;                   // rows that one load of the wave covers
   // LDS rows, padded against bank conflicts
-  constexpr int KSTR = RB + 16, VSTR = DH * EB + (EB == 2 ? 32 : 16);
+  constexpr int KSTR = RB + 16, VSTR = RB + (EC == 2 ? 32 : 16), OSTR = DH * EB + 16;
   constexpr int KBYTES = TK * KSTR, WBYTES = KBYTES + TK * VSTR;
-  static_assert(TK * ROWP % kWave == 0, "a tile's rows split evenly over the lanes");
-  static_assert(16 * DH * 4 <= WBYTES || SW == 1, "the outputs to join fit in the tiles' LDS");
+  static_assert(TK * ROWP % kWave == 0 && NB % SB == 0, "a tile's rows split evenly over the lanes");
+  static_assert((SW == 1 ? 16 * OSTR : 16 * DH * 4) <= WBYTES && WBYTES % 16 == 0, "outputs fit in the tiles' LDS");
   __shared__ __attribute__((aligned(16))) unsigned char lds[4 * WBYTES];
   __shared__ float jm[4][16], jl[4][16];
 
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
   const int grp = lane >> 4, ln = lane & 15;
-  const int n_tasks = a.n_seqs * a.c.n_kv_heads * a.qblocks;
-  const int unit = SW == 1 ? blockIdx.x * 4 + wave : blockIdx.x;
-  const int part = unit / n_tasks, task = unit - part * n_tasks;
-  if (part >= a.parts) return;                        // (SW == 1: the grid's tail)
-  const int qb = task % a.qblocks, bh = task / a.qblocks;
+  // Blocks of 16 heads of one key head read the same keys (ONCE: there is one block, and the reads
+  // are non-temporal): side by side in a workgroup, or eight workgroups apart, on one XCD, whose L2
+  // then has them.
+  const int heads = a.n_seqs * a.c.n_kv_heads;
+  int unit, qb;
+  if constexpr (SW == 1) {
+    unit = blockIdx.x * 4 + wave;
+    qb = unit % a.qblocks;
+    unit /= a.qblocks;
+  } else {
+    const int x = blockIdx.x / 8;
+    qb = x % a.qblocks;
+    unit = x / a.qblocks * 8 + blockIdx.x % 8;
+  }
+  const int part = unit / heads, bh = unit - part * heads;
+  if (part >= a.parts) return;                        // the grid's tail
   const int hk = bh % a.c.n_kv_heads, b = bh / a.c.n_kv_heads;
   const int len = max(0, min(a.lens[b], a.max_len));  // max_len is at most the table's reach
   const int c0 = part * a.chunk, c1 = min(len, c0 + a.chunk);
@@ -188,6 +253,12 @@ __global__ __launch_bounds__(256) void paged_attn_kernel(PagedAttnArgs a) {
     }
     return p;
   };
+  auto any_hole = [&](const Pages& p) {
+    int x = p.id[0];
+#pragma unroll
+    for (int j = 1; j < NB; ++j) x |= p.id[j];
+    return x < 0;
+  };
   // A tile's rows of a pool, whole lines a load: lane l takes piece l % ROWP of row l / ROWP + RPL u.
   // Rows behind the length re-read the last one; of a hole, some page's (both masked below).
   const int row0 = lane / ROWP, col = lane % ROWP * 16;
@@ -200,14 +271,21 @@ __global__ __launch_bounds__(256) void paged_attn_kernel(PagedAttnArgs a) {
 #pragma unroll
       for (int u = 0; u < NP; ++u) {
         const int row = row0 + u * RPL;
-        r[u] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(
-            (RPL <= 16 ? at[u * RPL / 16] : at[NB > 1 && row >= 16]) + (row & 15) * RB));
+        const char* base = RPL <= 16 ? at[u * RPL / 16] : row0 >= 16 ? at[u * RPL / 16 + 1] : at[u * RPL / 16];
+        const u32x4* q = reinterpret_cast<const u32x4*>(base + (row & 15) * RB);
+        if constexpr (ONCE) r[u] = __builtin_nontemporal_load(q);
+        else r[u] = *q;
       }
     } else {
 #pragma unroll
       for (int u = 0; u < NP; ++u) {
         const int row = min(row0 + u * RPL, last);
-        r[u] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(at[NB > 1 && row >= 16] + (row & 15) * RB));
+        const char* base = at[0];
+#pragma unroll
+        for (int j = 1; j < NB; ++j) base = row >= 16 * j ? at[j] : base;
+        const u32x4* q = reinterpret_cast<const u32x4*>(base + (row & 15) * RB);
+        if constexpr (ONCE) r[u] = __builtin_nontemporal_load(q);
+        else r[u] = *q;
       }
     }
   };
@@ -256,25 +334,20 @@ __global__ __launch_bounds__(256) void paged_attn_kernel(PagedAttnArgs a) {
         }
         sc[j] = acc;
       }
-      // the tile's values to LDS, in the model dtype.  What lies behind the length, or on no page,
-      // may be anything: no 0 * NaN from it
-      if (t + TK > len || pg.id[0] < 0 || pg.id[NB - 1] < 0) {
+      // The tile's values to LDS.  What lies behind the length, or on no page, may be anything: no
+      // 0 * NaN from it
+      if (t + TK > len || any_hole(pg)) {
 #pragma unroll
         for (int u = 0; u < NP; ++u) {
           const int row = row0 + u * RPL;
-          if (t + row >= len || (NB > 1 && row >= 16 ? pg.id[NB - 1] : pg.id[0]) < 0) vr[u] = u32x4{0, 0, 0, 0};
+          int id = pg.id[0];
+#pragma unroll
+          for (int j = 1; j < NB; ++j) id = row >= 16 * j ? pg.id[j] : id;
+          if (t + row >= len || id < 0) vr[u] = u32x4{0, 0, 0, 0};
         }
       }
 #pragma unroll
-      for (int u = 0; u < NP; ++u) {
-        unsigned char* d = vs + (row0 + u * RPL) * VSTR + col * (F8 ? 2 : 1);
-        if constexpr (F8) {
-          *reinterpret_cast<u32x4*>(d) = f8_to_f16x8(vr[u].x, vr[u].y);
-          *reinterpret_cast<u32x4*>(d + 16) = f8_to_f16x8(vr[u].z, vr[u].w);
-        } else {
-          *reinterpret_cast<u32x4*>(d) = vr[u];
-        }
-      }
+      for (int u = 0; u < NP; ++u) *reinterpret_cast<u32x4*>(vs + (row0 + u * RPL) * VSTR + col) = vr[u];
       if (more) load(Vp, tn, pn, vr);
       float cmax = -INFINITY;
 #pragma unroll
@@ -309,28 +382,38 @@ __global__ __launch_bounds__(256) void paged_attn_kernel(PagedAttnArgs a) {
         }
       }
       wave_fence();
-      if constexpr (EB == 2) {
-        T pe[8];
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
+      for (int j = 0; j < NB; j += SB) {
+        if constexpr (EB == 2) {
+          T pe[8];
 #pragma unroll
-          for (int r = 0; r < 4; ++r) pe[4 * j + r] = from_f32<T>(sc[j][r]);
-        const u32x4 pf = __builtin_bit_cast(u32x4, pe);
-        const unsigned char* vcol = vs + (4 * grp + (ln >> 2)) * VSTR + (ln & 3) * 8;
+          for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int c = 0; c < CB; ++c) {
-          const uint2 lo = lds_column4(vcol + c * 32), hi = lds_column4(vcol + 16 * VSTR + c * 32);
-          o[c] = Mfma<T>::step(pf, u32x4{lo.x, lo.y, hi.x, hi.y}, o[c]);
-        }
-      } else {
-        const u32x4 pf = __builtin_bit_cast(u32x4, sc[0]);
-        const unsigned char* vrow = vs + 4 * grp * VSTR + ln * 4;
+            for (int r = 0; r < 4; ++r) pe[4 * i + r] = from_f32<T>(sc[j + i][r]);
+          const u32x4 pf = __builtin_bit_cast(u32x4, pe);
+          // the lane's part of the columns' reads: rows 4 grp.. of both blocks
+          const unsigned char* vcol = F8 ? vs + (16 * (j + (ln >> 3)) + 4 * grp + (ln >> 1 & 3)) * VSTR + (ln & 1) * 8
+                                         : vs + (16 * j + 4 * grp + (ln >> 2)) * VSTR + (ln & 3) * 8;
 #pragma unroll
-        for (int c = 0; c < CB; ++c) {
-          u32x4 vf;
+          for (int c = 0; c < CB; ++c) {
+            if constexpr (F8) {
+              const uint2 w = lds_column8(vcol + c * 16);
+              o[c] = Mfma<T>::step(pf, f8_to_f16x8(w.x, w.y), o[c]);
+            } else {
+              const uint2 lo = lds_column4(vcol + c * 32), hi = lds_column4(vcol + 16 * VSTR + c * 32);
+              o[c] = Mfma<T>::step(pf, u32x4{lo.x, lo.y, hi.x, hi.y}, o[c]);
+            }
+          }
+        } else {
+          const u32x4 pf = __builtin_bit_cast(u32x4, sc[j]);
+          const unsigned char* vrow = vs + (16 * j + 4 * grp) * VSTR + ln * 4;
 #pragma unroll
-          for (int r = 0; r < 4; ++r) vf[r] = *reinterpret_cast<const unsigned*>(vrow + r * VSTR + c * 64);
-          o[c] = Mfma<T>::step(pf, vf, o[c]);
+          for (int c = 0; c < CB; ++c) {
+            u32x4 vf;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) vf[r] = *reinterpret_cast<const unsigned*>(vrow + r * VSTR + c * 64);
+            o[c] = Mfma<T>::step(pf, vf, o[c]);
+          }
         }
       }
       wave_fence();
@@ -344,7 +427,7 @@ __global__ __launch_bounds__(256) void paged_attn_kernel(PagedAttnArgs a) {
 
   T* out = static_cast<T*>(a.out) + (size_t)b * a.out_ld + (size_t)h0 * DH;
   const size_t prow = ((size_t)part * a.n_seqs + b) * a.n_heads + h0;   // of the workspace
-  if constexpr (SW == 1) {
+  if constexpr (SW == 1) {   // the rows through LDS, to leave in 16-byte pieces
     const float inv = lsum == 0.f ? 0.f : 1.0f / lsum;
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
@@ -352,14 +435,19 @@ __global__ __launch_bounds__(256) void paged_attn_kernel(PagedAttnArgs a) {
       const float ir = __shfl(inv, i, kWave);
       if (i < nq)
 #pragma unroll
-        for (int c = 0; c < CB; ++c) out[i * DH + c * 16 + ln] = from_f32<T>(o[c][r] * ir);
+        for (int c = 0; c < CB; ++c)
+          *reinterpret_cast<T*>(ks + i * OSTR + (c * 16 + ln) * EB) = from_f32<T>(o[c][r] * ir);
     }
+    wave_fence();
+    constexpr int OP = DH * EB / 16;
+    for (int e = lane; e < nq * OP; e += kWave)
+      *reinterpret_cast<u32x4*>(reinterpret_cast<char*>(out + e / OP * DH) + e % OP * 16) =
+          *reinterpret_cast<const u32x4*>(ks + e / OP * OSTR + e % OP * 16);
     return;
   } else {
     // a wave's outputs lie where its own tiles were
     constexpr int JW = WBYTES / 4;
     float* jo = reinterpret_cast<float*>(lds);
-    static_assert(WBYTES % 16 == 0, "16-byte rows");
     if (grp == 0) {
       jm[wave][ln] = m;
       jl[wave][ln] = lsum;
@@ -464,13 +552,13 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnArgs a) {
   }
 }
 
-template <typename T, int DH, typename KV>
+template <typename T, int DH, typename KV, bool ONCE>
 hipError_t attn_launch(const PagedAttnArgs& a, hipStream_t s) {
-  const unsigned units = (unsigned)(a.n_seqs * a.c.n_kv_heads * a.qblocks * a.parts);
+  const unsigned units = (unsigned)(a.n_seqs * a.c.n_kv_heads * a.parts);
   if (a.waves == 1) {
-    NT_LAUNCH((paged_attn_kernel<T, DH, KV, 1>), dim3((units + 3) / 4), dim3(256), 0, s, a);
+    NT_LAUNCH((paged_attn_kernel<T, DH, KV, 1, ONCE>), dim3((units * a.qblocks + 3) / 4), dim3(256), 0, s, a);
   } else {
-    NT_LAUNCH((paged_attn_kernel<T, DH, KV, 4>), dim3(units), dim3(256), 0, s, a);
+    NT_LAUNCH((paged_attn_kernel<T, DH, KV, 4, ONCE>), dim3((units + 7) / 8 * 8 * a.qblocks), dim3(256), 0, s, a);
   }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.parts == 1) return e;
@@ -478,29 +566,49 @@ hipError_t attn_launch(const PagedAttnArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
+template <typename T, int DH, typename KV>
+hipError_t attn_once(const PagedAttnArgs& a, hipStream_t s) {
+  return a.qblocks == 1 ? attn_launch<T, DH, KV, true>(a, s) : attn_launch<T, DH, KV, false>(a, s);
+}
+
 template <typename T, typename KV>
 hipError_t attn_dh(const PagedAttnArgs& a, hipStream_t s) {
   switch (a.c.d_head) {
-    case 32: return attn_launch<T, 32, KV>(a, s);
-    case 64: return attn_launch<T, 64, KV>(a, s);
-    case 128: return attn_launch<T, 128, KV>(a, s);
+    case 32: return attn_once<T, 32, KV>(a, s);
+    case 64: return attn_once<T, 64, KV>(a, s);
+    case 128: return attn_once<T, 128, KV>(a, s);
     default: return hipErrorInvalidValue;
   }
 }
 
+template <typename T, bool F8>
+void append_launch(const KvAppendArgs& a, bool wide, dim3 grid, hipStream_t s) {
+  if (wide) NT_LAUNCH((kv_append_kernel<T, F8, 8>), grid, dim3(256), 0, s, a);
+  else NT_LAUNCH((kv_append_kernel<T, F8, 4>), grid, dim3(256), 0, s, a);
+}
+
 }  // namespace
 
-hipError_t kv_append(const KvAppendArgs& a, hipStream_t s) {
-  if (a.rows <= 0) return hipSuccess;
-  const dim3 grid((unsigned)((a.rows + 3) / 4));
+hipError_t kv_append(const KvAppendArgs& args, hipStream_t s) {
+  if (args.rows <= 0) return hipSuccess;
+  KvAppendArgs a = args;
+  const int pieces = (int)(a.c.n_kv_heads * a.c.d_head * dt_bytes(a.c.dt) / 16);   // 4 at least
+  a.piece_shift = 2;
+  while (a.piece_shift < 6 && 1 << a.piece_shift < pieces) ++a.piece_shift;
+  const int chunks = (pieces + (1 << a.piece_shift) - 1) >> a.piece_shift;
+  const bool wide = chunks > 1;
+  a.wave_rows = (kWave >> a.piece_shift) * std::max(1, (wide ? 8 : 4) / chunks);   // at most 64
+  // few rows: as many waves as there are
+  while (a.wave_rows > kWave >> a.piece_shift && (long long)a.rows < 4096ll * a.wave_rows) a.wave_rows /= 2;
+  const dim3 grid((unsigned)((a.rows + 4ll * a.wave_rows - 1) / (4 * a.wave_rows)));
   if (a.c.fp8 && a.c.dt != DT::F16) return hipErrorInvalidValue;   // the E4M3 cache pairs with fp16
   switch (a.c.dt) {
-    case DT::F32: NT_LAUNCH((kv_append_kernel<float, false>), grid, dim3(256), 0, s, a); break;
+    case DT::F32: append_launch<float, false>(a, wide, grid, s); break;
     case DT::F16:
-      if (a.c.fp8) NT_LAUNCH((kv_append_kernel<f16, true>), grid, dim3(256), 0, s, a);
-      else NT_LAUNCH((kv_append_kernel<f16, false>), grid, dim3(256), 0, s, a);
+      if (a.c.fp8) append_launch<f16, true>(a, wide, grid, s);
+      else append_launch<f16, false>(a, wide, grid, s);
       break;
-    case DT::BF16: NT_LAUNCH((kv_append_kernel<bf16, false>), grid, dim3(256), 0, s, a); break;
+    case DT::BF16: append_launch<bf16, false>(a, wide, grid, s); break;
   }
   return hipGetLastError();
 }

@@ -338,8 +338,8 @@ nt_status nt_op_gemm_ln(int32_t dtype, const void* d_A, int32_t lda, const void*
  *  pre-norm LayerNorm of A's rows is folded in, as for nt_op_gemm_ln: A_m . Bt_n becomes
  *  rstd_m (A_m . Bt_n - mu_m colsum[n]) with K the whole row, colsum[n] = sum_k Bt[n][k].
  *  Products, activation and product of the two are fp32, rounded once into out; each result is
- *  the same whatever M and N.  out overlaps no input.  Asynchronous, one launch (A past 2^32
- *  bytes: one for each 2^32), on the current device.  NT_E_INVALID for a null or misaligned
+ *  the same whatever M and N.  out overlaps no input.  Asynchronous, one launch (more for A past
+ *  2^32 bytes), on the current device.  NT_E_INVALID for a null or misaligned
  *  pointer, a bad size, act or ln_eps; NT_E_UNSUPPORTED for K % 64 != 0, Bt past 2^32 bytes or rows
  *  of A past 2^22 bytes.
  * Defined by: the FFN of Sec. 2.1's Transformer with a gated activation in place of ReLU, a common
@@ -422,8 +422,8 @@ nt_status nt_op_select_tiled_noalloc(const float* d_logits, int32_t rows, int32_
  * that is 0), in use until the call's work is done: calls that may overlap need their own.
  * Asynchronous, one or two launches, on the current device.  NT_E_INVALID for a null pointer, a
  * negative size, ld < V, logits not aligned to their type or a misaligned workspace;
- * NT_E_UNSUPPORTED for k outside [0, min(32, V)] or 2^24 rows and more; NT_E_WORKSPACE if ws_bytes
- * is too small (the message states the bytes required).
+ * NT_E_UNSUPPORTED for k outside [0, min(32, V)], 2^24 rows and more or V past 2^30;
+ * NT_E_WORKSPACE if ws_bytes is too small (the message states the bytes required).
  * Defined by: log p(w) of Sec. 4.1's search, whose log_softmax Sec. 4.4 drops: one pass here. */
 nt_status nt_op_token_logp(int32_t dtype, const void* d_logits, int32_t ld, int32_t rows, int32_t V,
                            const int32_t* d_tokens, int32_t n_tok, int32_t k, float* d_logp, float* d_lse,
@@ -463,7 +463,7 @@ typedef struct {
  * the same page (sequences that share a page they both extend) leave either in it.
  * Asynchronous, on the current device.  NT_E_INVALID for a null pointer, a negative size, a
  * shape the struct does not allow, or rows that are not 16-byte aligned; NT_E_UNSUPPORTED for
- * fp8 with another dtype than NT_F16. */
+ * fp8 with another dtype than NT_F16 and for more than 2^30 rows or sequences. */
 nt_status nt_op_kv_append(const nt_kv_pages* cache, const void* d_k, const void* d_v, int32_t ld,
                           const int32_t* d_off, const int32_t* d_lens, int32_t n_seqs, int32_t n_rows, void* stream);
 

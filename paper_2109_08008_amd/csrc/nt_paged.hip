@@ -93,7 +93,7 @@ __global__ __launch_bounds__(256) void kv_append_kernel(KvAppendArgs a) {
       behind = b < a.n_seqs && a.off[b] <= row ? a.off[b + 1] - row : 0;   // 0: not a row of any sequence
     }
     if (lane < a.wave_rows && row < a.rows && behind > 0) {
-      const int pos = a.lens[b] - behind;
+      const int pos = max(a.lens[b], 0) - behind;
       if (pos >= 0 && (pos >> a.c.page_shift) < a.c.max_pages) {
         const int page = a.c.table[(size_t)b * a.c.max_pages + (pos >> a.c.page_shift)];
         if ((unsigned)page < (unsigned)a.c.n_pages)
@@ -632,7 +632,8 @@ void paged_attn_plan(PagedAttnArgs* a) {
   const int tasks = a->n_seqs * a->c.n_kv_heads * a->qblocks;
   const int tiles = (a->max_len + 127) / 128;
   const long long units = (long long)tiles * tasks;
-  const int per = (int)std::max({1ll, std::min(8ll, (units + 511) / 512), (units + 32767) / 32768});
+  const int per = (int)std::min<long long>(
+      std::max({1ll, std::min(8ll, (units + 511) / 512), (units + 32767) / 32768}), std::max(tiles, 1));
   a->chunk = per * 128;
   a->parts = std::max(1, (tiles + per - 1) / per);
   // one wave a task instead of four that share it

@@ -1327,12 +1327,21 @@ bool gated_fits(size_t eb, int lda, int N, int K) {
   return (2 * (size_t)N + 512) * K * eb < kLim32 && (size_t)lda * eb * 1024 < kLim32;
 }
 
+// Rows of one launch: the kernels' offsets into A are 32 bits, and a grid has less than 2^32 threads
+// (512 for 64 rows and 32 of the 2N columns, at the most).
+int gated_launch_rows(size_t eb, int lda, int N) {
+  const size_t by_offset = (kLim32 / (lda * eb) - 256) / 256 * 256;
+  const size_t by_grid = std::max<size_t>(256, (kLim32 / 512 / ((2 * (size_t)N + 31) / 32) * 64 - 64) / 256 * 256);
+  return (int)std::min<size_t>({by_offset, by_grid, (size_t)1 << 30});
+}
+
 // The cut of a nt_op_token_logp call and the bytes its parts take.
 nt_status token_logp_cut(int dtype, int rows, int V, int k, nt::TokenLogpArgs* a, size_t* bytes) {
   if (dtype < NT_F32 || dtype > NT_BF16) return fail(NT_E_INVALID, "unknown dtype %d", dtype);
   if (rows < 0 || V <= 0) return fail(NT_E_INVALID, "rows must be >= 0 and V > 0");
   if (k < 0 || k > 32 || k > V) return fail(NT_E_UNSUPPORTED, "k must be in [0, min(32, V)]");
   if (rows >= 1 << 24) return fail(NT_E_UNSUPPORTED, "at most 16777215 rows");
+  if (V > 1 << 30) return fail(NT_E_UNSUPPORTED, "V must be at most 1073741824");
   a->rows = rows;
   a->V = V;
   a->k = k;
@@ -1987,12 +1996,11 @@ nt_status nt_op_gemm_gated(int32_t dtype, const void* d_A, int32_t lda, const vo
   e.ldc = ldc;
   e.lnf_colsum = d_colsum;
   e.lnf_eps = ln_eps;
-  // the kernels' offsets into A are 32 bits: the rows of a launch stay below that
-  const int most = (int)std::min<size_t>(M, (kLim32 / (lda * eb) - 256) / 256 * 256);
-  for (int m = 0; m < M; m += most) {
+  const int most = gated_launch_rows(eb, lda, N);
+  for (long long m = 0; m < M; m += most) {
     e.out = static_cast<char*>(d_out) + (size_t)m * ldc * eb;
     NT_HIP(nt::gemm_gated(static_cast<DT>(dtype), static_cast<const char*>(d_A) + (size_t)m * lda * eb, lda, d_Bt,
-                          std::min(M - m, most), N, K, e, static_cast<hipStream_t>(stream)));
+                          (int)std::min<long long>(M - m, most), N, K, e, static_cast<hipStream_t>(stream)));
   }
   return NT_OK;
 }
@@ -2001,8 +2009,7 @@ int32_t nt_op_gemm_gated_rows(int32_t dtype, int32_t M, int32_t N, int32_t K, in
   if (dtype < NT_F32 || dtype > NT_BF16 || M < 0 || N <= 0 || K <= 0 || K % 64 != 0) return -1;
   const size_t eb = nt::dt_bytes(static_cast<DT>(dtype));
   if (!gated_fits(eb, K, N, K)) return -1;
-  const int most = (int)std::min<size_t>(M, (kLim32 / (K * eb) - 256) / 256 * 256);
-  return nt::gated_rows(static_cast<DT>(dtype), most, N, ln != 0);
+  return nt::gated_rows(static_cast<DT>(dtype), std::min(M, gated_launch_rows(eb, K, N)), N, ln != 0);
 }
 
 int32_t nt_op_gemm_rows(int32_t dtype, int32_t lda, int32_t M, int32_t N, int32_t K, int32_t ln, int32_t f8,
@@ -2138,6 +2145,7 @@ nt_status nt_op_kv_append(const nt_kv_pages* cache, const void* d_k, const void*
   NT_TRY(paged_cache(cache, true, &a.c));
   if (!d_k || !d_v || !d_lens) return fail(NT_E_INVALID, "null argument to nt_op_kv_append");
   if (n_seqs < 0 || n_rows < 0) return fail(NT_E_INVALID, "n_seqs and n_rows must be >= 0");
+  if (n_seqs > 1 << 30 || n_rows > 1 << 30) return fail(NT_E_UNSUPPORTED, "at most 1073741824 sequences and rows");
   if (!d_off && n_rows != n_seqs) return fail(NT_E_INVALID, "without d_off every sequence has one new row: n_rows == n_seqs");
   NT_TRY(check_rows("d_k", d_k, ld, a.c.n_kv_heads, a.c));
   NT_TRY(check_rows("d_v", d_v, ld, a.c.n_kv_heads, a.c));

@@ -44,11 +44,12 @@ constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 struct Stats {
   float m, s, t;
 };
-// (m, s, t) as seen from the maximum `to` >= m.  A part without a finite value (m = -inf) has
-// s = t = 0, or NaN where it held a NaN, and keeps them.
+// (m, s, t) as seen from another reference `to`.  A part without a finite value (m = -inf) has
+// s = t = 0, or NaN where it held a NaN, and keeps them.  (Bounded, so that what the type's lowest
+// value has summed up leaves with 0 and not with -inf * 0.)
 __device__ __forceinline__ Stats rescale(Stats a, float to) {
   if (a.m == -INFINITY) return {to, a.s, a.t};
-  const float d = a.m - to, f = __builtin_amdgcn_exp2f(d * LOG2E);
+  const float d = fmaxf(a.m - to, -1e30f), f = __builtin_amdgcn_exp2f(d * LOG2E);
   return {to, a.s * f, (a.t + a.s * d) * f};
 }
 // The wave's, seen from the largest `best`, which is at least each lane's a.m.
@@ -183,7 +184,7 @@ __device__ __forceinline__ float take_batch(const u32x4 (&q)[SCORE_BATCH], int c
         t[e & 1] = fmaf(p, d, t[e & 1]);
       }
     }
-    const float f = 1.0f - r * LN2;   // 2^-r
+    const float f = __builtin_amdgcn_exp2f(-r);
     const float sb = s[0] + s[1], tb = (t[0] + t[1] - r * sb) * (LN2 * f);
     careful = __ballot(tb != tb) != 0;
     if (!careful && !__ballot((best - ref) * LOG2E > 64.f)) {

@@ -27,6 +27,9 @@ def test_tiles(nt):   # noqa: F811
     rows = nt.nt_op_gemm_gated_rows
     assert rows("f16", 1, 64, 96) == rows("f16", -1, 64, 128) == rows("f16", 1, 0, 128) == -1
     assert rows("f16", 8, 1 << 24, 128) == -1
+    # as many rows a launch as its offsets and its grid take
+    assert rows("f16", 2 ** 31 - 1, 64, 64) == rows("f16", 1 << 24, 64, 64) == 256
+    assert rows("f32", 2 ** 31 - 1, 1 << 20, 64) == 64
     seen = {(dt, ln): {rows(dt, m, 1024, 512, ln) for m in (1, 100, 500, 1024, 2300, 5000, 16384)}
             for dt in ("f16", "bf16", "f32") for ln in (False, True)}
     for dt in ("f16", "bf16"):

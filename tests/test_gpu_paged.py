@@ -231,6 +231,18 @@ def test_attention_over_holes(dtype, fp8, lens):
     assert torch.equal(again, got) or lens[0] < max(lens)
 
 
+@pytest.mark.parametrize("n", [1, 700, 3000])
+def test_attention_over_nothing(n):
+    """No positions anywhere, max_len 0 and not: zeros."""
+    import torch
+    pages = Pages([0] * n, 1, 64, 16, "bf16", seed=1, extra_pages=300)
+    q = _q(n, 2, 64, "bf16", 1)
+    for max_len in (0, 16, 4800):
+        assert (attend(pages, q, 0.125, max_len=max_len) == 0).all()
+    pages.lens.fill_(-2 ** 31)
+    assert (attend(pages, q, 0.125, max_len=100) == 0).all()
+
+
 def test_attention_leaves_other_rows():
     """Rows behind the last sequence, and what lies between the rows, stay as they were."""
     import torch

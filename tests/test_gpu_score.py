@@ -47,7 +47,7 @@ def _expected(x, tokens, k):
         s = e.sum(1, keepdims=True)
         lse = (m + np.log(s))[:, 0]
         ent = np.where(s[:, 0] == 0, 0.0, np.log(s[:, 0]) - np.where(e > 0, e * d, 0.0).sum(1) / s[:, 0])
-        lp = np.where(x == -np.inf, -np.inf, x - np.where(lse == -np.inf, 0, lse)[:, None])
+        lp = np.where(x == -np.inf, -np.inf, d - np.log(s))     # (x - lse would lose log s beside 3e38)
     logp = np.zeros(tokens.shape)
     ok = (tokens >= 0) & (tokens < V)
     r, c = np.nonzero(ok)
@@ -96,6 +96,13 @@ def _logits(rows, V, kind, seed):
             x[1, V // 2] = -3.0
         if rows > 2:
             x[2, : V // 2] = -np.inf
+    elif kind == "offset":     # far from zero: x log2(e) is rounded by more than the probabilities may be
+        x = rng.standard_normal((rows, V)) * 3 + np.where(np.arange(rows) % 2, -1.0, 1.0)[:, None] * 50000.0
+    elif kind == "lowest":     # ruled out by the type's lowest value: the first half of the row at least
+        x = rng.standard_normal((rows, V)) * 3
+        x[:, : V // 2 + 1] = -np.inf       # (made finite by _case)
+        x[rng.random((rows, V)) < 0.3] = -np.inf
+        x[0] = -np.inf
     elif kind == "steps":      # one thread's values in 16 hold everything that is large, all different
         x = rng.standard_normal((rows, V)) - 20
         big = (np.arange(V) // 8) % 64 < 4
@@ -114,6 +121,8 @@ def _case(rows, V, kind, dtype, k, n_tok, seed, pad=0):
     import torch
     x = torch.full((rows, V + pad), float("nan"), dtype=torch_dtype(dtype))
     x[:, :V] = torch.from_numpy(_logits(rows, V, kind, seed)).to(x.dtype)
+    if kind == "lowest":
+        x[:, :V] = x[:, :V].clamp(min=torch.finfo(x.dtype).min)
     rng = np.random.default_rng(seed + 1)
     tokens = rng.integers(0, V, (rows, n_tok)).astype(np.int32)
     if n_tok > 1:
@@ -122,7 +131,7 @@ def _case(rows, V, kind, dtype, k, n_tok, seed, pad=0):
     return x.cuda()[:, :V], torch.from_numpy(tokens).cuda(), _expected(x64, tokens, k)
 
 
-KINDS = ["normal", "ties", "peaked", "masked", "steps", "sorted", "constant"]
+KINDS = ["normal", "ties", "peaked", "masked", "steps", "sorted", "constant", "lowest", "offset"]
 
 
 @pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])

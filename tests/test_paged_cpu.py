@@ -64,6 +64,11 @@ def test_append_refuses(nt, kw):
     assert _append(nt, _cache(nt), **kw) == nt.NT_E_INVALID
 
 
+def test_append_sizes_past_its_indices(nt):
+    for kw in (dict(n_rows=(1 << 30) + 1), dict(n_seqs=(1 << 30) + 1)):
+        assert _append(nt, _cache(nt), **kw) == nt.NT_E_UNSUPPORTED
+
+
 @pytest.mark.parametrize("kw,code", [
     (dict(d_q=None), 1), (dict(d_out=None), 1), (dict(d_lens=None), 1), (dict(n_seqs=-1), 1), (dict(max_len=-1), 1),
     (dict(n_heads=0), 1), (dict(n_heads=3), 1), (dict(n_heads=-2), 1), (dict(q_ld=255), 1), (dict(out_ld=248), 1),
@@ -92,6 +97,8 @@ def test_workspace_sizes(nt):
     for n in (1, 7, 5000):      # a part of a task holds two heads' sums; 32768 parts and one a task at most
         assert size(n, 1 << 24) <= (32768 + 2 * n) * 2 * 66 * 4 + 256
     assert size(1, 2 ** 31 - 1) == size(1, 1 << 24)     # the table's reach
+    wide = _cache(nt, max_pages=2 ** 31 - 1, page_len=256)
+    assert nt.nt_op_attn_paged_workspace(wide, 2, 1 << 21, 2 ** 31 - 1) == 0   # one part each
     assert nt.nt_op_attn_paged_workspace(_cache(nt), 4, 1, 1 << 24) == 0     # 64 positions
     for bad in ((3, 1, 10), (4, -1, 10), (4, 1, -1)):
         with pytest.raises(nt.NTError):

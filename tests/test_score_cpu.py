@@ -17,7 +17,7 @@ def _call(nt, **kw):   # noqa: F811
     (dict(dtype=3), 1), (dict(dtype=-1), 1), (dict(x=None), 1), (dict(tokens=None), 1), (dict(logp=None), 1),
     (dict(topi=None), 1), (dict(toplp=None), 1), (dict(rows=-1), 1), (dict(V=0), 1), (dict(V=-5), 1), (dict(ld=99), 1),
     (dict(n_tok=-1), 1), (dict(x=P + 2), 1), (dict(dtype=1, x=P + 1), 1), (dict(k=-1), 2), (dict(k=33), 2),
-    (dict(V=3, k=4), 2), (dict(rows=1 << 24), 2),
+    (dict(V=3, k=4), 2), (dict(rows=1 << 24), 2), (dict(rows=1, V=(1 << 30) + 1, ld=(1 << 30) + 1), 2),
     (dict(rows=1, V=100000, ld=100000), 3), (dict(rows=1, V=100000, ld=100000, ws=P, size=64), 3),
     (dict(rows=1, V=100000, ld=100000, ws=P + 16, size=1 << 20), 1),
     (dict(rows=0), 0), (dict(rows=0, n_tok=0, tokens=None, logp=None, k=0, topi=None, toplp=None, lse=None, ent=None), 0)])

@@ -185,11 +185,8 @@ constexpr int tile_keys() {
   return sizeof(T) == 4 ? (DH == 32 ? 32 : 16) : sizeof(KV) == 1 && DH <= 64 ? 64 : 32;
 }
 
-// (A wave a task, d_head 64: three waves a SIMD read the cache faster than four: 2160 x 16 heads of up
-// to 231 bf16 keys 160 us / 163.)
 template <typename T, int DH, typename KV, int SW, bool ONCE>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, SW == 1 && DH == 64 ? 3 : 8)))
-void paged_attn_kernel(PagedAttnArgs a) {
+__global__ __launch_bounds__(256) void paged_attn_kernel(PagedAttnArgs a) {
   constexpr int EB = sizeof(T), EC = sizeof(KV);
   constexpr bool F8 = EC == 1;
   constexpr int TK = tile_keys<T, DH, KV>();
@@ -309,145 +306,126 @@ void paged_attn_kernel(PagedAttnArgs a) {
   u32x4 kr[NP], vr[NP];
   const int step = SW * TK;
   int t = c0 + (SW == 1 ? 0 : wave * TK);
-  // A tile, its keys and values in kr and vr; with `more` the next one's (from key tn, pages pn) are
-  // loaded as soon as the registers are free.
-  auto tile = [&](auto more, int t, const Pages& pg, int tn, const Pages& pn) {
-#pragma unroll
-    for (int u = 0; u < NP; ++u) *reinterpret_cast<u32x4*>(ks + (row0 + u * RPL) * KSTR + col) = kr[u];
-    if (more) load(Kp, tn, pn, kr);
-    wave_fence();
-    floatx4 sc[NB];
-#pragma unroll
-    for (int j = 0; j < NB; ++j) {
-      const unsigned char* krow = ks + (16 * j + ln) * KSTR;
-      floatx4 acc = floatx4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int st = 0; st < QK; ++st) {
-        u32x4 kf;
-        if constexpr (!F8) {
-          kf = *reinterpret_cast<const u32x4*>(krow + st * 64 + grp * 16);
-        } else if constexpr (DH == 32) {
-          const uint2 w = *reinterpret_cast<const uint2*>(krow + grp * 8);
-          kf = f8_to_f16x8(w.x, w.y);
-        } else {
-          const uint2 w = *reinterpret_cast<const uint2*>(krow + st / 2 * 64 + grp * 16 + st % 2 * 8);
-          kf = f8_to_f16x8(w.x, w.y);
-        }
-        acc = Mfma<T>::step(kf, qf[st], acc);
-      }
-      sc[j] = acc;
-    }
-    // The tile's values to LDS.  What lies behind the length, or on no page, may be anything: no
-    // 0 * NaN from it
-    if (t + TK > len || any_hole(pg)) {
-#pragma unroll
-      for (int u = 0; u < NP; ++u) {
-        const int row = row0 + u * RPL;
-        int id = pg.id[0];
-#pragma unroll
-        for (int j = 1; j < NB; ++j) id = row >= 16 * j ? pg.id[j] : id;
-        if (t + row >= len || id < 0) vr[u] = u32x4{0, 0, 0, 0};
-      }
-    }
-#pragma unroll
-    for (int u = 0; u < NP; ++u) *reinterpret_cast<u32x4*>(vs + (row0 + u * RPL) * VSTR + col) = vr[u];
-    if (more) load(Vp, tn, pn, vr);
-    float cmax = -INFINITY;
-#pragma unroll
-    for (int j = 0; j < NB; ++j)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int key = t + 16 * j + 4 * grp + r;
-        sc[j][r] = key < len && pg.id[j] >= 0 ? sc[j][r] * a.scale_log2 : -INFINITY;
-        cmax = fmaxf(cmax, sc[j][r]);
-      }
-    cmax = fmaxf(cmax, __shfl_xor(cmax, 16, kWave));
-    cmax = fmaxf(cmax, __shfl_xor(cmax, 32, kWave));
-    const float mn = fmaxf(m, cmax);
-    const float ref = mn == -INFINITY ? 0.f : mn;   // nothing but masked keys so far
-    const float alpha = __builtin_amdgcn_exp2f(m - ref);
-    float ps = 0.f;
-#pragma unroll
-    for (int j = 0; j < NB; ++j)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        sc[j][r] = __builtin_amdgcn_exp2f(sc[j][r] - ref);
-        ps += sc[j][r];
-      }
-    lsum = lsum * alpha + ps;
-    m = mn;
-    if (__ballot(alpha != 1.f)) {
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const float ar = __shfl(alpha, 4 * grp + r, kWave);
-#pragma unroll
-        for (int c = 0; c < CB; ++c) o[c][r] *= ar;
-      }
-    }
-    wave_fence();
-#pragma unroll
-    for (int j = 0; j < NB; j += SB) {
-      if constexpr (EB == 2) {
-        T pe[8];
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) pe[4 * i + r] = from_f32<T>(sc[j + i][r]);
-        const u32x4 pf = __builtin_bit_cast(u32x4, pe);
-        // the lane's part of the columns' reads: rows 4 grp.. of both blocks
-        const unsigned char* vcol = F8 ? vs + (16 * (j + (ln >> 3)) + 4 * grp + (ln >> 1 & 3)) * VSTR + (ln & 1) * 8
-                                       : vs + (16 * j + 4 * grp + (ln >> 2)) * VSTR + (ln & 3) * 8;
-#pragma unroll
-        for (int c = 0; c < CB; ++c) {
-          if constexpr (F8) {
-            const uint2 w = lds_column8(vcol + c * 16);
-            o[c] = Mfma<T>::step(pf, f8_to_f16x8(w.x, w.y), o[c]);
-          } else {
-            const uint2 lo = lds_column4(vcol + c * 32), hi = lds_column4(vcol + 16 * VSTR + c * 32);
-            o[c] = Mfma<T>::step(pf, u32x4{lo.x, lo.y, hi.x, hi.y}, o[c]);
-          }
-        }
-      } else {
-        const u32x4 pf = __builtin_bit_cast(u32x4, sc[j]);
-        const unsigned char* vrow = vs + (16 * j + 4 * grp) * VSTR + ln * 4;
-#pragma unroll
-        for (int c = 0; c < CB; ++c) {
-          u32x4 vf;
-#pragma unroll
-          for (int r = 0; r < 4; ++r) vf[r] = *reinterpret_cast<const unsigned*>(vrow + r * VSTR + c * 64);
-          o[c] = Mfma<T>::step(pf, vf, o[c]);
-        }
-      }
-    }
-    wave_fence();
-  };
   if (t < c1) {
     Pages pg = pages_of(t);
     load(Kp, t, pg, kr);
     load(Vp, t, pg, vr);
-    // Of a loop in which only some turns load, the compiler waits for every load under way: the last
-    // tile is code of its own (us one copy / two: 8 x 8 heads of 16000 fp16 keys, d_head 64, 50.2 / 46.6;
-    // 33 x 3 of up to 72423, d_head 32, 90 / 86; 79 x 3 of up to 7691 E4M3 keys, d_head 64, 31.6 / 30.2;
-    // 40 x 8 of up to 6000 bf16, d_head 128, 20 query heads each, 123.7 / 121.8).  It does not pay for
-    // the longest rows, which leave enough under way (32 x 8 of up to 8000 fp32 keys, d_head 128,
-    // 207 / 211), nor for the few tiles that a wave takes alone (2160 x 16 of up to 231 bf16 keys 160 / 162).
-    if constexpr (SW == 1 || RB >= 512) {
-      for (;;) {
-        const bool more = t + step < c1;
-        Pages pn = pg;
-        if (more) pn = pages_of(t + step);
-        tile(more, t, pg, t + step, pn);
-        if (!more) break;
-        t += step;
-        pg = pn;
+    for (;;) {
+      const int tn = t + step;
+      const bool more = tn < c1;
+      Pages pn = pg;
+      if (more) pn = pages_of(tn);
+#pragma unroll
+      for (int u = 0; u < NP; ++u) *reinterpret_cast<u32x4*>(ks + (row0 + u * RPL) * KSTR + col) = kr[u];
+      if (more) load(Kp, tn, pn, kr);
+      wave_fence();
+      floatx4 sc[NB];
+#pragma unroll
+      for (int j = 0; j < NB; ++j) {
+        const unsigned char* krow = ks + (16 * j + ln) * KSTR;
+        floatx4 acc = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int st = 0; st < QK; ++st) {
+          u32x4 kf;
+          if constexpr (!F8) {
+            kf = *reinterpret_cast<const u32x4*>(krow + st * 64 + grp * 16);
+          } else if constexpr (DH == 32) {
+            const uint2 w = *reinterpret_cast<const uint2*>(krow + grp * 8);
+            kf = f8_to_f16x8(w.x, w.y);
+          } else {
+            const uint2 w = *reinterpret_cast<const uint2*>(krow + st / 2 * 64 + grp * 16 + st % 2 * 8);
+            kf = f8_to_f16x8(w.x, w.y);
+          }
+          acc = Mfma<T>::step(kf, qf[st], acc);
+        }
+        sc[j] = acc;
       }
-    } else {
-      for (; t + step < c1; t += step) {
-        const Pages pn = pages_of(t + step);
-        tile(std::true_type{}, t, pg, t + step, pn);
-        pg = pn;
+      // The tile's values to LDS.  What lies behind the length, or on no page, may be anything: no
+      // 0 * NaN from it
+      if (t + TK > len || any_hole(pg)) {
+#pragma unroll
+        for (int u = 0; u < NP; ++u) {
+          const int row = row0 + u * RPL;
+          int id = pg.id[0];
+#pragma unroll
+          for (int j = 1; j < NB; ++j) id = row >= 16 * j ? pg.id[j] : id;
+          if (t + row >= len || id < 0) vr[u] = u32x4{0, 0, 0, 0};
+        }
       }
-      tile(std::false_type{}, t, pg, t, pg);
+#pragma unroll
+      for (int u = 0; u < NP; ++u) *reinterpret_cast<u32x4*>(vs + (row0 + u * RPL) * VSTR + col) = vr[u];
+      if (more) load(Vp, tn, pn, vr);
+      float cmax = -INFINITY;
+#pragma unroll
+      for (int j = 0; j < NB; ++j)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int key = t + 16 * j + 4 * grp + r;
+          sc[j][r] = key < len && pg.id[j] >= 0 ? sc[j][r] * a.scale_log2 : -INFINITY;
+          cmax = fmaxf(cmax, sc[j][r]);
+        }
+      cmax = fmaxf(cmax, __shfl_xor(cmax, 16, kWave));
+      cmax = fmaxf(cmax, __shfl_xor(cmax, 32, kWave));
+      const float mn = fmaxf(m, cmax);
+      const float ref = mn == -INFINITY ? 0.f : mn;   // nothing but masked keys so far
+      const float alpha = __builtin_amdgcn_exp2f(m - ref);
+      float ps = 0.f;
+#pragma unroll
+      for (int j = 0; j < NB; ++j)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          sc[j][r] = __builtin_amdgcn_exp2f(sc[j][r] - ref);
+          ps += sc[j][r];
+        }
+      lsum = lsum * alpha + ps;
+      m = mn;
+      if (__ballot(alpha != 1.f)) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const float ar = __shfl(alpha, 4 * grp + r, kWave);
+#pragma unroll
+          for (int c = 0; c < CB; ++c) o[c][r] *= ar;
+        }
+      }
+      wave_fence();
+#pragma unroll
+      for (int j = 0; j < NB; j += SB) {
+        if constexpr (EB == 2) {
+          T pe[8];
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) pe[4 * i + r] = from_f32<T>(sc[j + i][r]);
+          const u32x4 pf = __builtin_bit_cast(u32x4, pe);
+          // the lane's part of the columns' reads: rows 4 grp.. of both blocks
+          const unsigned char* vcol = F8 ? vs + (16 * (j + (ln >> 3)) + 4 * grp + (ln >> 1 & 3)) * VSTR + (ln & 1) * 8
+                                         : vs + (16 * j + 4 * grp + (ln >> 2)) * VSTR + (ln & 3) * 8;
+#pragma unroll
+          for (int c = 0; c < CB; ++c) {
+            if constexpr (F8) {
+              const uint2 w = lds_column8(vcol + c * 16);
+              o[c] = Mfma<T>::step(pf, f8_to_f16x8(w.x, w.y), o[c]);
+            } else {
+              const uint2 lo = lds_column4(vcol + c * 32), hi = lds_column4(vcol + 16 * VSTR + c * 32);
+              o[c] = Mfma<T>::step(pf, u32x4{lo.x, lo.y, hi.x, hi.y}, o[c]);
+            }
+          }
+        } else {
+          const u32x4 pf = __builtin_bit_cast(u32x4, sc[j]);
+          const unsigned char* vrow = vs + (16 * j + 4 * grp) * VSTR + ln * 4;
+#pragma unroll
+          for (int c = 0; c < CB; ++c) {
+            u32x4 vf;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) vf[r] = *reinterpret_cast<const unsigned*>(vrow + r * VSTR + c * 64);
+            o[c] = Mfma<T>::step(pf, vf, o[c]);
+          }
+        }
+      }
+      wave_fence();
+      if (!more) break;
+      t = tn;
+      pg = pn;
     }
   }
   lsum += __shfl_xor(lsum, 16, kWave);

@@ -226,60 +226,72 @@ __global__ __launch_bounds__(SCORE_THREADS) void token_logp_kernel(TokenLogpArgs
   const int c0 = part * a.part_len, n = min(a.part_len, a.V - c0);
   const T* x = static_cast<const T*>(a.logits) + (size_t)row * a.ld + c0;
   const int tid = threadIdx.x, wave = tid / kWave, lane = tid % kWave;
-  // the given tokens' logits, under way with the row
-  float given = 0.f;
   int token = -1;
-  if (a.parts == 1 && tid < a.n_tok) {
-    token = a.tokens[(size_t)row * a.n_tok + tid];
-    if ((unsigned)token < (unsigned)a.V) given = to_f32(x[token]);
-  }
+  if (a.parts == 1 && a.n_tok > 0) token = a.tokens[(size_t)row * a.n_tok + min(tid, a.n_tok - 1)];
   if (a.k > 0) clear(cand);
   // `head` single values up to a 128-byte line (a load that straddles lines fetches both: 8192 rows
   // of 32001 bf16 values 98 us from 16-byte boundaries, of 32000 89), nv vectors and a tail; threads
   // 0 .. HEAD - 1 take the head's, the next ones the tail's
   constexpr int HEAD = 128 / (int)sizeof(T);
-  const int head = min(n, (int)((128 - (reinterpret_cast<uintptr_t>(x) & 127)) & 127) / (int)sizeof(T));
+  auto up = [](const T* p) { return (int)((128 - (reinterpret_cast<uintptr_t>(p) & 127)) & 127) / (int)sizeof(T); };
+  const int head = min(n, up(x));
   const int nv = (n - head) / VN, tail = head + nv * VN;
-  const u32x4* xv = reinterpret_cast<const u32x4*>(x + head);
+  // (no vector at all, in a short last part: the row's first)
+  const T* x0 = static_cast<const T*>(a.logits) + (size_t)row * a.ld;
+  const u32x4* xv = reinterpret_cast<const u32x4*>(nv > 0 ? x + head : x0 + up(x0));
   const int single = tid < HEAD ? (tid < head ? tid : -1) : tail + tid - HEAD < n ? tail + tid - HEAD : -1;
+  const T single_raw = x[max(single, 0)];
+  const int batches = (nv + NT * SCORE_BATCH - 1) / (NT * SCORE_BATCH);
+  // (Past the last vector: that one again.  Of loads that only some lanes or turns issue, the compiler
+  // would wait for every one under way; those of one address cost little.)
+  const int last = max(nv - 1, 0);
+  auto load = [&](u32x4 (&q)[SCORE_BATCH], int batch) {
+#pragma unroll
+    for (int u = 0; u < SCORE_BATCH; ++u)
+      q[u] = __builtin_nontemporal_load(xv + min(tid + (batch * SCORE_BATCH + u) * NT, last));
+  };
+  u32x4 q0[SCORE_BATCH], q1[SCORE_BATCH];
+  load(q0, 0);
   Stats acc{-INFINITY, 0.f, 0.f};
   float single_value = -INFINITY;
   if (single >= 0) {
-    const float c = to_f32(x[single]);
+    const float c = to_f32(single_raw);
     single_value = acc.m = fmaxf(c, -INFINITY);
     acc.s = c == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(c - c);   // 1; NaN of an infinity or a NaN
     acc.t = c == -INFINITY ? 0.f : c - c;
   }
-  const int batches = (nv + NT * SCORE_BATCH - 1) / (NT * SCORE_BATCH);
-  auto load = [&](u32x4 (&q)[SCORE_BATCH], int batch) {
-#pragma unroll
-    for (int u = 0; u < SCORE_BATCH; ++u) {
-      const int i = tid + (batch * SCORE_BATCH + u) * NT;
-      q[u] = i < nv ? __builtin_nontemporal_load(xv + i) : minus_infinity<T>();
-    }
-  };
   // the best batch's maximum, which one it is, and the best of all others
   float first = -INFINITY, second = -INFINITY;
   int first_batch = 0;
   bool careful = false;
   auto take = [&](u32x4 (&q)[SCORE_BATCH], int batch) {
-    const float best = (batch + 1) * SCORE_BATCH * NT <= nv
-                           ? take_batch<T, true>(q, SCORE_BATCH, acc, careful)
-                           : take_batch<T, false>(q, (nv - tid + NT - 1) / NT - batch * SCORE_BATCH, acc, careful);
+    float best;
+    if ((batch + 1) * SCORE_BATCH * NT <= nv) {
+      best = take_batch<T, true>(q, SCORE_BATCH, acc, careful);
+    } else {
+      const int count = (nv - tid + NT - 1) / NT - batch * SCORE_BATCH;
+#pragma unroll
+      for (int u = 0; u < SCORE_BATCH; ++u)
+        if (u >= count) q[u] = minus_infinity<T>();
+      best = take_batch<T, false>(q, count, acc, careful);
+    }
     second = fmaxf(second, fminf(first, best));
     first_batch = best > first ? batch : first_batch;
     first = fmaxf(first, best);
   };
-  u32x4 q0[SCORE_BATCH], q1[SCORE_BATCH];
-  load(q0, 0);
-  for (int b = 0; b < batches;) {
-    if (b + 1 < batches) load(q1, b + 1);
-    take(q0, b);
-    if (++b >= batches) break;
-    if (b + 1 < batches) load(q0, b + 1);
-    take(q1, b);
-    ++b;
+  if (batches > 0) {
+    for (int b = 0;;) {
+      load(q1, b + 1);
+      take(q0, b);
+      if (++b >= batches) break;
+      load(q0, b + 1);
+      take(q1, b);
+      if (++b >= batches) break;
+    }
   }
+  // the given tokens' logits, under way until the end
+  T given_raw{};
+  if (a.parts == 1 && a.n_tok > 0) given_raw = x[(unsigned)token < (unsigned)a.V ? token : 0];
   const float mine = fmaxf(first, single_value);   // acc.m is a reference near it
   {
     const Stats w = wave_stats(acc, mine);
@@ -310,6 +322,12 @@ __global__ __launch_bounds__(SCORE_THREADS) void token_logp_kernel(TokenLogpArgs
       if (a.lse) a.lse[row] = none ? -INFINITY : all.m + log_s;
       if (a.entropy) a.entropy[row] = none ? 0.f : log_s - all.t / all.s;
     }
+  } else if (tid == 0) {
+    *reinterpret_cast<float4*>(a.part_stats + ((size_t)row * a.parts + part) * 4) = make_float4(all.m, all.s, all.t, 0.f);
+  }
+  auto put_given = [&] {
+    if (a.parts > 1) return;   // (the join's)
+    float given = to_f32(given_raw);
     for (int j = tid; j < a.n_tok; j += NT) {
       if (j >= NT) {
         token = a.tokens[(size_t)row * a.n_tok + j];
@@ -318,10 +336,11 @@ __global__ __launch_bounds__(SCORE_THREADS) void token_logp_kernel(TokenLogpArgs
       const float lp = given == -INFINITY && all.s == all.s ? -INFINITY : (given - all.m) - log_s;
       a.logp[(size_t)row * a.n_tok + j] = (unsigned)token < (unsigned)a.V ? lp : 0.f;
     }
-  } else if (tid == 0) {
-    *reinterpret_cast<float4*>(a.part_stats + ((size_t)row * a.parts + part) * 4) = make_float4(all.m, all.s, all.t, 0.f);
+  };
+  if (a.k == 0) {
+    put_given();
+    return;
   }
-  if (a.k == 0) return;
 
   // The k-th largest group maximum: each wave counts the maxima above 16 groups' ones (lane l
   // group 16 wave + l % 16 against 16 others), the smallest with fewer than k above it is it.
@@ -349,7 +368,7 @@ __global__ __launch_bounds__(SCORE_THREADS) void token_logp_kernel(TokenLogpArgs
       if (v[e] >= thr && v[e] != -INFINITY) put(cand, v[e], head + VN * i + e);
   };
   if (single >= 0) {
-    const float c = to_f32(x[single]);
+    const float c = to_f32(single_raw);
     if (c >= thr && c != -INFINITY) put(cand, c, single);
   }
   // The wave's candidate threads, G at a time: a lane for each value of their best batches.  (Each
@@ -464,6 +483,7 @@ __global__ __launch_bounds__(SCORE_THREADS) void token_logp_kernel(TokenLogpArgs
       a.part_i[out + e] = INT_MAX;
     }
   }
+  put_given();
 }
 
 // Rows of up to SHORT values: a wave a row, its values in registers, and everything within the wave.

@@ -241,7 +241,6 @@ __global__ __launch_bounds__(SCORE_THREADS) void token_logp_kernel(TokenLogpArgs
   const u32x4* xv = reinterpret_cast<const u32x4*>(nv > 0 ? x + head : x0 + up(x0));
   const int single = tid < HEAD ? (tid < head ? tid : -1) : tail + tid - HEAD < n ? tail + tid - HEAD : -1;
   const T single_raw = x[max(single, 0)];
-  const int batches = (nv + NT * SCORE_BATCH - 1) / (NT * SCORE_BATCH);
   // (Past the last vector: that one again.  Of loads that only some lanes or turns issue, the compiler
   // would wait for every one under way; those of one address cost little.)
   const int last = max(nv - 1, 0);
@@ -264,30 +263,33 @@ __global__ __launch_bounds__(SCORE_THREADS) void token_logp_kernel(TokenLogpArgs
   float first = -INFINITY, second = -INFINITY;
   int first_batch = 0;
   bool careful = false;
-  auto take = [&](u32x4 (&q)[SCORE_BATCH], int batch) {
-    float best;
-    if ((batch + 1) * SCORE_BATCH * NT <= nv) {
-      best = take_batch<T, true>(q, SCORE_BATCH, acc, careful);
-    } else {
-      const int count = (nv - tid + NT - 1) / NT - batch * SCORE_BATCH;
-#pragma unroll
-      for (int u = 0; u < SCORE_BATCH; ++u)
-        if (u >= count) q[u] = minus_infinity<T>();
-      best = take_batch<T, false>(q, count, acc, careful);
-    }
+  auto note = [&](float best, int batch) {
     second = fmaxf(second, fminf(first, best));
     first_batch = best > first ? batch : first_batch;
     first = fmaxf(first, best);
   };
-  if (batches > 0) {
-    for (int b = 0;;) {
-      load(q1, b + 1);
-      take(q0, b);
-      if (++b >= batches) break;
-      load(q0, b + 1);
-      take(q1, b);
-      if (++b >= batches) break;
+  auto take = [&](u32x4 (&q)[SCORE_BATCH], int batch) { note(take_batch<T, true>(q, SCORE_BATCH, acc, careful), batch); };
+  auto take_rest = [&](u32x4 (&q)[SCORE_BATCH], int batch) {   // behind the whole batches
+    if (batch * SCORE_BATCH * NT >= nv) return;
+    const int count = (nv - tid + NT - 1) / NT - batch * SCORE_BATCH;
+#pragma unroll
+    for (int u = 0; u < SCORE_BATCH; ++u)
+      if (u >= count) q[u] = minus_infinity<T>();
+    note(take_batch<T, false>(q, count, acc, careful), batch);
+  };
+  for (int b = 0, whole = nv / (NT * SCORE_BATCH);;) {
+    if (b >= whole) {
+      take_rest(q0, b);
+      break;
     }
+    load(q1, b + 1);
+    take(q0, b++);
+    if (b >= whole) {
+      take_rest(q1, b);
+      break;
+    }
+    load(q0, b + 1);
+    take(q1, b++);
   }
   // the given tokens' logits, under way until the end
   T given_raw{};

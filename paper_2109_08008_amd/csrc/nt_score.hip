@@ -21,8 +21,8 @@
 // Few long rows are cut into parts over workgroups; a part leaves (m, s, t) and its k best, and
 // logp_join_kernel merges them.  Short rows are a wave's each (short_logp_kernel).
 //
-// Measured, us (GB/s): 4000 rows of 32000 fp32 values, k = 8, 86 (5960; k = 0 82); 8192 of 32001
-// bf16, k = 5, 100 (5240; k = 0 87); 1300 of 32000 fp32 36 (4600: every row is in flight at once, and
+// Measured, us (GB/s): 4000 rows of 32000 fp32 values, k = 8, 84 (6080; k = 0 82); 8192 of 32001
+// bf16, k = 5, 90 (5830; k = 0 84); 1300 of 32000 fp32 32.5 (5120: every row is in flight at once, and
 // nothing covers their ends); 8192 of 1000 bf16 14; 2 of 131072 fp32, k = 20, 12.7 in two launches.
 // Reads alone reach 6200 GB/s on this card, 7000 non-temporal.
 #include <limits.h>
@@ -233,17 +233,16 @@ __global__ __launch_bounds__(SCORE_THREADS) void token_logp_kernel(TokenLogpArgs
   // of 32001 bf16 values 98 us from 16-byte boundaries, of 32000 89), nv vectors and a tail; threads
   // 0 .. HEAD - 1 take the head's, the next ones the tail's
   constexpr int HEAD = 128 / (int)sizeof(T);
-  auto up = [](const T* p) { return (int)((128 - (reinterpret_cast<uintptr_t>(p) & 127)) & 127) / (int)sizeof(T); };
-  const int head = min(n, up(x));
+  const int head = (int)((128 - (reinterpret_cast<uintptr_t>(x) & 127)) & 127) / (int)sizeof(T);
   const int nv = (n - head) / VN, tail = head + nv * VN;
-  // (no vector at all, in a short last part: the row's first)
-  const T* x0 = static_cast<const T*>(a.logits) + (size_t)row * a.ld;
-  const u32x4* xv = reinterpret_cast<const u32x4*>(nv > 0 ? x + head : x0 + up(x0));
+  // (there are some: a row here has more than SHORT values, a part 8 KB, and the last one at most a
+  // value less for each other part)
+  const u32x4* xv = reinterpret_cast<const u32x4*>(x + head);
   const int single = tid < HEAD ? (tid < head ? tid : -1) : tail + tid - HEAD < n ? tail + tid - HEAD : -1;
   const T single_raw = x[max(single, 0)];
   // (Past the last vector: that one again.  Of loads that only some lanes or turns issue, the compiler
   // would wait for every one under way; those of one address cost little.)
-  const int last = max(nv - 1, 0);
+  const int last = nv - 1;
   auto load = [&](u32x4 (&q)[SCORE_BATCH], int batch) {
 #pragma unroll
     for (int u = 0; u < SCORE_BATCH; ++u)
@@ -626,7 +625,9 @@ __global__ __launch_bounds__(SCORE_THREADS) void logp_join_kernel(TokenLogpArgs 
   constexpr int NT = SCORE_THREADS;
   static_assert(SCORE_PARTS <= kWave && SCORE_PARTS % 4 == 0, "a part a lane");
   static_assert(SCORE_PARTS == 32 && SCORE_CAP >= 32 * 33 / 2, "what is left of the entries fits");
-  __shared__ __attribute__((aligned(16))) float hv[SCORE_PARTS];   // the parts' best
+  // the parts' best, second, fourth, .. 32nd best values (-inf: none)
+  __shared__ __attribute__((aligned(16))) float hv[6][SCORE_PARTS];
+  __shared__ float least[6];
   __shared__ Candidates cand;
   const int row = blockIdx.x, tid = threadIdx.x, lane = tid % kWave;
   const int n = a.parts * a.k;
@@ -644,7 +645,10 @@ __global__ __launch_bounds__(SCORE_THREADS) void logp_join_kernel(TokenLogpArgs 
     ei[u] = a.k > 8 * u ? a.part_i[e] : INT_MAX;
     if (!in) ei[u] = INT_MAX;
   }
-  if (a.k > 0 && tid < SCORE_PARTS) hv[tid] = tid < a.parts ? a.part_v[(size_t)row * n + tid * a.k] : -INFINITY;
+  // (levels but the first are of use where k (k + 1) / 2 entries are more than there are threads)
+  const int level = tid / SCORE_PARTS, of = tid % SCORE_PARTS, levels = a.k * (a.k + 1) / 2 > NT ? 6 : 1;
+  if (a.k > 0 && level < levels)
+    hv[level][of] = of < a.parts && 1 << level <= a.k ? a.part_v[(size_t)row * n + of * a.k + (1 << level) - 1] : -INFINITY;
   if (a.k > 0) clear(cand);
   Stats all{-INFINITY, 0.f, 0.f};
   if (lane < a.parts) {
@@ -669,9 +673,31 @@ __global__ __launch_bounds__(SCORE_THREADS) void logp_join_kernel(TokenLogpArgs 
   }
   if (a.k == 0) return;
   __syncthreads();
+  // Where r parts' l-th best reach a value, r l entries do: the ceil(k / l)-th largest of the l-th bests
+  // is no more than the k-th entry of all, for l = 1, 2, 4, ..  (64 rows of 50000, k = 32, in parts: 37 us
+  // without it, 21 with.)
+  float thr = -INFINITY;
+  if (levels > 1) {
+    if (level < levels) {
+      const float own_v = hv[level][of];
+      int above = 0;
+#pragma unroll
+      for (int j = 0; j < SCORE_PARTS; j += 4) {
+        const float4 v = *reinterpret_cast<const float4*>(&hv[level][j]);
+        above += (v.x > own_v) + (v.y > own_v) + (v.z > own_v) + (v.w > own_v);
+      }
+      float low = above << level < a.k ? -own_v : -INFINITY;   // (fewer than ceil(k / l) above it)
+#pragma unroll
+      for (int o = 1; o < SCORE_PARTS; o <<= 1) low = fmaxf(low, __shfl_xor(low, o, kWave));
+      if (of == 0) least[level] = -low;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int l = 0; l < 6; ++l) thr = fmaxf(thr, least[l]);
+  }
   // An entry behind `place` of its own part and behind the best of h other parts (of equal values the
-  // earlier part's) is behind place + h: what is left of all parts' entries where that is below k is a
-  // list of a few k.
+  // earlier part's) is behind place + h.  What reaches the threshold and is left of all parts' entries
+  // where that is below k is a list of little more than k, with many equal values of a few k.
 #pragma unroll
   for (int u = 0; u < 4; ++u) {
     if (8 * u >= a.k) break;
@@ -679,13 +705,13 @@ __global__ __launch_bounds__(SCORE_THREADS) void logp_join_kernel(TokenLogpArgs 
     int heads = 0;
 #pragma unroll
     for (int j = 0; j < SCORE_PARTS; j += 4) {
-      const float4 v = *reinterpret_cast<const float4*>(hv + j);
+      const float4 v = *reinterpret_cast<const float4*>(&hv[0][j]);
       heads += (j < own ? v.x >= ev[u] : v.x > ev[u]) + (j + 1 < own ? v.y >= ev[u] : v.y > ev[u]) +
                (j + 2 < own ? v.z >= ev[u] : v.z > ev[u]) + (j + 3 < own ? v.w >= ev[u] : v.w > ev[u]);
     }
     // (its own part's best, where that is above it, is one of the `place` already)
-    if (ev[u] < hv[own]) --heads;
-    if (ei[u] != INT_MAX && place + heads < a.k) put(cand, ev[u], ei[u]);
+    if (ev[u] < hv[0][own]) --heads;
+    if (ei[u] != INT_MAX && ev[u] >= thr && place + heads < a.k) put(cand, ev[u], ei[u]);
   }
   __syncthreads();
   const int found = cand.count;   // at most k + (k - 1) + .. + 1 of them
@@ -717,15 +743,20 @@ hipError_t logp_launch(const TokenLogpArgs& a, hipStream_t s) {
 
 }  // namespace
 
-// A row of fewer than 160 KB is one workgroup's: the join costs what the parts save (fp32, k = 8, us
-// whole / in parts of 8 KB: 1 row of 32000 9.4 / 9.3, 100 rows 13.3 / 12.6; k = 20, 2 rows of 131072
-// 22.4 / 12.4, 64 rows of 131072 bf16 values 27 / 19).  Longer ones are cut while that makes no more
-// than 1024 workgroups.
+// Whether a row is one workgroup's or cut into parts, which cost a second launch and a selection each: cut
+// where its time (as of 7 bytes a fp32 value and 5 a 16-bit one) is past a bound that grows
+// with the rows, which occupy the GPU too, and doubles with the largest k.  Measured, us whole / cut:
+// fp32, k = 8: 1 row of 32000 8.0 / 9.5, of 50000 9.9 / 9.6, of 100000 14.2 / 9.6; 64 of 50000
+// 11.4 / 12.2, of 70000 13.7 / 13.4, of 100000 17.1 / 14.2; 128 of 70000 16.0 / 16.0, of 100000
+// 20.0 / 18.3; 200 of 150000 26.7 / 28.7; bf16: 2 of 65000 10.4 / 10.1, 128 of 100000 15.0 / 16.2,
+// of 150000 18.8 / 18.0; k = 32: 2 of 50000 14.0 / 15.9, of 100000 18.6 / 16.5.
+// No more than 1024 workgroups come of it.
 void token_logp_plan(DT dt, TokenLogpArgs* a) {
-  const long long row_bytes = (long long)a->V * dt_bytes(dt);
+  const long long row_bytes = (long long)a->V * dt_bytes(dt), rows = a->rows;
+  const long long bound = (336 + 2 * rows + rows * rows / 128) << (a->k > 20 ? 11 : 10);
   long long parts = 1;
-  if (row_bytes >= 160 << 10 && a->rows > 0)
-    parts = std::max(1ll, std::min<long long>({1024 / a->rows, row_bytes / 8192, SCORE_PARTS}));
+  if (rows > 0 && row_bytes + 3ll * a->V >= bound)
+    parts = std::max(1ll, std::min<long long>({1024 / rows, row_bytes / 8192, SCORE_PARTS}));
   a->part_len = (int)((a->V + parts - 1) / parts);
   a->parts = (a->V + a->part_len - 1) / a->part_len;
 }

@@ -148,6 +148,17 @@ def test_against_float64(rows, V, k, n_tok, kind, dtype):
     _check(_run(x, tokens, k), want, V, (kind, dtype))
 
 
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("rows,V,k", [(3, 150003, 22), (3, 150007, 23), (2, 160031, 32), (70, 160001, 1)])
+def test_cut_rows(rows, V, k, kind, dtype):
+    """Rows in parts on both sides of the alternatives that a merge takes as they are."""
+    from paper_2109_08008_amd import nt
+    assert nt.nt_op_token_logp_workspace(dtype, rows, V, k) > 0
+    x, tokens, want = _case(rows, V, kind, dtype, k, 1, V + rows, pad=3)
+    _check(_run(x, tokens, k), want, V, (kind, dtype))
+
+
 def test_cut_and_uncut_agree_on_alternatives():
     """The same rows alone (cut into parts) and among many (not cut)."""
     import torch

@@ -631,6 +631,10 @@ __global__ __launch_bounds__(SCORE_THREADS) void logp_join_kernel(TokenLogpArgs 
   __shared__ Candidates cand;
   const int row = blockIdx.x, tid = threadIdx.x, lane = tid % kWave;
   const int n = a.parts * a.k;
+  const T* logits = static_cast<const T*>(a.logits) + (size_t)row * a.ld;
+  int token = -1;
+  T given{};
+  if (tid < a.n_tok) token = a.tokens[(size_t)row * a.n_tok + tid];
   // thread t takes places t % 8, t % 8 + 8, .. of part t / 8
   static_assert(NT == 8 * SCORE_PARTS, "eight threads a part");
   const int own = tid / 8;
@@ -650,6 +654,7 @@ __global__ __launch_bounds__(SCORE_THREADS) void logp_join_kernel(TokenLogpArgs 
   if (a.k > 0 && level < levels)
     hv[level][of] = of < a.parts && 1 << level <= a.k ? a.part_v[(size_t)row * n + of * a.k + (1 << level) - 1] : -INFINITY;
   if (a.k > 0) clear(cand);
+  if ((unsigned)token < (unsigned)a.V) given = logits[token];   // looked at at the end
   Stats all{-INFINITY, 0.f, 0.f};
   if (lane < a.parts) {
     const float4 q = *reinterpret_cast<const float4*>(a.part_stats + ((size_t)row * a.parts + lane) * 4);
@@ -662,16 +667,20 @@ __global__ __launch_bounds__(SCORE_THREADS) void logp_join_kernel(TokenLogpArgs 
     if (a.lse) a.lse[row] = none ? -INFINITY : all.m + log_s;
     if (a.entropy) a.entropy[row] = none ? 0.f : log_s - all.t / all.s;
   }
-  for (int j = tid; j < a.n_tok; j += NT) {
-    const int token = a.tokens[(size_t)row * a.n_tok + j];
-    float lp = 0.f;
-    if ((unsigned)token < (unsigned)a.V) {
-      const float x = to_f32(static_cast<const T*>(a.logits)[(size_t)row * a.ld + token]);
-      lp = x == -INFINITY && all.s == all.s ? -INFINITY : (x - all.m) - log_s;
+  auto put_given = [&] {
+    for (int j = tid; j < a.n_tok; j += NT) {
+      if (j >= NT) {
+        token = a.tokens[(size_t)row * a.n_tok + j];
+        if ((unsigned)token < (unsigned)a.V) given = logits[token];
+      }
+      const float x = to_f32(given), lp = x == -INFINITY && all.s == all.s ? -INFINITY : (x - all.m) - log_s;
+      a.logp[(size_t)row * a.n_tok + j] = (unsigned)token < (unsigned)a.V ? lp : 0.f;
     }
-    a.logp[(size_t)row * a.n_tok + j] = lp;
+  };
+  if (a.k == 0) {
+    put_given();
+    return;
   }
-  if (a.k == 0) return;
   __syncthreads();
   // Where r parts' l-th best reach a value, r l entries do: the ceil(k / l)-th largest of the l-th bests
   // is no more than the k-th entry of all, for l = 1, 2, 4, ..  (64 rows of 50000, k = 32, in parts: 37 us
@@ -726,6 +735,7 @@ __global__ __launch_bounds__(SCORE_THREADS) void logp_join_kernel(TokenLogpArgs 
     a.topi[(size_t)row * a.k + e] = INT_MAX;
     a.toplp[(size_t)row * a.k + e] = -INFINITY;
   }
+  put_given();
 }
 
 template <typename T>

@@ -377,32 +377,49 @@ __global__ __launch_bounds__(SCORE_THREADS) void token_logp_kernel(TokenLogpArgs
   // any: a third of what a row of 32000 16-bit values takes in all.)
   unsigned long long who = __ballot(first >= thr && first != -INFINITY);
   constexpr int PER = SCORE_BATCH * VN, G = kWave / PER;
-  while (who && *(volatile int*)&cand.count <= SCORE_CAP) {
-    int l = -1, batch = 0;
+  auto gather = [&](auto turns_c) {   // so many turns' values under way together
+    constexpr int U = decltype(turns_c)::value;
+    int at[U];
+    float c[U];
 #pragma unroll
-    for (int g = 0; g < G; ++g) {
-      const int next = who ? __builtin_ctzll(who) : -1;
-      who &= who - 1;   // (0 stays 0)
-      if (lane / PER == g) {
-        l = next;
-        batch = readlane_i(first_batch, max(next, 0));
+    for (int t = 0; t < U; ++t) {
+      int l = -1, batch = 0;
+#pragma unroll
+      for (int g = 0; g < G; ++g) {
+        const int next = who ? __builtin_ctzll(who) : -1;
+        who &= who - 1;   // (0 stays 0)
+        if (lane / PER == g) {
+          l = next;
+          batch = readlane_i(first_batch, max(next, 0));
+        }
       }
+      const int e = lane % PER, i = wave * kWave + l + (batch * SCORE_BATCH + e / VN) * NT;
+      at[t] = l >= 0 && i < nv ? head + VN * i + e % VN : -1;
+      c[t] = to_f32(x[max(at[t], 0)]);
     }
-    const int e = lane % PER, i = wave * kWave + l + (batch * SCORE_BATCH + e / VN) * NT;
-    const bool in = l >= 0 && i < nv;
-    const int at = in ? head + VN * i + e % VN : 0;
-    const float c = in ? to_f32(x[at]) : -INFINITY;
-    const bool hit = c >= thr && c != -INFINITY;
-    const unsigned long long hits = __ballot(hit);
-    if (!hits) continue;
-    int base = 0;
-    if (lane == 0) base = atomicAdd(&cand.count, __popcll(hits));
-    const int place = __builtin_amdgcn_readfirstlane(base) +
-                      __builtin_amdgcn_mbcnt_hi((unsigned)(hits >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)hits, 0));
-    if (hit && place < SCORE_CAP) {
-      cand.v[place] = c;
-      cand.i[place] = at;
+    unsigned long long hits[U];
+    int total = 0;
+#pragma unroll
+    for (int t = 0; t < U; ++t) {
+      hits[t] = __ballot(at[t] >= 0 && c[t] >= thr && c[t] != -INFINITY);
+      total += __popcll(hits[t]);
     }
+    int place = 0;
+    if (lane == 0) place = atomicAdd(&cand.count, total);
+    place = __builtin_amdgcn_readfirstlane(place);
+#pragma unroll
+    for (int t = 0; t < U; ++t) {
+      const int own = place + __builtin_amdgcn_mbcnt_hi((unsigned)(hits[t] >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)hits[t], 0));
+      if ((hits[t] >> lane & 1) && own < SCORE_CAP) {
+        cand.v[own] = c[t];
+        cand.i[own] = at[t];
+      }
+      place += __popcll(hits[t]);
+    }
+  };
+  while (who && *(volatile int*)&cand.count <= SCORE_CAP) {
+    if (__popcll(who) <= G) gather(std::integral_constant<int, 1>{});
+    else gather(std::integral_constant<int, 4>{});
   }
   // The few threads with a second batch that reaches it: the wave goes through their other vectors,
   // lane u reading u, u + 64, .. (Reading all of every candidate thread's again, a 128-byte line for

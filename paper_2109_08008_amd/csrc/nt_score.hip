@@ -11,7 +11,7 @@
 // the vector units: ten slots an element, four of them the exponential's.
 //
 // The alternatives are found as in the beam selection (nt_search.hip): the maxima of 64
-// quads of threads give a threshold that the row's k best reach, only the threads whose
+// groups of threads give a threshold that the row's k best reach, only the threads whose
 // maximum reaches it look at their values again, and each value found counts the ones
 // before it under (value desc, index asc).  A row with more than SCORE_CAP values at the
 // threshold (ties, above all 16-bit ones) raises it to the k-th best of some of those
@@ -72,8 +72,9 @@ struct Candidates {
   __attribute__((aligned(16))) int i[SCORE_CAP + 8];
   int count;
 };
-__device__ __forceinline__ void clear(Candidates& c) {   // by the workgroup; a barrier before the first put
-  for (int e = threadIdx.x; e < SCORE_CAP + 8; e += SCORE_THREADS) {
+template <int NT>
+__device__ __forceinline__ void clear(Candidates& c) {   // by NT threads; a barrier before the first put
+  for (int e = threadIdx.x; e < SCORE_CAP + 8; e += NT) {
     c.v[e] = -INFINITY;
     c.i[e] = INT_MAX;
   }
@@ -214,10 +215,10 @@ __device__ __forceinline__ float take_batch(const u32x4 (&q)[SCORE_BATCH], int c
   return best;
 }
 
-template <typename T>
-__global__ __launch_bounds__(SCORE_THREADS) void token_logp_kernel(TokenLogpArgs a) {
-  constexpr int NT = SCORE_THREADS, NW = NT / kWave, VN = Vec<T>::N;
-  static_assert(NT == 4 * 64, "groups are quads");
+template <typename T, int NT>
+__global__ __launch_bounds__(NT) void token_logp_kernel(TokenLogpArgs a) {
+  constexpr int NW = NT / kWave, VN = Vec<T>::N;
+  static_assert(NT == 4 * 64 || NT == 2 * 64, "64 groups, of four threads or two");
   __shared__ float sm[NW], ss[NW], st[NW], kth[NW];
   __shared__ float4 gmax[16];
   __shared__ Candidates cand;
@@ -228,7 +229,7 @@ __global__ __launch_bounds__(SCORE_THREADS) void token_logp_kernel(TokenLogpArgs
   const int tid = threadIdx.x, wave = tid / kWave, lane = tid % kWave;
   int token = -1;
   if (a.parts == 1 && a.n_tok > 0) token = a.tokens[(size_t)row * a.n_tok + min(tid, a.n_tok - 1)];
-  if (a.k > 0) clear(cand);
+  if (a.k > 0) clear<NT>(cand);
   // `head` single values up to a 128-byte line (a load that straddles lines fetches both: 8192 rows
   // of 32001 bf16 values 98 us from 16-byte boundaries, of 32000 89), nv vectors and a tail; threads
   // 0 .. HEAD - 1 take the head's, the next ones the tail's
@@ -304,12 +305,12 @@ __global__ __launch_bounds__(SCORE_THREADS) void token_logp_kernel(TokenLogpArgs
   }
   if (a.k > 0) {
     float g = fmaxf(mine, dpp_mov<DPP_XOR1>(mine));
-    g = fmaxf(g, dpp_mov<DPP_XOR2>(g));
-    if (tid % 4 == 0) reinterpret_cast<float*>(gmax)[tid / 4] = g;
+    if constexpr (NW == 4) g = fmaxf(g, dpp_mov<DPP_XOR2>(g));
+    if (tid % NW == 0) reinterpret_cast<float*>(gmax)[tid / NW] = g;
   }
   __syncthreads();
-  Stats all{fmaxf(fmaxf(sm[0], sm[1]), fmaxf(sm[2], sm[3])), 0.f, 0.f};
-  static_assert(NW == 4, "four waves");
+  Stats all{fmaxf(sm[0], sm[1]), 0.f, 0.f};
+  if constexpr (NW == 4) all.m = fmaxf(all.m, fmaxf(sm[2], sm[3]));
 #pragma unroll
   for (int w = 0; w < NW; ++w) {
     const Stats r = rescale(Stats{sm[w], ss[w], st[w]}, all.m);
@@ -343,24 +344,26 @@ __global__ __launch_bounds__(SCORE_THREADS) void token_logp_kernel(TokenLogpArgs
     return;
   }
 
-  // The k-th largest group maximum: each wave counts the maxima above 16 groups' ones (lane l
-  // group 16 wave + l % 16 against 16 others), the smallest with fewer than k above it is it.
+  // The k-th largest group maximum: each wave counts the maxima above GW groups' ones (lane l group
+  // GW wave + l % GW against GW others), the smallest with fewer than k above it is it.
   float thr;
   {
-    const float g = reinterpret_cast<const float*>(gmax)[16 * wave + lane % 16];
+    constexpr int GW = 64 / NW;
+    const float g = reinterpret_cast<const float*>(gmax)[GW * wave + lane % GW];
     float above = 0.f;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const float4 o = gmax[lane / 16 * 4 + j];
+    for (int j = 0; j < GW / 4; ++j) {
+      const float4 o = gmax[lane / GW * (GW / 4) + j];
       above += (o.x > g ? 1.f : 0.f) + (o.y > g ? 1.f : 0.f) + (o.z > g ? 1.f : 0.f) + (o.w > g ? 1.f : 0.f);
     }
-    above += __shfl_xor(above, 16, kWave);
+    if constexpr (NW == 4) above += __shfl_xor(above, 16, kWave);
     above += __shfl_xor(above, 32, kWave);
     const float low = -wave_max(above < (float)a.k ? -g : -INFINITY);
     if (lane == 0) kth[wave] = low;
   }
   __syncthreads();
-  thr = fminf(fminf(kth[0], kth[1]), fminf(kth[2], kth[3]));
+  thr = fminf(kth[0], kth[1]);
+  if constexpr (NW == 4) thr = fminf(thr, fminf(kth[2], kth[3]));
   auto take_values = [&](u32x4 q, int i) {
     float v[VN];
     widen<T>(q, v);
@@ -445,7 +448,7 @@ __global__ __launch_bounds__(SCORE_THREADS) void token_logp_kernel(TokenLogpArgs
       __syncthreads();
       thr = raised;
       __syncthreads();
-      clear(cand);
+      clear<NT>(cand);
       __syncthreads();
       for (int i0 = tid; i0 < n; i0 += 16 * NT) {
         T c[16];
@@ -670,7 +673,7 @@ __global__ __launch_bounds__(SCORE_THREADS) void logp_join_kernel(TokenLogpArgs 
   const int level = tid / SCORE_PARTS, of = tid % SCORE_PARTS, levels = a.k * (a.k + 1) / 2 > NT ? 6 : 1;
   if (a.k > 0 && level < levels)
     hv[level][of] = of < a.parts && 1 << level <= a.k ? a.part_v[(size_t)row * n + of * a.k + (1 << level) - 1] : -INFINITY;
-  if (a.k > 0) clear(cand);
+  if (a.k > 0) clear<NT>(cand);
   if ((unsigned)token < (unsigned)a.V) given = logits[token];   // looked at at the end
   Stats all{-INFINITY, 0.f, 0.f};
   if (lane < a.parts) {
@@ -755,13 +758,27 @@ __global__ __launch_bounds__(SCORE_THREADS) void logp_join_kernel(TokenLogpArgs 
   put_given();
 }
 
+// Many rows that are not long take two waves each instead of four: what a wave does besides its values
+// is a third to a half of its work.  us four / two waves, k = 8: 8192 rows of 2100 bf16 values 40 / 26,
+// of 8200 49 / 38, of 12000 57 / 47, of 20000 75 / 64 (k = 32: 94 / 95); of 4100 fp32 38 / 32, of 8200
+// 52 / 52 (k = 32: 71 / 78); 1000 of 4100 bf16 8.5 / 7.6, of 8200 9.6 / 9.8; 100 of 4100 6.1 / 6.4.
+template <typename T>
+bool two_waves(const TokenLogpArgs& a) {
+  const long long bytes = (long long)a.V * sizeof(T);
+  return a.parts == 1 && a.rows >= 512 && bytes <= (a.rows >= 4096 ? 24 << 10 : 9 << 10);
+}
+
 template <typename T>
 hipError_t logp_launch(const TokenLogpArgs& a, hipStream_t s) {
   if (a.V <= SHORT) {
     NT_LAUNCH((short_logp_kernel<T>), dim3((unsigned)((a.rows + 3) / 4)), dim3(256), 0, s, a);
     return hipGetLastError();
   }
-  NT_LAUNCH((token_logp_kernel<T>), dim3((unsigned)(a.rows * a.parts)), dim3(SCORE_THREADS), 0, s, a);
+  if (two_waves<T>(a)) {
+    NT_LAUNCH((token_logp_kernel<T, 128>), dim3((unsigned)a.rows), dim3(128), 0, s, a);
+    return hipGetLastError();
+  }
+  NT_LAUNCH((token_logp_kernel<T, SCORE_THREADS>), dim3((unsigned)(a.rows * a.parts)), dim3(SCORE_THREADS), 0, s, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.parts == 1) return e;
   NT_LAUNCH((logp_join_kernel<T>), dim3((unsigned)a.rows), dim3(SCORE_THREADS), 0, s, a);

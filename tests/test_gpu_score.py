@@ -159,6 +159,14 @@ def test_cut_rows(rows, V, k, kind, dtype):
     _check(_run(x, tokens, k), want, V, (kind, dtype))
 
 
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("rows,V,k", [(515, 2201, 20), (520, 2049, 32), (4100, 2153, 3)])
+def test_many_rows_of_a_few_thousand(rows, V, k, kind, dtype):
+    x, tokens, want = _case(rows, V, kind, dtype, k, 1, V + rows, pad=1)
+    _check(_run(x, tokens, k), want, V, (kind, dtype))
+
+
 def test_cut_and_uncut_agree_on_alternatives():
     """The same rows alone (cut into parts) and among many (not cut)."""
     import torch

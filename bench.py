@@ -50,7 +50,7 @@ GEMM_CLASSES = (0, 1, 2)
 # the counters were taken on (sha256 over `files`); otherwise the bench reports null.
 GEMM_FILES = ["paper_2109_08008_amd/csrc/" + f for f in
               ("nt_gemm.hip", "nt_gemm_common.h", "nt_gemm_phased.h", "nt_common.h")]
-GEMM_SHA256 = "ae988a98c7ef3c96267dcc98a2ea866293ec53072d7357bef9eba50719b39b16"
+GEMM_SHA256 = "1c4351c8005c0de1841cd837aee309b655ea11e455bba98228d38e7c8f7add41"
 TRAFFIC = {
     ("gemm_enc", "base-6-6"): {
         "files": GEMM_FILES, "sha256": GEMM_SHA256,

@@ -218,7 +218,7 @@ __device__ __forceinline__ float take_batch(const u32x4 (&q)[SCORE_BATCH], int c
 template <typename T, int NT>
 __global__ __launch_bounds__(NT) void token_logp_kernel(TokenLogpArgs a) {
   constexpr int NW = NT / kWave, VN = Vec<T>::N;
-  static_assert(NT == 4 * 64 || NT == 2 * 64, "64 groups, of four threads or two");
+  static_assert(NT == 2 * 64 || NT == 4 * 64 || NT == 16 * 64, "64 groups of NW threads");
   __shared__ float sm[NW], ss[NW], st[NW], kth[NW];
   __shared__ float4 gmax[16];
   __shared__ Candidates cand;
@@ -305,17 +305,25 @@ __global__ __launch_bounds__(NT) void token_logp_kernel(TokenLogpArgs a) {
   }
   if (a.k > 0) {
     float g = fmaxf(mine, dpp_mov<DPP_XOR1>(mine));
-    if constexpr (NW == 4) g = fmaxf(g, dpp_mov<DPP_XOR2>(g));
+    if constexpr (NW >= 4) g = fmaxf(g, dpp_mov<DPP_XOR2>(g));
+#pragma unroll
+    for (int o = 4; o < NW; o <<= 1) g = fmaxf(g, __shfl_xor(g, o, kWave));
     if (tid % NW == 0) reinterpret_cast<float*>(gmax)[tid / NW] = g;
   }
   __syncthreads();
-  Stats all{fmaxf(sm[0], sm[1]), 0.f, 0.f};
-  if constexpr (NW == 4) all.m = fmaxf(all.m, fmaxf(sm[2], sm[3]));
+  Stats all{-INFINITY, 0.f, 0.f};
+  if constexpr (NW > 4) {   // a wave of the workgroup's a lane
+    if (lane < NW) all = Stats{sm[lane], ss[lane], st[lane]};
+    all = wave_stats(all, all.m);
+  } else {
 #pragma unroll
-  for (int w = 0; w < NW; ++w) {
-    const Stats r = rescale(Stats{sm[w], ss[w], st[w]}, all.m);
-    all.s += r.s;
-    all.t += r.t;
+    for (int w = 0; w < NW; ++w) all.m = fmaxf(all.m, sm[w]);
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      const Stats r = rescale(Stats{sm[w], ss[w], st[w]}, all.m);
+      all.s += r.s;
+      all.t += r.t;
+    }
   }
   const float log_s = logf(all.s);
   if (a.parts == 1) {
@@ -356,14 +364,15 @@ __global__ __launch_bounds__(NT) void token_logp_kernel(TokenLogpArgs a) {
       const float4 o = gmax[lane / GW * (GW / 4) + j];
       above += (o.x > g ? 1.f : 0.f) + (o.y > g ? 1.f : 0.f) + (o.z > g ? 1.f : 0.f) + (o.w > g ? 1.f : 0.f);
     }
-    if constexpr (NW == 4) above += __shfl_xor(above, 16, kWave);
-    above += __shfl_xor(above, 32, kWave);
+#pragma unroll
+    for (int o = GW; o < kWave; o <<= 1) above += __shfl_xor(above, o, kWave);
     const float low = -wave_max(above < (float)a.k ? -g : -INFINITY);
     if (lane == 0) kth[wave] = low;
   }
   __syncthreads();
-  thr = fminf(kth[0], kth[1]);
-  if constexpr (NW == 4) thr = fminf(thr, fminf(kth[2], kth[3]));
+  thr = kth[0];
+#pragma unroll
+  for (int w = 1; w < NW; ++w) thr = fminf(thr, kth[w]);
   auto take_values = [&](u32x4 q, int i) {
     float v[VN];
     widen<T>(q, v);
@@ -768,6 +777,12 @@ bool two_waves(const TokenLogpArgs& a) {
   return a.parts == 1 && a.rows >= 512 && bytes <= (a.rows >= 4096 ? 24 << 10 : 9 << 10);
 }
 
+// No more rows than CUs take sixteen each: more of a row under way, and more threads to share out the
+// alternatives (us four / sixteen waves, fp32, k = 8: 1 row of 32000 8.0 / 7.7, 128 of 32000 10.0 / 9.2,
+// 64 of 70000 13.7 / 11.9; k = 32: 128 of 32000 12.8 / 11.6; but 64 of 4100 6.3 / 6.8, 400 of 32000
+// 14.0 / 17.7).
+bool sixteen_waves(const TokenLogpArgs& a) { return a.parts == 1 && a.rows <= 256 && a.V >= 12000; }
+
 template <typename T>
 hipError_t logp_launch(const TokenLogpArgs& a, hipStream_t s) {
   if (a.V <= SHORT) {
@@ -776,6 +791,10 @@ hipError_t logp_launch(const TokenLogpArgs& a, hipStream_t s) {
   }
   if (two_waves<T>(a)) {
     NT_LAUNCH((token_logp_kernel<T, 128>), dim3((unsigned)a.rows), dim3(128), 0, s, a);
+    return hipGetLastError();
+  }
+  if (sixteen_waves(a)) {
+    NT_LAUNCH((token_logp_kernel<T, 1024>), dim3((unsigned)a.rows), dim3(1024), 0, s, a);
     return hipGetLastError();
   }
   NT_LAUNCH((token_logp_kernel<T, SCORE_THREADS>), dim3((unsigned)(a.rows * a.parts)), dim3(SCORE_THREADS), 0, s, a);
@@ -790,14 +809,14 @@ hipError_t logp_launch(const TokenLogpArgs& a, hipStream_t s) {
 // Whether a row is one workgroup's or cut into parts, which cost a second launch and a selection each: cut
 // where its time (as of 7 bytes a fp32 value and 5 a 16-bit one) is past a bound that grows
 // with the rows, which occupy the GPU too, and doubles with the largest k.  Measured, us whole / cut:
-// fp32, k = 8: 1 row of 32000 8.0 / 9.5, of 50000 9.9 / 9.6, of 100000 14.2 / 9.6; 64 of 50000
-// 11.4 / 12.2, of 70000 13.7 / 13.4, of 100000 17.1 / 14.2; 128 of 70000 16.0 / 16.0, of 100000
-// 20.0 / 18.3; 200 of 150000 26.7 / 28.7; bf16: 2 of 65000 10.4 / 10.1, 128 of 100000 15.0 / 16.2,
-// of 150000 18.8 / 18.0; k = 32: 2 of 50000 14.0 / 15.9, of 100000 18.6 / 16.5.
+// fp32, k = 8: 1 row of 32000 7.7 / 9.5, of 70000 9.8 / 9.2, of 131072 12.6 / 9.3; 64 of 70000
+// 11.9 / 14.2, of 131072 16.9 / 15.2; 128 of 131072 19.5 / 20.4, of 300000 35.6 / 33.5; 256 of 300000
+// 53 / 57; bf16: 2 of 70000 9.9 / 9.6, 64 of 131072 13.8 / 13.5; k = 32, fp32: 1 of 131072 14.8 / 15.2,
+// 64 of 131072 19.0 / 24.2, of 300000 33.6 / 31.6.
 // No more than 1024 workgroups come of it.
 void token_logp_plan(DT dt, TokenLogpArgs* a) {
   const long long row_bytes = (long long)a->V * dt_bytes(dt), rows = a->rows;
-  const long long bound = (336 + 2 * rows + rows * rows / 128) << (a->k > 20 ? 11 : 10);
+  const long long bound = (444 + 5 * rows + rows * rows / 128) << (a->k > 20 ? 11 : 10);
   long long parts = 1;
   if (rows > 0 && row_bytes + 3ll * a->V >= bound)
     parts = std::max(1ll, std::min<long long>({1024 / rows, row_bytes / 8192, SCORE_PARTS}));

@@ -521,10 +521,14 @@ __global__ __launch_bounds__(NT) void token_logp_kernel(TokenLogpArgs a) {
 // of a wave-wide search for the next one.
 // (A workgroup a row has most of its threads idle and half its groups empty: 8192 rows of 1000 bf16
 // values, k = 5, took 38 us, with k = 32, where no threshold came of them, 566.)
-constexpr int SHORT = 2048, SHORT_CAP = 192;
-template <typename T>
+// From VEC_FROM values on, a lane reads 16 bytes at a time, at whatever alignment the row has (the last
+// ones end with the row and hold some of their neighbour's); shorter rows a value at a time, so that no
+// lane is without (1000 rows of 2001 bf16 values, k = 8, 8.1 us by single values, 6.7 by vectors; but
+// 8192 of 300, k = 32, 15 / 29: too few maxima for the threshold).
+constexpr int SHORT = 2048, SHORT_CAP = 192, VEC_FROM = 1024;
+template <typename T, bool VEC>
 __global__ __launch_bounds__(256) void short_logp_kernel(TokenLogpArgs a) {
-  constexpr int NJ = SHORT / kWave;
+  constexpr int VN = VEC ? Vec<T>::N : 1, NV = (VEC ? SHORT : VEC_FROM) / (kWave * VN);
   __shared__ __attribute__((aligned(16))) float cv[4][SHORT_CAP + 8];
   __shared__ __attribute__((aligned(16))) int ci[4][SHORT_CAP + 8];
   __shared__ __attribute__((aligned(16))) float best[4][kWave];
@@ -532,29 +536,47 @@ __global__ __launch_bounds__(256) void short_logp_kernel(TokenLogpArgs a) {
   const int row = blockIdx.x * 4 + wave;
   if (row >= a.rows) return;            // whole wave; no workgroup barrier below
   const T* x = static_cast<const T*>(a.logits) + (size_t)row * a.ld;
-  T raw[NJ];                            // (all under way together: nothing looks at one before)
+  auto first = [&](int j) { return min((j * kWave + lane) * VN, a.V - VN); };   // of vector j
+  struct Values { T t[VN]; };
+  Values raw[NV];                       // (all under way together: nothing looks at one before)
 #pragma unroll
-  for (int j = 0; j < NJ; ++j) raw[j] = x[min(j * kWave + lane, a.V - 1)];
+  for (int j = 0; j < NV; ++j) __builtin_memcpy(&raw[j], x + first(j), sizeof(Values));
   int token = -1;
   float given = 0.f;
   if (lane < a.n_tok) {
     token = a.tokens[(size_t)row * a.n_tok + lane];
     if ((unsigned)token < (unsigned)a.V) given = to_f32(x[token]);
   }
-  float v[NJ], mine = -INFINITY;
+  float v[NV * VN], mine = -INFINITY;
 #pragma unroll
-  for (int j = 0; j < NJ; ++j) {
-    v[j] = j * kWave + lane < a.V ? to_f32(raw[j]) : -INFINITY;
-    mine = fmaxf(mine, v[j]);
+  for (int j = 0; j < NV; ++j) {
+    if constexpr (VEC) {
+      float w[VN];
+      widen<T>(__builtin_bit_cast(u32x4, raw[j]), w);
+#pragma unroll
+      for (int e = 0; e < VN; ++e) v[j * VN + e] = w[e];
+    } else {
+      v[j] = to_f32(raw[j].t[0]);
+    }
+    if ((j + 1) * kWave * VN > a.V) {   // values of an earlier lane
+      const int skip = (j * kWave + lane) * VN - first(j);
+#pragma unroll
+      for (int e = 0; e < VN; ++e) v[j * VN + e] = e < skip ? -INFINITY : v[j * VN + e];
+    }
+#pragma unroll
+    for (int e = 0; e < VN; ++e) mine = fmaxf(mine, v[j * VN + e]);
   }
   const float m = wave_max(mine), ref = m == -INFINITY ? 0.f : m;
   float s = 0.f, t = 0.f;
 #pragma unroll
-  for (int j = 0; j < NJ; ++j) {
-    if (j * kWave >= a.V) break;
-    const float d = v[j] - ref, p = __builtin_amdgcn_exp2f(d * LOG2E);
-    s += p;
-    t = fmaf(p, fmaxf(d, -1e30f), t);   // 0, not NaN, of a logit of -inf
+  for (int j = 0; j < NV; ++j) {
+    if (j * kWave * VN >= a.V) break;
+#pragma unroll
+    for (int e = 0; e < VN; ++e) {
+      const float d = v[j * VN + e] - ref, p = __builtin_amdgcn_exp2f(d * LOG2E);
+      s += p;
+      t = fmaf(p, fmaxf(d, -1e30f), t);   // 0, not NaN, of a logit of -inf
+    }
   }
   s = wave_sum(s);
   t = wave_sum(t);
@@ -584,17 +606,20 @@ __global__ __launch_bounds__(256) void short_logp_kernel(TokenLogpArgs a) {
   const float thr = -wave_max(above < a.k ? -mine : -INFINITY);
   int found = 0;
 #pragma unroll
-  for (int j = 0; j < NJ; ++j) {
-    if (j * kWave >= a.V) break;
-    const bool hit = v[j] >= thr && v[j] != -INFINITY;
-    const unsigned long long hits = __ballot(hit);
-    if (!hits) continue;
-    const int place = found + __builtin_amdgcn_mbcnt_hi((unsigned)(hits >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)hits, 0));
-    if (hit && place < SHORT_CAP) {
-      cv[wave][place] = v[j];
-      ci[wave][place] = j * kWave + lane;
+  for (int j = 0; j < NV; ++j) {
+    if (j * kWave * VN >= a.V) break;
+#pragma unroll
+    for (int e = 0; e < VN; ++e) {
+      const float c = v[j * VN + e];
+      const unsigned long long hits = __ballot(c >= thr && c != -INFINITY);
+      if (!hits) continue;
+      const int place = found + __builtin_amdgcn_mbcnt_hi((unsigned)(hits >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)hits, 0));
+      if ((hits >> lane & 1) && place < SHORT_CAP) {
+        cv[wave][place] = c;
+        ci[wave][place] = first(j) + e;
+      }
+      found += __popcll(hits);
     }
-    found += __popcll(hits);
   }
   const size_t out = (size_t)row * a.k;
   if (found <= SHORT_CAP) {
@@ -617,8 +642,8 @@ __global__ __launch_bounds__(256) void short_logp_kernel(TokenLogpArgs a) {
       float bv = -INFINITY;
       int bi = INT_MAX;
 #pragma unroll
-      for (int j = NJ - 1; j >= 0; --j) {
-        const int i = j * kWave + lane;
+      for (int j = NV * VN - 1; j >= 0; --j) {
+        const int i = first(j / VN) + j % VN;
         if (before(pv, pi, v[j], i) && v[j] >= bv && v[j] != -INFINITY) {
           bv = v[j];
           bi = i;
@@ -786,7 +811,9 @@ bool sixteen_waves(const TokenLogpArgs& a) { return a.parts == 1 && a.rows <= 25
 template <typename T>
 hipError_t logp_launch(const TokenLogpArgs& a, hipStream_t s) {
   if (a.V <= SHORT) {
-    NT_LAUNCH((short_logp_kernel<T>), dim3((unsigned)((a.rows + 3) / 4)), dim3(256), 0, s, a);
+    const dim3 grid((unsigned)((a.rows + 3) / 4));
+    if (a.V >= VEC_FROM) NT_LAUNCH((short_logp_kernel<T, true>), grid, dim3(256), 0, s, a);
+    else NT_LAUNCH((short_logp_kernel<T, false>), grid, dim3(256), 0, s, a);
     return hipGetLastError();
   }
   if (two_waves<T>(a)) {

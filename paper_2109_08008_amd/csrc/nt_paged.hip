@@ -143,8 +143,12 @@ __global__ __launch_bounds__(256) void kv_append_kernel(KvAppendArgs a) {
 // lane.  Scores are transposed, S^T = K.Q^T, so that lane l holds head l % 16's scores of
 // four keys of each 16, which are the ones it supplies to P.V; the values are read key-major
 // (16-bit and E4M3: the transposing LDS reads).  The softmax's running maximum and sum are
-// fp32, in powers of two; P enters P.V in the model dtype (each p_j is off by at most half a
-// step, as the values themselves are).
+// fp32, in powers of two; P enters P.V in the model dtype, each p_j off by at most half a step.
+// For fp16 it is 2^14 times as large there (p_scale), as far up as e^{s - m} <= 1 goes: a step
+// keeps its relative size down to 2^-28 of the largest probability, and what is lost of one below
+// that is at most 2^-39 of it.  (As they are, probabilities below 2^-14 would lose bits and those
+// below 2^-25 would leave the product while the sum keeps them: one key 17.4 above 131000 equal
+// ones gave those no weight instead of 0.0036.)  The factor goes with the division by the sum.
 //
 // SW waves share a task (sequence, key head, block of 16 heads, part of the length): they
 // take its tiles in turn and join in LDS at the end.  A length is split into parts of
@@ -185,6 +189,12 @@ constexpr int tile_keys() {
   return sizeof(T) == 4 ? (DH == 32 ? 32 : 16) : sizeof(KV) == 1 && DH <= 64 ? 64 : 32;
 }
 
+// What the probabilities are multiplied by in the second product.
+template <typename T>
+constexpr float p_scale() {
+  return std::is_same<T, f16>::value ? 16384.f : 1.f;
+}
+
 template <typename T, int DH, typename KV, int SW, bool ONCE>
 __global__ __launch_bounds__(256) void paged_attn_kernel(PagedAttnArgs a) {
   constexpr int EB = sizeof(T), EC = sizeof(KV);
@@ -198,6 +208,7 @@ __global__ __launch_bounds__(256) void paged_attn_kernel(PagedAttnArgs a) {
   constexpr int ROWP = RB / 16;                       // 16-byte pieces of a key
   constexpr int NP = TK * ROWP / kWave;               // pieces a lane takes of a tile's keys
   constexpr int RPL = kWave / ROWP;                   // rows that one load of the wave covers
+  constexpr float PS = p_scale<T>();
   // LDS rows, padded against bank conflicts
   constexpr int KSTR = RB + 16, VSTR = RB + (EC == 2 ? 32 : 16), OSTR = DH * EB + 16;
   constexpr int KBYTES = TK * KSTR, WBYTES = KBYTES + TK * VSTR;
@@ -395,7 +406,7 @@ __global__ __launch_bounds__(256) void paged_attn_kernel(PagedAttnArgs a) {
 #pragma unroll
           for (int i = 0; i < 2; ++i)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) pe[4 * i + r] = from_f32<T>(sc[j + i][r]);
+            for (int r = 0; r < 4; ++r) pe[4 * i + r] = from_f32<T>(sc[j + i][r] * PS);
           const u32x4 pf = __builtin_bit_cast(u32x4, pe);
           // the lane's part of the columns' reads: rows 4 grp.. of both blocks
           const unsigned char* vcol = F8 ? vs + (16 * (j + (ln >> 3)) + 4 * grp + (ln >> 1 & 3)) * VSTR + (ln & 1) * 8
@@ -434,7 +445,7 @@ __global__ __launch_bounds__(256) void paged_attn_kernel(PagedAttnArgs a) {
   T* out = static_cast<T*>(a.out) + (size_t)b * a.out_ld + (size_t)h0 * DH;
   const size_t prow = ((size_t)part * a.n_seqs + b) * a.n_heads + h0;   // of the workspace
   if constexpr (SW == 1) {   // the rows through LDS, to leave in 16-byte pieces
-    const float inv = lsum == 0.f ? 0.f : 1.0f / lsum;
+    const float inv = lsum == 0.f ? 0.f : 1.0f / (lsum * PS);
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       const int i = 4 * grp + r;
@@ -478,7 +489,7 @@ __global__ __launch_bounds__(256) void paged_attn_kernel(PagedAttnArgs a) {
       for (int w = 0; w < SW; ++w) {
         const float f = __builtin_amdgcn_exp2f(jm[w][i] - ref);
         l += f * jl[w][i];
-        s += f * *reinterpret_cast<const floatx4*>(jo + w * JW + i * DH + x);
+        s += f * (1.0f / PS) * *reinterpret_cast<const floatx4*>(jo + w * JW + i * DH + x);
       }
       if (a.parts == 1) {
         const float inv = l == 0.f ? 0.f : 1.0f / l;

@@ -389,3 +389,40 @@ def test_undersized_workspace_is_reported():
         with pytest.raises(nt.NTError) as e:
             nt.nt_op_attn_paged(pages.cache, q.data_ptr(), 64, 1, pages.lens.data_ptr(), 1, 4000, 0.1, q.data_ptr(), 64, ptr, size)
         assert e.value.status == nt.NT_E_WORKSPACE and str(need) in e.value.message
+
+
+# ---- how exactly the probabilities enter the second product -------------------------------
+def _set(pool, index, value, fp8):
+    """pool[index] = value, in the cache's type."""
+    import torch
+    x = torch.as_tensor(value, dtype=torch.float32)
+    pool[index] = (x.to(torch.float8_e4m3fn).view(torch.uint8) if fp8 else x.to(pool.dtype)).to(pool.device)
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("d_head", [32, 64, 128])
+@pytest.mark.parametrize("n,length", [(1, 60000), (64, 8000), (2048, 250)])
+def test_attention_keeps_the_tail_of_a_dominant_key(fp8, d_head, n, length):
+    """One key far above thousands of equal ones, whose values alone are not zero: the output is the
+    others' weight.  A probability is off by at most half a step of fp16 (2^-11 of itself) down to
+    2^-28 of the largest and by half of fp16's least value below that, 2^-39 of the largest."""
+    import torch
+    pages = Pages([length] * n, 1, d_head, 64, "f16", fp8, seed=3)
+    q = torch.zeros(n, 1, d_head, dtype=torch.float16, device="cuda")
+    q[:, :, 0] = 1.0
+    for at in (0, length - 1):
+        first = pages.table[:, at // 64].long()
+        for gap in (9.0, 11.0, 18.0, 20.0, 24.0):      # exact in every type
+            _set(pages.k, slice(None), 0.0, fp8)
+            _set(pages.v, slice(None), 1.0, fp8)
+            _set(pages.k, (first, 0, at % 64, 0), gap, fp8)
+            _set(pages.v, (first, 0, at % 64), 0.0, fp8)
+            got = attend(pages, q, 1.0)
+            e = np.exp(-gap)
+            mass = (length - 1) * e / (1 + (length - 1) * e)
+            # (scores of one product are exact but for the scaling and the exponential's 2^-21; sums of
+            # `length` terms; the output's half step, or half of fp16's least value)
+            tol = mass * (2.0 ** -11 + 2.0 ** -11 + 4 * gap * 2.0 ** -24 + 2.0 ** -20 + length * 2.0 ** -24) + (
+                length * 2.0 ** -39 + 2.0 ** -25)
+            off = (got.double() - mass).abs().max().item()
+            assert off <= tol, (at, gap, mass, off, tol)

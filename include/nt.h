@@ -474,7 +474,7 @@ nt_status nt_op_kv_append(const nt_kv_pages* cache, const void* d_k, const void*
  * b * q_ld / b * out_ld, head h at h * d_head within.  d_lens: [n_seqs] device int32.
  * max_len: at least every length (host; what the work is divided by): positions past it are
  * not read.  Scores, softmax and sums are fp32; the probabilities enter the second product in
- * dtype.  Positions in holes are left out; a row with nothing to attend to (length 0 or less)
+ * two terms of dtype that hold 2^-19 (fp16) or 2^-16 (bf16) of each.  Positions in holes are left out; a row with nothing to attend to (length 0 or less)
  * is zero.  What lies in the pages behind a length is never part of a result, whatever it is.
  * d_ws: workspace of at least nt_op_attn_paged_workspace bytes (256-byte aligned; may be NULL
  * when that is 0), in use until the call's work is done: calls that may overlap need their

@@ -143,12 +143,14 @@ __global__ __launch_bounds__(256) void kv_append_kernel(KvAppendArgs a) {
 // lane.  Scores are transposed, S^T = K.Q^T, so that lane l holds head l % 16's scores of
 // four keys of each 16, which are the ones it supplies to P.V; the values are read key-major
 // (16-bit and E4M3: the transposing LDS reads).  The softmax's running maximum and sum are
-// fp32, in powers of two; P enters P.V in the model dtype, each p_j off by at most half a step.
-// For fp16 it is 2^14 times as large there (p_scale), as far up as e^{s - m} <= 1 goes: a step
-// keeps its relative size down to 2^-28 of the largest probability, and what is lost of one below
-// that is at most 2^-39 of it.  (As they are, probabilities below 2^-14 would lose bits and those
-// below 2^-25 would leave the product while the sum keeps them: one key 17.4 above 131000 equal
-// ones gave those no weight instead of 0.0036.)  The factor goes with the division by the sum.
+// fp32, in powers of two; with 16-bit values P enters P.V as two terms of that type (two_terms),
+// a matrix product each, so that the output's own rounding is what 16 bits cost.  (With P rounded
+// once the output was off by 1.2 times that, and where the values cancel by any factor of it.)
+// For fp16 P is 2^14 times as large there (p_scale), as far up as e^{s - m} <= 1 goes: what is lost
+// of a probability is at most 2^-39 of the largest one.  (As they are, probabilities below 2^-14
+// would lose bits and those below 2^-25 would leave the product while the sum keeps them: one key
+// 17.4 above 131000 equal ones gave those no weight instead of 0.0036.)  The factor goes with the
+// division by the sum.
 //
 // SW waves share a task (sequence, key head, block of 16 heads, part of the length): they
 // take its tiles in turn and join in LDS at the end.  A length is split into parts of
@@ -193,6 +195,32 @@ constexpr int tile_keys() {
 template <typename T>
 constexpr float p_scale() {
   return std::is_same<T, f16>::value ? 16384.f : 1.f;
+}
+
+// Eight probabilities, p_scale times as large, as hi + lo of the type.  hi is below each p by a few
+// of its last places and never equal to it, so that both terms are positive, as p is, and an
+// infinite value gives an infinite output, not inf - inf or 0 * inf (fp16: for p of 2^-28 and more).
+//  fp16: hi = p (1 - 2^-10) cut, lo = p - hi < 2^-9 p cut: 2^-19 p is lost, or 2^-24 (of p_scale);
+//  bf16: hi = the last fp32 value below p, cut, lo = p - hi <= 2^-7 p rounded: 2^-16 p.
+template <typename T>
+__device__ __forceinline__ void two_terms(const float (&p)[8], u32x4& hi, u32x4& lo) {
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    const float a = p[2 * w], b = p[2 * w + 1];
+    if constexpr (std::is_same<T, f16>::value) {
+      constexpr float S = p_scale<T>(), BELOW = S * (1.0f - 1.0f / 1024);
+      const auto h = __builtin_amdgcn_cvt_pkrtz(a * BELOW, b * BELOW);
+      const auto l = __builtin_amdgcn_cvt_pkrtz(fmaf(a, S, -(float)h[0]), fmaf(b, S, -(float)h[1]));
+      hi[w] = __builtin_bit_cast(unsigned, h);
+      lo[w] = __builtin_bit_cast(unsigned, l);
+    } else {
+      const unsigned x = __builtin_elementwise_sub_sat(__float_as_uint(a), 1u);   // (0 stays 0)
+      const unsigned y = __builtin_elementwise_sub_sat(__float_as_uint(b), 1u);
+      hi[w] = __builtin_amdgcn_perm(y, x, 0x07060302);
+      const T l[2] = {from_f32<T>(a - __uint_as_float(x & 0xffff0000u)), from_f32<T>(b - __uint_as_float(y & 0xffff0000u))};
+      lo[w] = __builtin_bit_cast(unsigned, l);
+    }
+  }
 }
 
 template <typename T, int DH, typename KV, int SW, bool ONCE>
@@ -402,12 +430,13 @@ __global__ __launch_bounds__(256) void paged_attn_kernel(PagedAttnArgs a) {
 #pragma unroll
       for (int j = 0; j < NB; j += SB) {
         if constexpr (EB == 2) {
-          T pe[8];
+          float p[8];
 #pragma unroll
           for (int i = 0; i < 2; ++i)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) pe[4 * i + r] = from_f32<T>(sc[j + i][r] * PS);
-          const u32x4 pf = __builtin_bit_cast(u32x4, pe);
+            for (int r = 0; r < 4; ++r) p[4 * i + r] = sc[j + i][r];
+          u32x4 hi, lo;
+          two_terms<T>(p, hi, lo);
           // the lane's part of the columns' reads: rows 4 grp.. of both blocks
           const unsigned char* vcol = F8 ? vs + (16 * (j + (ln >> 3)) + 4 * grp + (ln >> 1 & 3)) * VSTR + (ln & 1) * 8
                                          : vs + (16 * j + 4 * grp + (ln >> 2)) * VSTR + (ln & 3) * 8;
@@ -415,10 +444,14 @@ __global__ __launch_bounds__(256) void paged_attn_kernel(PagedAttnArgs a) {
           for (int c = 0; c < CB; ++c) {
             if constexpr (F8) {
               const uint2 w = lds_column8(vcol + c * 16);
-              o[c] = Mfma<T>::step(pf, f8_to_f16x8(w.x, w.y), o[c]);
+              const u32x4 vf = f8_to_f16x8(w.x, w.y);
+              o[c] = Mfma<T>::step(lo, vf, o[c]);
+              o[c] = Mfma<T>::step(hi, vf, o[c]);
             } else {
-              const uint2 lo = lds_column4(vcol + c * 32), hi = lds_column4(vcol + 16 * VSTR + c * 32);
-              o[c] = Mfma<T>::step(pf, u32x4{lo.x, lo.y, hi.x, hi.y}, o[c]);
+              const uint2 v0 = lds_column4(vcol + c * 32), v1 = lds_column4(vcol + 16 * VSTR + c * 32);
+              const u32x4 vf = u32x4{v0.x, v0.y, v1.x, v1.y};
+              o[c] = Mfma<T>::step(lo, vf, o[c]);
+              o[c] = Mfma<T>::step(hi, vf, o[c]);
             }
           }
         } else {

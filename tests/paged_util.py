@@ -126,3 +126,46 @@ def assert_within(got, want, bound, what=""):
     assert torch.isfinite(got).all(), what
     over = (got - want).abs() - bound
     assert float(over.max()) <= 0, (what, float(over.max()), float((got - want).abs().max()))
+
+
+def attention_of_many(pages, q, scale, p_rel, p_abs):
+    """attention() of many sequences at once, in float64 on the GPU, with the probabilities' part of the
+    bound as given: each is off by at most p_rel of itself and p_abs of the largest."""
+    import torch
+    n, heads, dh = q.shape
+    hkv, group, page = pages.kv_heads, heads // pages.kv_heads, pages.page
+    length = pages.max_pages * page
+    out = torch.empty(q.shape, dtype=torch.float64)
+    bound = torch.empty(q.shape, dtype=torch.float64)
+    u = EPS[pages.dtype] / 2
+    step = max(1, (1 << 25) // (hkv * length * dh))
+    lens = torch.tensor(pages.lens_list, device=q.device)
+    for b in range(0, n, step):
+        table = pages.table[b:b + step].long()
+        real = (table >= 0) & (table < pages.n_pages)
+        held = real.repeat_interleave(page, 1) & (torch.arange(length, device=q.device) < lens[b:b + step, None])
+
+        def cells(pool):   # [n, hkv, length, dh], 0 where nothing is held
+            x = pool[torch.where(real, table, torch.zeros_like(table))]
+            x = (x.view(torch.float8_e4m3fn).float() if pages.fp8 else x).double()
+            x = x.permute(0, 2, 1, 3, 4).reshape(-1, hkv, length, dh)
+            return torch.where(held[:, None, :, None], x, torch.zeros_like(x)).contiguous()
+
+        k, v = cells(pages.k), cells(pages.v)
+        qq = q[b:b + step].double().reshape(-1, hkv, group, dh).transpose(2, 3).contiguous()
+        s = torch.matmul(k, qq).transpose(2, 3).contiguous() * scale                      # [n, hkv, group, length]
+        size = torch.matmul(k.abs(), qq.abs()).amax(2)[..., None] * abs(scale)
+        s = s.masked_fill(~held[:, None, None], -float("inf"))
+        m = s.amax(3, keepdim=True)
+        e = torch.exp(s - torch.where(torch.isfinite(m), m, torch.zeros_like(m)))
+        z = e.sum(3, keepdim=True)
+        p = e / torch.where(z == 0, torch.ones_like(z), z)
+        o, a = torch.matmul(p, v), torch.matmul(p, v.abs())
+        ds = (dh + 2) * 2.0 ** -24 * size + 2.0 ** -21
+        keys = held.sum(1).double()[:, None, None, None]
+        err = u * o.abs() + p_rel * a + p_abs * keys * v.abs().amax(2)[:, :, None] + (2 * ds + keys * 2.0 ** -24 + 2.0 ** -20) * a
+        if pages.dtype == "f16":
+            err = err + 2.0 ** -25
+        out[b:b + step] = o.reshape(-1, heads, dh).cpu()
+        bound[b:b + step] = err.reshape(-1, heads, dh).cpu()
+    return out, bound

@@ -2,7 +2,7 @@
 import numpy as np
 import pytest
 
-from tests.paged_util import Pages, assert_within, attend, torch_dtype
+from tests.paged_util import Pages, assert_within, attend, attention_of_many, torch_dtype
 
 pytestmark = pytest.mark.gpu
 
@@ -426,3 +426,42 @@ def test_attention_keeps_the_tail_of_a_dominant_key(fp8, d_head, n, length):
                 length * 2.0 ** -39 + 2.0 ** -25)
             off = (got.double() - mass).abs().max().item()
             assert off <= tol, (at, gap, mass, off, tol)
+
+
+# What a probability may be off by in P.V, of itself and of the largest: two terms of 16 bits hold it to
+# 2^-19 (fp16; its least value being 2^-38 of the largest probability) and 2^-16 (bf16).
+P_REL = {"f16": 2.0 ** -19, "bf16": 2.0 ** -16, "f32": 0.0}
+P_ABS = {"f16": 2.0 ** -38, "bf16": 0.0, "f32": 0.0}
+
+
+@pytest.mark.parametrize("dtype,fp8", TYPES)
+@pytest.mark.parametrize("d_head", [32, 64, 128])
+@pytest.mark.parametrize("n,length", [(3, 21), (1, 3000), (2100, 200)])
+def test_attention_of_values_that_cancel(dtype, fp8, d_head, n, length):
+    """A third of the keys at a score above the others' by about log 2, values of opposite sign: the
+    output is what is left of sums a thousand times as large, so that a step of P would show."""
+    import torch
+    pages = Pages([length] * n, 1, d_head, 16, dtype, fp8, seed=5)
+    gaps = [0.625, 0.6875, 0.703125, 0.75, 1.0, 0.3125]
+    q = torch.zeros(n, len(gaps), d_head, dtype=torch_dtype(dtype), device="cuda")
+    q[:, :, 0] = torch.tensor(gaps, dtype=q.dtype)
+    third = (torch.arange(16 * pages.max_pages) % 3 == 0).float().view(pages.max_pages, 16)
+    value = torch.where(third[..., None] > 0, torch.ones(d_head), -(torch.arange(d_head) % 16 + 1) / 16.0)
+    for j in range(pages.max_pages):
+        at = pages.table[:, j].long()
+        _set(pages.k, (at, 0), 0.0, fp8)
+        _set(pages.k, (at, 0, slice(None), 0), third[j], fp8)
+        _set(pages.v, (at, 0), value[j], fp8)
+    got = attend(pages, q, 1.0)
+    assert_within(got, *attention_of_many(pages, q, 1.0, P_REL[dtype], P_ABS[dtype]))
+
+
+@pytest.mark.parametrize("dtype,fp8", TYPES)
+@pytest.mark.parametrize("d_head", [32, 64, 128])
+@pytest.mark.parametrize("lens", [EDGE, [3000, 1, 0, 769, 2049]])
+def test_attention_rounds_the_output_only(dtype, fp8, d_head, lens):
+    """Random keys and values: half a step of the output, and fp32's roundings."""
+    pages = Pages(lens, 2, d_head, 32, dtype, fp8, seed=d_head).fill(21)
+    q = _q(len(lens), 6, d_head, dtype, 22)
+    got = attend(pages, q, d_head ** -0.5)
+    assert_within(got, *attention_of_many(pages, q, d_head ** -0.5, P_REL[dtype], P_ABS[dtype]))

@@ -157,10 +157,11 @@ __device__ __forceinline__ float best_of(const u32x4 (&q)[SCORE_BATCH]) {
 // one turn over the values is enough; where a batch rises more than 2^64 above it, and in the first
 // batch, the reference moves first.
 // With c = ref log2(e) as rounded and r its rounding error, x log2(e) - c is one operation and
-// equals (x - ref) log2(e) + r: the sums are put right by r once a batch.  What that form cannot
-// take (-inf: 0 * -inf; NaN, and values past 2e38) shows as a NaN in t; the batch is then done by
-// differences, p max(x - ref, -1e30) (a logit of -inf adds nothing, a NaN stays one), and `careful`
-// sends the wave's next batches there at once.
+// equals (x - ref) log2(e) + r: the sums are put right by r once a batch.  That form cannot take an r
+// past 1 (|ref| past 1.1e7: t and r s cancel in ever more places, and near |ref| = 2e9, where r reaches
+// 128, 2^r or 2^-r leaves fp32's range) nor -inf (0 * -inf), NaN and values past 2e38, which show as a
+// NaN in t; the batch is then done by differences, p max(x - ref, -1e30) (a logit of -inf adds nothing, a
+// NaN stays one), and `careful` sends the wave's next batches there at once.
 template <typename T, bool WHOLE>
 __device__ __forceinline__ float take_batch(const u32x4 (&q)[SCORE_BATCH], int count, Stats& acc, bool& careful) {
   constexpr int VN = Vec<T>::N;
@@ -187,7 +188,7 @@ __device__ __forceinline__ float take_batch(const u32x4 (&q)[SCORE_BATCH], int c
     }
     const float f = __builtin_amdgcn_exp2f(-r);
     const float sb = s[0] + s[1], tb = (t[0] + t[1] - r * sb) * (LN2 * f);
-    careful = __ballot(tb != tb) != 0;
+    careful = __ballot(tb != tb || fabsf(r) > 1.f) != 0;
     if (!careful && !__ballot((best - ref) * LOG2E > 64.f)) {
       acc.s += sb * f;
       acc.t += tb;

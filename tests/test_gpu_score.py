@@ -288,3 +288,42 @@ def test_forced_decoding_is_scored():
         # two log-sum-exps of the same fp32 logits, each off by at most _check's bound
         np.testing.assert_allclose(logp[b], [s[b] for s in scored], rtol=2.0 ** -20, atol=2.0 ** -17)
     model.close()
+
+
+def _far_from_zero(V, seed):
+    """Rows whose largest values are far from zero: constant ones, among them those where the rounding
+    error of x log2(e) is near -127 and near 127, and rows of neighbouring fp32 values below and above
+    a base."""
+    rng = np.random.default_rng(seed)
+    base = [2041724160.0, 2727315712.0, -2041724160.0]
+    base += (2.0 ** rng.uniform(20, 36, 20)).tolist() + (-2.0 ** rng.uniform(20, 36, 6)).tolist() + [3e37, -3e38]
+    # the largest errors among some thousands of values
+    many = np.float32(2.0 ** rng.uniform(30, 33, 20000)).astype(np.float32)
+    r = many.astype(np.float64) * np.float64(np.float32(1.4426950408889634))
+    r = r - r.astype(np.float32)
+    base += many[np.argsort(r)[[0, 1, -2, -1]]].tolist() + many[np.argsort(np.abs(r - 64))[:2]].tolist()
+    base = np.asarray(base, dtype=np.float32)
+    x = np.repeat(base[:, None], V, 1)
+    spread = rng.integers(-6, 1, x.shape) * np.spacing(np.abs(x))
+    spread[:, rng.random(V) < 0.5] = 0.0
+    x = np.concatenate([x, (x + spread).astype(np.float32)])
+    x[1::5, rng.random(V) < 0.01] = -np.inf
+    return x
+
+
+@pytest.mark.parametrize("rows,V,k", [(74, 32000, 8), (74, 2000, 5), (4, 150016, 3), (700, 2304, 8), (4100, 2304, 0),
+                                      (300, 12032, 20), (74, 12032, 0)])
+def test_logits_far_from_zero(rows, V, k):
+    """fp32 rows past 2^20 in size: one wave, two, four and sixteen waves a row, and cut; rows that start
+    on 128-byte lines (every value in vectors)."""
+    import torch
+    x = _far_from_zero(V, V)
+    x = np.resize(x, (rows, V)) if rows >= len(x) else x[[0, 1, 37, 38]]
+    tokens = np.random.default_rng(1).integers(0, V, (rows, 2)).astype(np.int32)
+    want = _expected(x.astype(np.float64), tokens, k)
+    got = _run(torch.from_numpy(np.ascontiguousarray(x)).cuda(), torch.from_numpy(tokens).cuda(), k)
+    # the log-sum-exp is the maximum and a logarithm, rounded once; everything else is of differences
+    lse = got.pop("lse").cpu().numpy().astype(np.float64)
+    E = (V / 256 + 64) * 2.0 ** -24 + 2.0 ** -21
+    assert (np.abs(lse - want["lse"]) <= 2.0 ** -24 * np.abs(want["lse"]) + E + 2.0 ** -20).all()
+    _check(got | {"lse": torch.from_numpy(want["lse"])}, want, V)

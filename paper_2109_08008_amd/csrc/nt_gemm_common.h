@@ -61,12 +61,15 @@ __device__ __forceinline__ void frag_stats(const u32x4& a, T c, float& s, float&
   }
 }
 
-// The same for a gated projection: s and q sum the values and their squares as they are, by dot
-// products of two (exact products, fp32 sums).  That takes a quarter of the operations, which stand
-// between the matrix phases, but the variance q / K - mean^2 cancels where the mean is large: a row
-// with mean^2 > ROW_RATIO var is read again (row_stats).
+// The same for a 16-bit gated projection: s and q sum the values and their squares as they are, by
+// dot products of two (exact products, fp32 sums).  That takes a quarter of the operations, which
+// stand between the matrix phases, but the variance q / K - mean^2 cancels where the mean is large: a
+// row with mean^2 > ROW_RATIO var is read again (row_stats).  Six of the sums' 24 bits go at that
+// ratio, which puts 1/std off by up to 2^-16 (1024 values), a thirtieth of fp16's half step.  For fp32
+// rows, where it would show, the sums are frag_stats', and a row whose first value, the shift,
+// lies more than four deviations from its mean is read again.
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-constexpr float ROW_RATIO = 64.f;
+constexpr float ROW_RATIO = 64.f, SHIFT_RATIO = 16.f;
 template <typename T>
 __device__ __forceinline__ void frag_sums(const u32x4& a, float& s, float& q) {
 #pragma unroll
@@ -76,15 +79,12 @@ __device__ __forceinline__ void frag_sums(const u32x4& a, float& s, float& q) {
       const half2v x = __builtin_bit_cast(half2v, u);
       s = __builtin_amdgcn_fdot2(x, half2v{(_Float16)1.0f, (_Float16)1.0f}, s, false);
       q = __builtin_amdgcn_fdot2(x, x, q, false);
-    } else if constexpr (std::is_same<T, bf16>::value) {
+    } else {
+      static_assert(std::is_same<T, bf16>::value, "16-bit rows");
       const unsigned ones = 0x3f803f80u;
       const bf16x2 x = __builtin_bit_cast(bf16x2, u);
       s = __builtin_amdgcn_fdot2_f32_bf16(x, __builtin_bit_cast(bf16x2, ones), s, false);
       q = __builtin_amdgcn_fdot2_f32_bf16(x, x, q, false);
-    } else {
-      const float x = __uint_as_float(u);
-      s += x;
-      q = fmaf(x, x, q);
     }
   }
 }

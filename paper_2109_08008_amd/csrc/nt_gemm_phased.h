@@ -1382,9 +1382,11 @@ __global__ __launch_bounds__(256) void gemm_slim_kernel(const T* __restrict__ A,
   }
   __builtin_amdgcn_s_barrier();
   float ls = 0.f, lq = 0.f;
-  float ls1 = 0.f, lq1 = 0.f;   // GATED: the second halves of the k-steps by themselves
+  // 16-bit gated projections sum the values as they are (frag_sums), all others from a shift
+  constexpr bool SUMS = LNF && ROLE == GATED && sizeof(T) == 2;
+  float ls1 = 0.f, lq1 = 0.f;   // SUMS: the second halves of the k-steps by themselves
   T sh{};
-  if constexpr (LNF && ROLE != GATED) sh = first_value<T>(__shfl(a0[0].x, fr, kWave));
+  if constexpr (LNF && !SUMS) sh = first_value<T>(__shfl(a0[0].x, fr, kWave));
 
   unsigned s0 = 0, s1 = SLOT;   // slots of this k-step and the next
   auto kstep = [&](int kt, u32x4 (&a)[2], u32x4 (&b)[FN][2], u32x4 (&na)[2], u32x4 (&nb)[FN][2]) {
@@ -1392,7 +1394,7 @@ __global__ __launch_bounds__(256) void gemm_slim_kernel(const T* __restrict__ A,
     const unsigned qa = pa + s1, qb = pb + s1;
     SlimPhase<T, FN>::template step<0, VM>(acc, a, b, na, nb, qa, qa ^ 64, qb, qb ^ 64, xa, Ab + at, uniform(ma + s0), xb,
                                        Bb + at, uniform(mb + s0));
-    if constexpr (LNF && ROLE == GATED) {
+    if constexpr (SUMS) {
       frag_sums<T>(a[0], ls, lq);
       frag_sums<T>(a[1], ls1, lq1);
     } else if constexpr (LNF) {
@@ -1411,22 +1413,26 @@ __global__ __launch_bounds__(256) void gemm_slim_kernel(const T* __restrict__ A,
   mfma_drain(acc);
   if (ROLE != GATED && FN != 2 && ahead.on) epi_ahead<T, FN, ROLE, LNF>(ahead, epi, M, m0 + wave * 16, n0, fr, fc);
   float mu[1] = {0.f}, rs[1] = {1.f};
-  if constexpr (LNF && ROLE == GATED) {   // (the order of the larger tiles, whose waves take a half each)
+  // rows of the wave to be read again
+  auto read_again = [&](bool which, float2 r) {
+    for (unsigned long long again = __ballot(fc == 0 && which); again; again &= again - 1) {
+      const int row = __builtin_ctzll(again);
+      const float2 t =
+          row_stats<T>(A + (size_t)min(m0 + wave * 16 + row, M - 1) * lda, K, 1.0f / (float)K, epi.lnf_eps, lane);
+      if (fr == row) r = t;
+    }
+    mu[0] = r.x;
+    rs[0] = r.y;
+  };
+  if constexpr (SUMS) {   // (the order of the larger tiles, whose waves take a half each)
     float* x[4] = {&ls, &lq, &ls1, &lq1};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       *x[i] += __shfl_xor(*x[i], 16, kWave);
       *x[i] += __shfl_xor(*x[i], 32, kWave);
     }
-    const float inv_k = 1.0f / (float)K;
-    float2 r = sums_stats(ls + ls1, lq + lq1, inv_k, epi.lnf_eps);
-    for (unsigned long long again = __ballot(fc == 0 && r.y == -1.f); again; again &= again - 1) {
-      const int row = __builtin_ctzll(again);
-      const float2 t = row_stats<T>(A + (size_t)min(m0 + wave * 16 + row, M - 1) * lda, K, inv_k, epi.lnf_eps, lane);
-      if (fr == row) r = t;
-    }
-    mu[0] = r.x;
-    rs[0] = r.y;
+    const float2 r = sums_stats(ls + ls1, lq + lq1, 1.0f / (float)K, epi.lnf_eps);
+    read_again(r.y == -1.f, r);
   } else if constexpr (LNF) {   // every lane of a row ends with its sums
     const float inv_k = 1.0f / (float)K;
     ls += __shfl_xor(ls, 16, kWave);
@@ -1437,6 +1443,7 @@ __global__ __launch_bounds__(256) void gemm_slim_kernel(const T* __restrict__ A,
     const float var = fmaxf(lq * inv_k - ms * ms, 0.f);
     mu[0] = to_f32(sh) + ms;
     rs[0] = 1.0f / sqrtf(var + epi.lnf_eps);
+    if constexpr (ROLE == GATED) read_again(ms * ms > SHIFT_RATIO * var, make_float2(mu[0], rs[0]));
   }
   if constexpr (ROLE == GATED)
     gated_epilogue<T, 1, FN, LNF>(acc, epi, live, N, m0 + wave * 16, n0 / 2, fr, fc, mu, rs, ahead);

@@ -220,3 +220,35 @@ def test_captured_and_replayed(M):
         want = _run("bf16", a, w, b, cs, "silu")
         torch.cuda.synchronize()
         assert torch.equal(out, want)
+
+
+@pytest.mark.parametrize("M,N,K", [(70, 96, 192), (300, 250, 448), (1100, 640, 960), (130, 1000, 1088)])
+def test_fp32_layernorm_keeps_the_variance(M, N, K):
+    """fp32 rows whose mean is 5 to 8 deviations from zero, of whole numbers, so that every sum is exact, and
+    weights that pick one value each: what is left are the roundings of the mean and the variance.
+
+    With u = 2^-24 and z the first value's distance from the mean in deviations: the mean less the
+    first value is off by 2 u of itself, the mean square by 2 u, its square by 5 u: together
+    u (3 + 7 z^2) of the variance, half of that in 1/std, whose root and quotient add 2 u; the mean is
+    rounded by u mean + 2 u z std, the value less the mean once and the result twice."""
+    import torch
+    rng = np.random.default_rng(K)
+    a = np.clip(72 + 10 * np.round(rng.standard_normal((M, K))), 32, 112)
+    a[:, 0] = rng.choice([62.0, 72.0, 82.0], M)
+    a = torch.from_numpy(a).float().cuda()
+    pick = torch.from_numpy(rng.integers(0, K, N)).cuda()
+    w = torch.zeros(2 * N, K, device="cuda")
+    w[torch.arange(N, device="cuda"), pick] = 1.0
+    b = torch.zeros(2 * N, device="cuda")
+    b[N:] = 1.0
+    cs = torch.cat([torch.ones(N), torch.zeros(N)]).cuda()
+    got = _run("f32", a, w, b, cs, "relu").double()
+    x = a.double()
+    mu = x.mean(1, keepdim=True)
+    rs = 1 / torch.sqrt(((x - mu) ** 2).mean(1, keepdim=True) + 1e-5)
+    want = torch.relu((x[:, pick] - mu) * rs)
+    u, z2 = 2.0 ** -24, ((x[:, :1] - mu) * rs) ** 2
+    assert float(z2.max()) < 4 and float((mu * rs).min()) > 5
+    tol = u * (mu * rs + 2 * z2.sqrt()) + want * u * (1.5 + 3.5 * z2 + 2 + 3) + 2.0 ** -40
+    over = (got - want).abs() - tol * (1 + 2.0 ** -10)
+    assert float(over.max()) <= 0, (float(over.max() / u), float((got - want).abs().max() / u))

@@ -252,3 +252,36 @@ def test_fp32_layernorm_keeps_the_variance(M, N, K):
     tol = u * (mu * rs + 2 * z2.sqrt()) + want * u * (1.5 + 3.5 * z2 + 2 + 3) + 2.0 ** -40
     over = (got - want).abs() - tol * (1 + 2.0 ** -10)
     assert float(over.max()) <= 0, (float(over.max() / u), float((got - want).abs().max() / u))
+
+
+def _awkward(dtype, M, N, K, seed):
+    """Rows of every kind that the statistics tell apart, side by side: ordinary ones, a common offset of
+    13 deviations in every third, of 20 in whole blocks of 40, a far first value, constant ones."""
+    import torch
+    a, w, b, cs = _inputs(dtype, M, N, K, True, True, seed)
+    a = a.contiguous()
+    a[1::3] += 20.0
+    a[100:140] += 30.0
+    a[-45:-5] -= 30.0
+    a[4::7, 0] = 60.0
+    a[5] = 2.0
+    a[M // 2] = 0.0
+    return a, w, b, cs
+
+
+@pytest.mark.parametrize("dtype,M,N,K,rows", [
+    ("f32", 70, 96, 512, 32), ("f32", 1111, 2050, 320, 64),
+    ("f16", 150, 96, 512, 32), ("f16", 1203, 2050, 576, 64), ("f16", 2165, 4100, 320, 128),
+    ("bf16", 150, 96, 512, 32), ("bf16", 1203, 2050, 576, 64), ("bf16", 2165, 4100, 320, 128)])
+def test_layernorm_of_awkward_rows_on_every_tile(dtype, M, N, K, rows):
+    """Rows that are read a second time among ones that are not, on each tile that folds a LayerNorm in:
+    every element against float64, and the first rows with the bits of the smallest tile."""
+    import torch
+    from paper_2109_08008_amd import nt
+    assert nt.nt_op_gemm_gated_rows(dtype, M, N, K, True) == rows
+    a, w, b, cs = _awkward(dtype, M, N, K, M)
+    got = _run(dtype, a, w, b, cs, "gelu")
+    _check(dtype, got, a, w, b, cs, "gelu")
+    few = 20
+    assert nt.nt_op_gemm_gated_rows(dtype, few, N, K, True) in (32, 64)
+    assert torch.equal(got[:few], _run(dtype, a[:few], w, b, cs, "gelu"))

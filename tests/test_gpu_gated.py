@@ -285,3 +285,27 @@ def test_layernorm_of_awkward_rows_on_every_tile(dtype, M, N, K, rows):
     few = 20
     assert nt.nt_op_gemm_gated_rows(dtype, few, N, K, True) in (32, 64)
     assert torch.equal(got[:few], _run(dtype, a[:few], w, b, cs, "gelu"))
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("M,N,K", [(2000, 4095, 576), (2000, 4001, 64), (2000, 4096, 128), (4000, 2000, 448),
+                                   (3900, 2043, 192), (8000, 1021, 448)])
+def test_the_largest_tile(dtype, M, N, K):
+    """256x256 tiles with ragged rows and columns, one k-step, odd and even numbers of them: every
+    element against float64, nothing beside the columns or behind the rows changed, and the first and
+    last rows alone, on other tiles and at other places of one, with the same bits."""
+    import torch
+    from paper_2109_08008_amd import nt
+    assert nt.nt_op_gemm_gated_rows(dtype, M, N, K) == 256
+    act = ACTS[(M + N + K) % 4]
+    a, w, b, _ = _inputs(dtype, M, N, K, False, N % 3 > 0, K)
+    big = torch.full((M + 60, N + 3), 7.0, dtype=a.dtype, device="cuda")
+    got = _run(dtype, a, w, b, None, act, out=big)[:M, :N]
+    _check(dtype, got, a, w, b, None, act)
+    assert (big[M:] == 7).all() and (big[:, N:] == 7).all()
+    seen = set()
+    for m in (20, 300, M // 2):
+        seen.add(nt.nt_op_gemm_gated_rows(dtype, m, N, K))
+        assert torch.equal(got[:m], _run(dtype, a[:m], w, b, None, act)), m
+        assert torch.equal(got[-m:], _run(dtype, a[-m:], w, b, None, act)), m
+    assert {32, 128} <= seen and 256 not in seen

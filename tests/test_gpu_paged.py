@@ -465,3 +465,103 @@ def test_attention_rounds_the_output_only(dtype, fp8, d_head, lens):
     q = _q(len(lens), 6, d_head, dtype, 22)
     got = attend(pages, q, d_head ** -0.5)
     assert_within(got, *attention_of_many(pages, q, d_head ** -0.5, P_REL[dtype], P_ABS[dtype]))
+
+
+# ---- many short tasks, a wave each ------------------------------------------------------
+def _fill_all(pages, seed):
+    """Random cells at every held position, NaN everywhere else, all sequences at once."""
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    page = pages.page
+    table = pages.table.long()
+    counts = (torch.tensor(pages.lens_list, device="cuda")[:, None] - page * torch.arange(table.shape[1], device="cuda")).clamp(0, page)
+    real = (table >= 0) & (table < pages.n_pages)
+    held = torch.zeros(pages.n_pages, page, dtype=torch.bool, device="cuda")
+    held[table[real]] = torch.arange(page, device="cuda") < counts[real][:, None]
+    for pool in (pages.k, pages.v):
+        x = torch.randn(pool.shape, generator=g, device="cuda")
+        x = x.to(torch.float8_e4m3fn).view(torch.uint8) if pages.fp8 else x.to(pool.dtype)
+        pool.copy_(torch.where(held[:, None, :, None], x, pool))
+    return pages
+
+
+@pytest.mark.parametrize("dtype,fp8", TYPES)
+@pytest.mark.parametrize("d_head", [32, 64, 128])
+@pytest.mark.parametrize("n,kv_heads,group,page,longest", [(2049, 1, 1, 16, 256), (683, 3, 3, 128, 256), (1025, 1, 17, 32, 256),
+                                                           (347, 2, 33, 16, 129), (1030, 2, 1, 64, 40), (2203, 1, 4, 256, 17)])
+def test_attention_of_many_short_tasks(dtype, fp8, d_head, n, kv_heads, group, page, longest):
+    """2048 tasks (sequence, key head, block of 16 query heads) and more of up to 256 keys, which are a
+    wave's each: lengths on both sides of every tile and page edge, none and negative ones, holes, more
+    than one block of heads, a number of tasks that four does not divide; nothing between the rows or
+    behind the last one changes."""
+    import torch
+    from paper_2109_08008_amd import nt
+    tasks = n * kv_heads * ((group + 15) // 16)
+    assert tasks >= 2048 and (n != 2049 or tasks % 4)
+    rng = np.random.default_rng(n + d_head)
+    lens = rng.integers(0, longest + 1, n)
+    edge = [x for x in EDGE if x <= longest] + [longest]
+    lens[rng.permutation(n)[:4 * len(edge)]] = np.tile(edge, 4)
+    pages = _fill_all(Pages(lens.tolist(), kv_heads, d_head, page, dtype, fp8, seed=n), n)
+    table = pages.table_np.copy()
+    table[rng.random(table.shape) < 0.04] = rng.choice([-1, pages.n_pages, 2 ** 31 - 1, -2 ** 31])
+    pages.retable(table)
+    lens[7] = -3
+    pages.lens_list = lens.tolist()
+    pages.lens = torch.from_numpy(lens.astype(np.int32)).cuda()
+    heads = kv_heads * group
+    assert nt.nt_op_attn_paged_workspace(pages.cache, heads, n, longest) == 0
+    q = _q(n, heads, d_head, dtype, 2, pad=8)
+    wide = torch.full((n + 3, heads * d_head + 16), 7.0, dtype=q.dtype, device="cuda")
+    out = wide[:, :heads * d_head].unflatten(1, (heads, d_head))
+    attend(pages, q, d_head ** -0.5, max_len=longest, out=out)
+    want, bound = attention_of_many(pages, q, d_head ** -0.5, P_REL[dtype], P_ABS[dtype])
+    assert_within(out[:n], want, bound)
+    assert (out[:n][torch.from_numpy(lens <= 0)] == 0).all()
+    assert (wide[n:] == 7).all() and (wide[:, heads * d_head:] == 7).all()
+
+
+# ---- appends of many and of wide rows -----------------------------------------------------
+def _append_all(pages, x, off, lens):
+    """_append_expected for many rows at once."""
+    import torch
+    w, page = pages.kv_heads * pages.d_head, pages.page
+    off, lens = np.asarray(off), np.asarray(lens)
+    seq = np.repeat(np.arange(len(lens)), np.diff(off))
+    row = np.arange(off[0], off[-1])
+    pos = lens[seq] - (off[seq + 1] - row)
+    assert (pos >= 0).all() and (pos < pages.max_pages * page).all()
+    at = torch.from_numpy(pages.table_np[seq, pos // page].astype(np.int64))
+    slot = torch.from_numpy(pos % page)
+    out = []
+    for part, pool in ((1, pages.k), (2, pages.v)):
+        new = x.cpu()[off[0]:off[-1], part * w:(part + 1) * w].reshape(-1, pages.kv_heads, pages.d_head)
+        if pages.fp8:
+            new = new.float().clamp(-448, 448).to(torch.float8_e4m3fn).view(torch.uint8)
+        p = pool.cpu().clone()
+        p[at, :, slot] = new
+        out.append(p)
+    return out
+
+
+@pytest.mark.parametrize("dtype,fp8", TYPES)
+@pytest.mark.parametrize("kv_heads,d_head,n,longest", [
+    (1, 32, 1500, 401),       # 300 thousand narrow rows: several a wave in several turns
+    (1, 64, 900, 301),        # the same of twice the width
+    (5, 64, 300, 201),        # rows that no power of two of lanes covers, several turns a wave
+    (16, 64, 400, 151),       # two turns a row, several rows a wave
+    (17, 128, 90, 231),       # ends of rows inside a turn
+    (40, 128, 12, 61)])       # rows past 8 KB: more turns than are under way at once
+def test_append_of_many_and_wide_rows(dtype, fp8, kv_heads, d_head, n, longest):
+    import torch
+    rng = np.random.default_rng(n)
+    new = rng.integers(0, longest, n)
+    new[[0, 1, n - 1]] = [3, 0, longest]
+    lens = new + rng.integers(0, 20, n)
+    off = 1 + np.concatenate([[0], np.cumsum(new)])
+    pages = Pages(lens.tolist(), kv_heads, d_head, 32, dtype, fp8, seed=n)
+    g = torch.Generator(device="cuda").manual_seed(n)
+    x = torch.randn(int(off[-1]) + 2, 3 * kv_heads * d_head, generator=g, device="cuda").to(torch_dtype(dtype))
+    want = _append_all(pages, x, off, lens)
+    _append(pages, x, off.tolist(), len(x))
+    assert _same(pages.k, want[0]) and _same(pages.v, want[1])

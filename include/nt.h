@@ -459,8 +459,10 @@ typedef struct {
  * sequence b's rows go to its last positions, the last row to d_lens[b] - 1.  n_rows: rows of
  * d_k and d_v (rows of no sequence, positions below 0 or past max_pages pages, and holes are
  * left out; nothing else of the pools changes).  An fp8 cache takes the E4M3 value nearest to
- * each element (ties to even, saturating at 448).  Two rows of one call for the same slot of
- * the same page (sequences that share a page they both extend) leave either in it.
+ * each element (ties to even, saturating at 448).  Where two rows of one call go to the same
+ * slot of the same page (sequences that share a page they both extend), the slot's contents are
+ * unspecified unless the rows are equal: its key may come from one row and its value, or a part
+ * of either, from the other.  Copy a shared page before its sequences extend it differently.
  * Asynchronous, on the current device.  NT_E_INVALID for a null pointer, a negative size, a
  * shape the struct does not allow, or rows that are not 16-byte aligned; NT_E_UNSUPPORTED for
  * fp8 with another dtype than NT_F16 and for more than 2^30 rows or sequences. */

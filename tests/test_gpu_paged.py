@@ -565,3 +565,19 @@ def test_append_of_many_and_wide_rows(dtype, fp8, kv_heads, d_head, n, longest):
     want = _append_all(pages, x, off, lens)
     _append(pages, x, off.tolist(), len(x))
     assert _same(pages.k, want[0]) and _same(pages.v, want[1])
+
+
+@pytest.mark.parametrize("dtype,fp8", TYPES)
+def test_append_of_equal_rows_to_a_shared_page(dtype, fp8):
+    """Sequences that extend a page they share by the same token: that token's row."""
+    import torch
+    n, hkv, dh = 70, 3, 64
+    pages = Pages([21] * n, hkv, dh, 16, dtype, fp8, seed=2)
+    table = pages.table_np.copy()
+    table[:, 1] = table[0, 1]
+    pages.retable(table)
+    x = torch.randn(1, 3 * hkv * dh, generator=torch.Generator().manual_seed(3)).to(torch_dtype(dtype)).cuda().repeat(n, 1)
+    w = hkv * dh
+    want = _append_expected(pages, x[:, w:2 * w].contiguous(), x[:, 2 * w:].contiguous(), None, pages.lens_list, n)
+    _append(pages, x, None, n)
+    assert _same(pages.k, want[0]) and _same(pages.v, want[1])

@@ -671,8 +671,10 @@ constexpr int GATED = 4;   // the kernels' ROLE
 __device__ __forceinline__ int gated_base(int row, int N) { return (row >> 4 & 1) * N; }         // of a tile's row
 __device__ __forceinline__ int gated_column(int row) { return (row >> 5 << 4) + (row & 15); }    //   and its output column
 
-// act(g) by EpiMode.  16-bit outputs take the hardware's exponential and reciprocal (each within an
-// ulp or two of fp32) and an error function to match, fp32 ones the library's functions.
+// act(g) by EpiMode.  16-bit outputs take the hardware's exponential and reciprocal and an error
+// function of its own, fp32 ones the library's functions.  The exponential's argument x is rounded,
+// which puts it off by up to |x| 2^-24: act(g) is within 2^-18 for g > -5 and within 2^-15 below, as far
+// as it is a normal number, a sixteenth of fp16's half step and less of bf16's.
 template <typename T, int MODE>
 __device__ __forceinline__ float gate_act(float g) {
   constexpr bool FAST = sizeof(T) == 2;
@@ -684,7 +686,7 @@ __device__ __forceinline__ float gate_act(float g) {
   else if constexpr (MODE == EPI_GATE_GELU && FAST) {
     // half of erfc(x) e^{x^2}, x = |g| / sqrt 2, as a polynomial in t = 1 / (1 + 0.375 x) without a
     // constant term: least squares reweighted to the smallest largest relative error over x in [0, 10],
-    // 6.4e-7 (with erff() 16384x2048x512 bf16 took 105 us, so 89)
+    // the polynomial's own being 6.4e-7 (with erff() 16384x2048x512 bf16 took 105 us, so 89)
     const float t = __builtin_amdgcn_rcpf(fmaf(fabsf(g), 0.375f * 0.70710678118654752f, 1.0f));
     float h = -0.06754793f;
     h = fmaf(h, t, 0.19396885f);

@@ -184,8 +184,7 @@ __device__ __forceinline__ uint2 lds_column8(const unsigned char* p) {
 
 // Keys of a tile: those of a P.V step, and twice that for the short rows of E4M3 keys, so that they
 // too have bytes enough under way (us with 32 / 64 keys: E4M3, d_head 64, 79 x 3 heads of 76..7691
-// keys 34.2 / 33.2; but d_head 128, 2184 x 16 of 9 keys 43 / 65, fp16, d_head 32, 33 x 3 of 72423
-// 208 / 220).
+// keys 32.7 / 32.5; but d_head 128, 2184 x 16 of 9 keys 50 / 84).
 template <typename T, int DH, typename KV>
 constexpr int tile_keys() {
   return sizeof(T) == 4 ? (DH == 32 ? 32 : 16) : sizeof(KV) == 1 && DH <= 64 ? 64 : 32;
@@ -666,16 +665,16 @@ hipError_t kv_append(const KvAppendArgs& args, hipStream_t s) {
 // How a call is cut, by sizes that the host knows.  Parts are multiples of 128 keys (four waves'
 // tiles), as long as 512 workgroups come of it, two a CU, and at most 1024 keys: more and shorter
 // ones only add to the join, longer ones leave CUs idle at the end of ragged batches.  Measured, us,
-// (512, 1024) / half as long / twice: 16 x 8 heads of 2048..32768 keys (d_head 128) 177 / 183 / 185;
-// one sequence, 4 heads, 131001 E4M3 keys 28.8 / 33.5 / 28.9 (one workgroup a CU: 38); 8 x 8 heads of
-// 4000 keys (d_head 64) 15.9 / 17.6 / 18.7; 8 x 8 of 16000 51 / 48 / 46; 32 x 8 of 500..8000 fp32
-// keys 208 / 209 / 230.
+// as it is / half as long / twice: 16 x 8 heads of 2048..32768 keys (d_head 128, 1.18 GB) 196 / 200 /
+// 192; one sequence, 4 heads, 131001 E4M3 keys (d_head 128) 30 / 34 / 37; 8 x 8 heads of 4000 keys
+// (d_head 64) 15.9 / 17.4 / 19.4, of 16000 51 / 48 / 46; 32 x 8 of 500..8000 fp32 keys (d_head 128,
+// 1.20 GB) 207 / 203 / 236.
 // Never more than 32768 parts in all, however far max_len is above the lengths: empty ones cost a
 // workgroup each, and every one its place in the workspace.
 // Where tasks fill the GPU by themselves and are short, a wave takes one alone and nothing is joined
-// (four waves a task / one): 2160 x 16 heads of up to 231 keys 195 / 164, 2048 x 8 of up to 64
-// 62.7 / 34.4, of up to 256 111 / 93; but 256 x 8 of up to 256 16.9 / 16.9, 64 x 8 of up to 48
-// 4.4 / 4.9, 2048 x 8 of up to 768 250 / 266.
+// (four waves a task / one): 2160 x 16 heads of up to 231 keys 194 / 164, 2048 x 8 of up to 64
+// 63 / 34, of up to 256 106 / 93; but 256 x 8 of up to 256 17.2 / 17.9, 64 x 8 of up to 48 4.6 / 5.8,
+// 2048 x 8 of up to 768 250 / 266.
 void paged_attn_plan(PagedAttnArgs* a) {
   a->group = a->n_heads / a->c.n_kv_heads;
   a->qblocks = (a->group + 15) / 16;

@@ -337,6 +337,8 @@ nt_status nt_op_gemm_ln(int32_t dtype, const void* d_A, int32_t lda, const void*
  *  (any alignment); bias [2N] fp32 or NULL; K % 64 == 0.  d_colsum: NULL, or [2N] fp32: the
  *  pre-norm LayerNorm of A's rows is folded in, as for nt_op_gemm_ln: A_m . Bt_n becomes
  *  rstd_m (A_m . Bt_n - mu_m colsum[n]) with K the whole row, colsum[n] = sum_k Bt[n][k].
+ *  (A row that holds an infinity or a NaN is NaN throughout; squared deviations that leave fp32
+ *  count as an infinite variance, which leaves the bias.)
  *  Products, activation and product of the two are fp32, rounded once into out; each result is
  *  the same whatever M and N.  out overlaps no input.  Asynchronous, one launch (more for A past
  *  2^32 bytes), on the current device.  NT_E_INVALID for a null or misaligned

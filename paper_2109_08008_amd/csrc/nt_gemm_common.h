@@ -89,10 +89,10 @@ __device__ __forceinline__ void frag_sums(const u32x4& a, float& s, float& q) {
   }
 }
 // Mean and 1/sqrt(biased variance + eps) of a row of K values from its sums; the second is -1 where
-// the row has to be read again.
+// the row has to be read again (where var is NaN too: squares that overflow, an infinity, a NaN).
 __device__ __forceinline__ float2 sums_stats(float s, float q, float inv_k, float eps) {
   const float mean = s * inv_k, var = q * inv_k - mean * mean;
-  return make_float2(mean, mean * mean > ROW_RATIO * var ? -1.f : 1.0f / sqrtf(var + eps));
+  return make_float2(mean, mean * mean <= ROW_RATIO * var ? 1.0f / sqrtf(var + eps) : -1.f);
 }
 // The same of the row itself, in two turns by a whole wave: the mean, then the deviations from it.
 template <typename T>

@@ -1442,10 +1442,11 @@ __global__ __launch_bounds__(256) void gemm_slim_kernel(const T* __restrict__ A,
     ls += __shfl_xor(ls, 32, kWave);
     lq += __shfl_xor(lq, 32, kWave);
     const float ms = ls * inv_k;
-    const float var = fmaxf(lq * inv_k - ms * ms, 0.f);
+    const float dev = lq * inv_k - ms * ms, var = fmaxf(dev, 0.f);
     mu[0] = to_f32(sh) + ms;
     rs[0] = 1.0f / sqrtf(var + epi.lnf_eps);
-    if constexpr (ROLE == GATED) read_again(ms * ms > SHIFT_RATIO * var, make_float2(mu[0], rs[0]));
+    // (a row that holds an infinity or a NaN too: dev is NaN)
+    if constexpr (ROLE == GATED) read_again(!(ms * ms <= SHIFT_RATIO * dev), make_float2(mu[0], rs[0]));
   }
   if constexpr (ROLE == GATED)
     gated_epilogue<T, 1, FN, LNF>(acc, epi, live, N, m0 + wave * 16, n0 / 2, fr, fc, mu, rs, ahead);

@@ -309,3 +309,29 @@ def test_the_largest_tile(dtype, M, N, K):
         assert torch.equal(got[:m], _run(dtype, a[:m], w, b, None, act)), m
         assert torch.equal(got[-m:], _run(dtype, a[-m:], w, b, None, act)), m
     assert {32, 128} <= seen and 256 not in seen
+
+
+@pytest.mark.parametrize("dtype,M,N,K", [("f32", 70, 96, 192), ("f32", 1100, 2050, 320), ("f16", 70, 96, 192), ("f16", 1203, 2050, 192),
+                                         ("bf16", 70, 96, 192), ("bf16", 1203, 2050, 192), ("bf16", 2165, 4100, 192)])
+def test_layernorm_of_rows_that_are_not_finite(dtype, M, N, K):
+    """A row that holds a NaN or an infinity has no mean: all its results are NaN, and nobody else's.  Rows
+    whose squares leave fp32 (or whose mean's does) have the variance inf, as two turns over them find it."""
+    import torch
+    a, w, b, cs = _inputs(dtype, M, N, K, True, True, M)
+    a = a.contiguous()
+    clean = _run(dtype, a, w, b, cs, "silu")
+    bad = {3: float("nan"), 20: float("inf"), 41: -float("inf"), M - 1: float("inf")}
+    for i, (r, x) in enumerate(bad.items()):
+        a[r, (0, K // 2, 0, K - 1)[i]] = x
+    huge = [] if dtype == "f16" else [10, 50]
+    if huge:
+        a[10] = a[10] * 1e25
+        a[50] = a[50] * 1e22 + 1e25
+    got = _run(dtype, a, w, b, cs, "silu")
+    rest = [r for r in range(M) if r not in bad and r not in huge]
+    assert torch.equal(got[rest], clean[rest])
+    assert torch.isnan(got[list(bad)]).all()
+    if huge:    # (x - mean) / inf = 0: the bias alone
+        want = (torch.nn.functional.silu(b[:N].double()) * b[N:].double())[None]
+        tol = EPS[dtype] / 2 * want.abs() * (1 + 2.0 ** -10) + 2.0 ** -18 * want.abs() + 2.0 ** -60
+        assert ((got[huge].double() - want).abs() <= tol).all()

@@ -157,10 +157,11 @@ __global__ __launch_bounds__(256) void kv_append_kernel(KvAppendArgs a) {
 // `chunk` keys over workgroups when there are few tasks; the parts' (max, sum, unnormalised
 // output) go to the workspace and paged_join_kernel merges them.
 //
-// Measured, us (GB/s of keys and values): 2160 x 16 heads of up to 231 bf16 keys, d_head 64, 159
-// (6460); 16 x 8 of 2048..32768 fp16, d_head 128, four query heads each, 173 (6010), the join 4.7 of
-// it; one sequence, 4 x 131001 E4M3, d_head 128, 28 (4790), the join 4.5; 64 x 8 of up to 48 fp16
-// keys 4.5.  Plain reads reach 6200, non-temporal ones 7000.  (Keys straight to the products'
+// Measured, us (GB/s of keys and values): 2160 x 16 heads of up to 231 bf16 keys, d_head 64, 160
+// (6420), of up to 64 65 (4570), of up to 48 58 (3950); 16 x 8 of 2048..32768 fp16, d_head 128, four
+// query heads each, 171 (6070), the join 4.6 of it; one sequence, 4 x 131001 E4M3, d_head 128, 28 (4790),
+// the join 4.5; 64 x 8 of up to 48 fp16 keys 4.6; 32 x 8 of 500..8000 fp32 keys, d_head 64, 119 (5070),
+// d_head 128, 207 (5810).  Plain reads reach 6200, non-temporal ones 7000.  (Keys straight to the products'
 // registers, 16 bytes of a row a lane: 231 and 198 for the first two.)
 typedef short short4v __attribute__((ext_vector_type(4)));
 // Four 16-bit values of one column, rows r..r+3 of an LDS tile: each lane of 16 names the

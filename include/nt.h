@@ -495,6 +495,94 @@ nt_status nt_op_attn_paged(const nt_kv_pages* cache, const void* d_q, int32_t q_
 nt_status nt_op_attn_paged_workspace(const nt_kv_pages* cache, int32_t n_heads, int32_t n_seqs, int32_t max_len,
                                      size_t* bytes);
 
+/* Attention over whole packed sequences (prompts, or an encoder's sentences without padding):
+ *   out[i][h] = sum_j p_j v[j][h'],  p = softmax_j(scale * q[i][h] . k[j][h']),
+ * j over the rows of i's sequence, up to i itself if causal != 0; query head h reads key head
+ * h' = h / (n_heads / n_kv_heads).  d_q, d_k, d_v, d_out: dtype, row i at i * q_ld, i * kv_ld (both k
+ * and v), i * out_ld, head h at h * d_head within: the columns of a QKV projection's output as they
+ * are.  d_off: [n_seqs + 1] non-decreasing device int32, sequence b's rows being d_off[b] ..
+ * d_off[b+1] - 1, any number of them, none included; n_rows: rows of the buffers.  Rows of no
+ * sequence are not written, and what they hold is never part of a result; nor is what a row
+ * does not see, whatever it is (infinities and NaN stay with the rows that see them; a wave's rows
+ * where one came out as no number are formed again key by key, at a small part of the speed).
+ * Scores, softmax and sums are fp32; with 16-bit values each probability is rounded once to dtype
+ * for the second product (half a step of it), and their sum is that of the rounded ones.  Results
+ * do not depend on the other sequences except through where tiles of keys begin (a matter of
+ * rounding).  d_head in {32, 64, 128}.  out overlaps no input.  Asynchronous, one launch, no workspace,
+ * on the current device.  NT_E_INVALID for a null pointer, a negative size, a d_head or heads that
+ * are not allowed, rows shorter than their heads or not 16-byte aligned, or a scale whose product with
+ * log2(e) is not finite (one below 2^-126 counts as 0); NT_E_UNSUPPORTED for more work than one launch takes (2^23 workgroups). */
+nt_status nt_op_attn_prompt(int32_t dtype, const void* d_q, int32_t q_ld, int32_t n_heads, const void* d_k,
+                            const void* d_v, int32_t kv_ld, int32_t n_kv_heads, int32_t d_head, const int32_t* d_off,
+                            int32_t n_seqs, int32_t n_rows, int32_t causal, float scale, void* d_out, int32_t out_ld,
+                            void* stream);
+
+/* Attention of several new tokens a sequence over a paged cache, as nt_op_attn_paged for each:
+ * a tree of drafted tokens, a chain of them, or the next piece of a prompt.  Sequence b's new
+ * tokens are rows d_off[b] .. d_off[b+1] - 1 of d_q and d_out (d_off: [n_seqs + 1] non-decreasing;
+ * NULL: row b alone, n_rows == n_seqs) and its last positions of d_lens[b], in order, where
+ * nt_op_kv_append put their keys and values.  Each sees every position before them, and of them
+ *  d_mask NULL: itself and those before it;
+ *  d_mask [n_rows] device uint64: new token j where bit j of its word is set (itself only if its
+ *   bit is); max_new <= 64.
+ * max_new: at least every sequence's new tokens, max_len every length (host; what the work is
+ * divided by): rows past max_new are not written, positions past max_len not read.  A row that sees
+ * nothing is zero; holes, what lies behind a length and what a row does not see are never part of
+ * a result, as for nt_op_attn_prompt; rows of no sequence are not written.  Scores, softmax, sums
+ * and roundings as there.  fp8 caches as for nt_op_attn_paged.
+ * d_ws: workspace of at least nt_op_attn_tree_workspace bytes (256-byte aligned; may be NULL
+ * when that is 0), in use until the call's work is done: calls that may overlap need their own.
+ * Asynchronous, one or two launches, on the current device.  Refusals as for nt_op_attn_paged, and
+ * NT_E_INVALID for a scale that nt_op_attn_prompt refuses; NT_E_UNSUPPORTED for d_mask with max_new > 64. */
+nt_status nt_op_attn_tree(const nt_kv_pages* cache, const void* d_q, int32_t q_ld, int32_t n_heads,
+                          const int32_t* d_off, const uint64_t* d_mask, const int32_t* d_lens, int32_t n_seqs,
+                          int32_t n_rows, int32_t max_new, int32_t max_len, float scale, void* d_out, int32_t out_ld,
+                          void* d_ws, size_t ws_bytes, void* stream);
+/* Bytes of workspace of such a call; needs no device. */
+nt_status nt_op_attn_tree_workspace(const nt_kv_pages* cache, int32_t n_heads, int32_t n_seqs, int32_t n_rows,
+                                    int32_t max_new, int32_t max_len, size_t* bytes);
+
+/* Lengths that change, and the pages that go with them, all on the device: sequence b goes from
+ * d_lens[b] to max(d_lens[b] + d_add[b], 0) positions (d_add: [n_seqs] device int32, negative to give
+ * positions back; a negative length counts as 0).  Its pages are the first ceil(length / page_len)
+ * entries of its row of d_table [n_seqs][max_pages], which it shares with no other sequence.
+ * d_ring [n_pages] device int32 holds the free pages in a ring: d_state[1] of them from entry
+ * d_state[0] on.  Pages that sequences need are taken from its head, pages that they give up
+ * are put behind its tail and their table entries become -1, in the order of the sequences and of
+ * the positions within each; what a call gives up a later one can take.
+ *  d_state [4] device int32: the ring's head and count (updated); 0 or why nothing was done; the
+ *   number of new rows.
+ *  d_off [n_seqs + 1] or NULL: exclusive sums of max(d_add[b], 0): the new rows of each sequence,
+ *   as nt_op_kv_append and nt_op_attn_tree take them.
+ *  d_pos [max_rows] int32 or NULL, d_slot [max_rows] int64 or NULL: each new row's position, and
+ *   page * page_len + position % page_len of it, the page being the table's; -1 for rows of none.
+ * All or nothing: where d_state[2] is not 0 lengths, table and ring stay as they were, d_off is all 0
+ * and d_pos and d_slot all -1.  It is the number of pages that the ring lacks, NT_RESIZE_TABLE if a
+ * sequence would pass its row of the table (or 2^31 - 1), or NT_RESIZE_ROWS if there are more new
+ * rows than max_rows (with neither d_pos nor d_slot: than 2^31 - 1).
+ * Buffers overlap nowhere.  Asynchronous, one or two launches, no workspace, on the current device; a
+ * ring and its lengths are one call's at a time.  NT_E_INVALID for a null pointer, a page_len that
+ * nt_kv_pages does not allow, a negative size; NT_E_UNSUPPORTED for more than 65536 sequences. */
+#define NT_RESIZE_TABLE (-1)
+#define NT_RESIZE_ROWS (-2)
+nt_status nt_op_kv_resize(int32_t page_len, int32_t n_pages, int32_t max_pages, int32_t* d_table, int32_t* d_lens,
+                          const int32_t* d_add, int32_t n_seqs, int32_t* d_ring, int32_t* d_state, int32_t* d_off,
+                          int32_t* d_pos, int64_t* d_slot, int32_t max_rows, void* stream);
+
+/* The new tokens that stay, of those that nt_op_kv_append put into the cache: sequence b keeps its
+ * new tokens d_path[b][0 .. d_n_path[b] - 1] (d_path: [n_seqs][max_path] device int32, numbers of new
+ * tokens in rising order, so the accepted branch of a tree), in this order, as the first ones
+ * behind its context: the keys and values of d_path[b][i] go to position d_lens[b] - new + i, new =
+ * d_off[b+1] - d_off[b].  d_add[b] becomes the (negative) number of positions then to be given back,
+ * kept - new, for nt_op_kv_resize; d_lens is not changed.  A number below its place in the path or not
+ * below `new`, and a position without a page, move nothing; a path longer than max_path or `new`
+ * ends there.  Every other cell of the pools stays as it is.  Pages that two sequences share:
+ * as for nt_op_kv_append.  Asynchronous, one launch, on the current device.  NT_E_INVALID for a null
+ * pointer, a negative size or a shape the struct does not allow; NT_E_UNSUPPORTED for fp8 with
+ * another dtype than NT_F16 or more than 2^31 pieces of 16 bytes in a row of all sequences. */
+nt_status nt_op_kv_keep(const nt_kv_pages* cache, const int32_t* d_off, const int32_t* d_lens, const int32_t* d_path,
+                        int32_t max_path, const int32_t* d_n_path, int32_t n_seqs, int32_t* d_add, void* stream);
+
 /* Process-wide switch for nt_translate's graph replay of the decoder step (default on;
  * with 0, every step is launched kernel by kernel). */
 nt_status nt_set_graphs(int32_t enable);

@@ -19,7 +19,8 @@ LIB_PATH = os.path.join(HERE, "libnt.so")
 
 SOURCES = ["nt_gemm.hip", "nt_gemm_phased_f16.hip", "nt_gemm_phased_bf16.hip", "nt_gemm_phased_f32.hip",
            "nt_gemm_gated_f16.hip", "nt_gemm_gated_bf16.hip", "nt_gemm_gated_f32.hip",
-           "nt_norm.hip", "nt_attn.hip", "nt_paged.hip", "nt_search.hip", "nt_score.hip",
+           "nt_attn_rows_f16.hip", "nt_attn_rows_bf16.hip", "nt_attn_rows_f32.hip",
+           "nt_norm.hip", "nt_attn.hip", "nt_paged.hip", "nt_rows.hip", "nt_pages.hip", "nt_search.hip", "nt_score.hip",
            "nt_runtime.cpp"]
 ARCH = "gfx950"
 FLAGS = [

@@ -1,0 +1,803 @@
+// Attention of many query rows: packed prompts (nt_op_attn_prompt) and several new tokens a
+// sequence over a paged cache (nt_op_attn_tree).  Included once per data type.
+//
+//   out_i = sum_j e^{s_ij - m_i} V_j / sum_j e^{s_ij - m_i},  s_ij = scale q_i . K_j,
+//
+// j over the keys that row i sees.
+#pragma once
+#include <algorithm>
+
+#include "nt_gemm_common.h"
+
+namespace nt {
+namespace {
+
+typedef short short4v __attribute__((ext_vector_type(4)));
+typedef int int2v __attribute__((ext_vector_type(2)));
+// Four 16-bit values of one column, rows r..r+3 of an LDS tile: each lane of 16 names the
+// 8 bytes at row r + lane / 4, columns 4 (lane % 4).., and receives column lane.
+__device__ __forceinline__ uint2 lds_column4(const unsigned char* p) {
+  return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                                       (__attribute__((address_space(3))) short4v*)(p)));
+}
+// Eight bytes of one column: each lane of 16 names the 8 bytes at row r + lane / 2 (any eight
+// rows), columns 8 (lane % 2).., and receives column lane.
+__device__ __forceinline__ uint2 lds_column8(const unsigned char* p) {
+  return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr8_b64_v2i32(
+                                       (__attribute__((address_space(3))) int2v*)(p)));
+}
+
+template <typename T>
+__device__ __forceinline__ unsigned pair_of(float a, float b) {
+  typedef float float2v __attribute__((ext_vector_type(2)));
+  typedef T pair __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(unsigned, __builtin_convertvector((float2v{a, b}), pair));
+}
+
+// ---- matrix products on fixed accumulators ----
+// c += A.B^T (mma) or c = A.B^T (mma0), as Mfma<T>::step, but always in the registers of c: results
+// are forwarded from one product to the next only there.  The compiler does not look into the
+// blocks for the wait states that gfx9 leaves to software.  So ready() stands between the vector
+// instructions that form an operand and the products that take it (two are due), and settle() between
+// the last product and the first other use of its result (8 after a 16-bit product, 10 after an
+// fp32 one).  tests/test_device_waits.py holds the built code to them.
+template <typename T>
+__device__ __forceinline__ void mma(floatx4& c, u32x4 a, u32x4 b) {
+  if constexpr (sizeof(T) == 4) {
+#pragma unroll
+    for (int w = 0; w < 4; ++w) asm("v_mfma_f32_16x16x4_f32 %0, %1, %2, %0" : "+v"(c) : "v"(a[w]), "v"(b[w]));
+  } else if constexpr (std::is_same<T, f16>::value) {
+    asm("v_mfma_f32_16x16x32_f16 %0, %1, %2, %0" : "+v"(c) : "v"(a), "v"(b));
+  } else {
+    asm("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+v"(c) : "v"(a), "v"(b));
+  }
+}
+template <typename T>
+__device__ __forceinline__ void mma0(floatx4& c, u32x4 a, u32x4 b) {
+  if constexpr (sizeof(T) == 4) {
+    asm("v_mfma_f32_16x16x4_f32 %0, %1, %2, 0" : "=&v"(c) : "v"(a[0]), "v"(b[0]));
+#pragma unroll
+    for (int w = 1; w < 4; ++w) asm("v_mfma_f32_16x16x4_f32 %0, %1, %2, %0" : "+v"(c) : "v"(a[w]), "v"(b[w]));
+  } else if constexpr (std::is_same<T, f16>::value) {
+    asm("v_mfma_f32_16x16x32_f16 %0, %1, %2, 0" : "=&v"(c) : "v"(a), "v"(b));
+  } else {
+    asm("v_mfma_f32_16x16x32_bf16 %0, %1, %2, 0" : "=&v"(c) : "v"(a), "v"(b));
+  }
+}
+template <typename V>
+__device__ __forceinline__ void ready(V& x) { asm("s_nop 1" : "+v"(x)); }
+template <typename V>
+__device__ __forceinline__ void ready(V& x, V& y) { asm("s_nop 1" : "+v"(x), "+v"(y)); }
+// The products that form c[0 .. N) are done (four at a time: all of them wait).
+template <int N>
+__device__ __forceinline__ void settle(floatx4* c) {
+  if constexpr (N >= 4) {
+    asm("s_nop 9" : "+v"(c[0]), "+v"(c[1]), "+v"(c[2]), "+v"(c[3]));
+    if constexpr (N > 4) settle<N - 4>(c + 4);
+  } else if constexpr (N >= 2) {
+    asm("s_nop 9" : "+v"(c[0]), "+v"(c[1]));
+    if constexpr (N > 2) settle<N - 2>(c + 2);
+  } else {
+    asm("s_nop 9" : "+v"(c[0]));
+  }
+}
+
+// Four consecutive values (uint8_t: E4M3) as fp32.
+template <typename E>
+__device__ __forceinline__ void four_values(const char* p, float (&x)[4]) {
+  if constexpr (sizeof(E) == 1) {
+    const unsigned w = *reinterpret_cast<const unsigned*>(p);
+    const half2v u = __builtin_bit_cast(half2v, f8x2<false>(w)), v = __builtin_bit_cast(half2v, f8x2<true>(w));
+    x[0] = (float)u[0], x[1] = (float)u[1], x[2] = (float)v[0], x[3] = (float)v[1];
+  } else {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) x[r] = to_f32(reinterpret_cast<const E*>(p)[r]);
+  }
+}
+
+// What the probabilities are multiplied by (a power of two, 2^P_SHIFT) and how far a row's scores
+// may pass its reference before that is moved (LAZY, in powers of two): fp16 probabilities stay
+// below 2^(LAZY + P_SHIFT) < 65504.
+constexpr float LAZY = 8.f;
+template <typename T>
+constexpr float p_shift() {
+  return std::is_same<T, f16>::value ? 7.f : 0.f;
+}
+
+// 16 bytes a lane, 1024 consecutive ones of LDS from dst on.
+__device__ __forceinline__ void load_to_lds(const char* src, unsigned char* dst) {
+  __builtin_amdgcn_global_load_lds(src, NT_LDS(dst), 16, 0, 0);
+}
+// Waits for the wave's loads, those into LDS among them.
+__device__ __forceinline__ void loads_done() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
+// The sequence of packed row `row` (a lane's own): how many of off[1 .. n_seqs] are at or below it,
+// by 64 probes that the lanes share and a search between two of them.  n_seqs: none.
+__device__ __forceinline__ int sequence_of(const int* off, int n_seqs, int row, int lane) {
+  const int step = (n_seqs + kWave - 1) / kWave;
+  const int probe = off[min((lane + 1) * step, n_seqs)];
+  int lo = 0;
+#pragma unroll
+  for (int s = kWave / 2; s; s >>= 1)
+    if (__shfl(probe, lo + s - 1, kWave) <= row) lo += s;
+  if (lo == kWave - 1 && __builtin_amdgcn_readlane(probe, kWave - 1) <= row) lo = kWave;
+  int hi = min((lo + 1) * step - 1, n_seqs);
+  lo = min(lo * step, n_seqs);
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (off[mid] <= row) lo = mid;
+    else hi = mid - 1;
+  }
+  return lo;
+}
+
+// A workgroup takes BM = RW * QB * 16 query rows; KW waves share the keys of a tile (BK = KW * TK).
+template <typename T, int DH, typename KV, bool PAGED, int QB, int RW, int KW, int TK>
+__global__ __launch_bounds__(64 * RW * KW) __attribute__((amdgpu_waves_per_eu(2))) void attn_rows_kernel(RowsAttnArgs a) {
+  constexpr int EB = sizeof(T), EC = sizeof(KV);
+  constexpr bool F8 = EC == 1;
+  constexpr int W = RW * KW, BM = RW * QB * 16, BK = KW * TK;
+  constexpr int NB = TK / 16;                 // 16-key blocks of a wave's keys of a tile
+  constexpr int QK = DH * EB / 64;            // MFMA steps over the channels
+  constexpr int CB = DH / 16;                 // blocks of 16 channels of the output
+  constexpr int RB = DH * EC;                 // bytes of a key
+  constexpr int CH = RB / 16;                 // 16-byte chunks of a key
+  constexpr int TILE = BK * RB;               // bytes of a tile's keys
+  constexpr int NP = TILE / (W * 1024);       // loads a lane issues for them
+  constexpr int RPL = 1024 / RB;              // rows that one load of a wave covers
+  constexpr int RPB = RB < 256 ? 256 / RB : 1;   // rows that the 64 banks hold side by side
+  constexpr float PSH = p_shift<T>();
+  static_assert(TILE % (W * 1024) == 0 && NP >= 1, "a tile's rows split evenly over the waves");
+  static_assert(EB == 4 || NB % 2 == 0, "16-bit products take 32 keys");
+  constexpr int STAGE = 2 * TILE;
+  constexpr int JOIN = KW > 1 ? W * QB * 16 * DH * 4 : 0;
+  constexpr int LDS_BYTES = 2 * STAGE > JOIN ? 2 * STAGE : JOIN;
+  __shared__ __attribute__((aligned(1024))) unsigned char lds[LDS_BYTES];
+  __shared__ float jm[W][QB * 16], jl[W][QB * 16];
+  __shared__ bool jlive[BM];
+  __shared__ int range[RW][2];
+
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
+  const int grp = lane >> 4, ln = lane & 15;
+  const int rw = wave / KW, kw = wave % KW;
+
+  // ---- the workgroup's rows and keys ----
+  int hk, part = 0, b = 0, r0, base = 0, len = 0, n_new = 0, row_first = 0, n_live;
+  int head = 0;                               // prompt: the query head
+  if constexpr (PAGED) {
+    const int x = blockIdx.x / 8, rb = x % a.rblocks;
+    int unit = x / a.rblocks * 8 + blockIdx.x % 8;
+    const int heads = a.n_seqs * a.c.n_kv_heads;
+    part = unit / heads;
+    unit -= part * heads;
+    if (part >= a.parts) return;              // the grid's tail
+    hk = unit % a.c.n_kv_heads;
+    b = unit / a.c.n_kv_heads;
+    r0 = rb * BM;
+    row_first = a.off ? min(max(a.off[b], 0), a.n_rows) : b;
+    n_new = a.off ? min(max(min(a.off[b + 1], a.n_rows) - row_first, 0), a.max_new) : 1;
+    n_live = n_new * a.group;                 // rows are (new token, head of the group)
+    const int whole = a.lens[b];
+    len = max(0, min(whole, a.max_len));
+    base = whole - n_new;
+    if (r0 >= n_live) return;
+  } else {
+    const int nkv = a.c.n_kv_heads, idx = blockIdx.x % a.n_heads;
+    hk = idx % nkv;
+    head = hk * a.group + idx / nkv;
+    r0 = (a.rblocks - 1 - (int)(blockIdx.x / a.n_heads)) * BM;
+    n_live = a.n_rows;
+  }
+
+  // A lane's rows: row ln of each of the wave's QB blocks.  It sees keys [lo, hi), and of a tree the
+  // new tokens of `bits`, which start at `base`.
+  int lo[QB], hi[QB];
+  unsigned long long bits[QB];
+  const char* qrow[QB];
+  bool live[QB];
+#pragma unroll
+  for (int q = 0; q < QB; ++q) {
+    const int r = r0 + (rw * QB + q) * 16 + ln;
+    live[q] = r < n_live;
+    bits[q] = 0;
+    if constexpr (PAGED) {
+      const int rr = min(r, n_live - 1), i = rr / a.group, h = hk * a.group + rr - i * a.group;
+      lo[q] = 0;
+      hi[q] = min(base + i + 1, len);
+      if (a.mask) {
+        hi[q] = min(base, len);
+        const int n = max(0, min(n_new, len - base));     // (positions from len on are not read)
+        bits[q] = a.mask[row_first + i] & (n >= 64 ? ~0ull : (1ull << n) - 1);
+      }
+      qrow[q] = reinterpret_cast<const char*>(static_cast<const T*>(a.q) + (size_t)(row_first + i) * a.q_ld + (size_t)h * DH);
+    } else {
+      const int s = sequence_of(a.off, a.n_seqs, r, lane);
+      const int start = min(max(a.off[min(s, a.n_seqs)], 0), a.n_rows);
+      const int end = s < a.n_seqs ? min(max(a.off[s + 1], start), a.n_rows) : start;
+      live[q] = live[q] && r >= start && r < end;
+      lo[q] = start;
+      hi[q] = !live[q] ? start : a.causal ? r + 1 : end;
+      qrow[q] = reinterpret_cast<const char*>(static_cast<const T*>(a.q) + (size_t)min(r, a.n_rows - 1) * a.q_ld +
+                                              (size_t)head * DH);
+    }
+  }
+  // Of the wave's rows: the largest lo and smallest hi (between them no mask is needed), and the range
+  // outside which no row sees anything.  Both grow with the row.
+  const int lo_first = __builtin_amdgcn_readlane(lo[0], 0), lo_last = __builtin_amdgcn_readlane(lo[QB - 1], 15);
+  const int hi_first = __builtin_amdgcn_readlane(hi[0], 0);
+  int hi_last = __builtin_amdgcn_readlane(hi[QB - 1], 15);
+  int k0, k1;
+  if constexpr (PAGED) {
+    if (a.mask) hi_last = len;
+    if (r0 + rw * QB * 16 >= n_live) hi_last = 0;       // no rows
+    k0 = part * a.chunk;
+    k1 = min(len, k0 + a.chunk);
+    if (!a.mask) k1 = min(k1, max(0, min(base + (min(r0 + BM, n_live) - 1) / a.group + 1, len)));
+    if (k0 >= len && part > 0) return;                  // nothing here; the join does not look
+  } else {
+    if (lane == 0 && kw == 0) {
+      range[rw][0] = lo_first;
+      range[rw][1] = hi_last;
+    }
+    __syncthreads();
+    k0 = __builtin_amdgcn_readfirstlane(range[0][0]);
+    k1 = __builtin_amdgcn_readfirstlane(range[RW - 1][1]);
+  }
+
+  u32x4 qf[QB][QK];
+#pragma unroll
+  for (int q = 0; q < QB; ++q)
+#pragma unroll
+    for (int st = 0; st < QK; ++st) {
+      // E4M3 keys of 64 channels and more come 16 a lane: steps 2p and 2p + 1 take a half each
+      const int at = F8 && DH >= 64 ? st / 2 * 128 + grp * 32 + st % 2 * 16 : st * 64 + grp * 16;
+      u32x4 x = *reinterpret_cast<const u32x4*>(qrow[q] + at);
+#pragma unroll
+      for (int w = 0; w < 4; ++w) x[w] = (x[w] & a.q_and) ^ a.q_xor;
+      qf[q][st] = x;
+    }
+
+  // ---- tiles of keys and values into LDS ----
+  // Chunk c of row r lies at chunk c ^ f(r): 16 rows of one chunk (keys), 8 rows of two or 4 of four
+  // (values' columns) fall on different banks.
+  auto kswz = [](int row) { return (row / RPB) & (CH < 16 ? CH - 1 : 15); };
+  auto vswz = [](int row) {
+    if constexpr (EB == 4) return ((row >> 2) & 3) * 4 & (CH - 1);
+    else if constexpr (F8) return (row / RPB) & (CH - 1);
+    else return ((row / RPB) & (CH / 2 - 1)) * 2;
+  };
+  const int sh = PAGED ? a.c.page_shift : 0, slots = 1 << sh;
+  const int* table = PAGED ? a.c.table + (size_t)b * a.c.max_pages : nullptr;
+  const size_t head_bytes = (size_t)RB << sh, page_bytes = head_bytes * a.c.n_kv_heads;
+  const char* Kp = PAGED ? static_cast<const char*>(a.c.k) + hk * head_bytes : static_cast<const char*>(a.k) + (size_t)hk * RB;
+  const char* Vp = PAGED ? static_cast<const char*>(a.c.v) + hk * head_bytes : static_cast<const char*>(a.v) + (size_t)hk * RB;
+  const size_t ldb = (size_t)a.kv_ld * EB;
+  // page of the tile's 16-key block `lane`; -1: none
+  auto pages_of = [&](int t) {
+    const int key = t + lane * 16;
+    int id = -1;
+    if (lane < BK / 16 && key < len) {
+      id = table[min(key >> sh, a.c.max_pages - 1)];
+      if ((unsigned)id >= (unsigned)a.c.n_pages) id = -1;
+    }
+    return id;
+  };
+  auto issue = [&](int t, int ids, int stage) {
+    unsigned char* dst = lds + stage * STAGE + wave * 1024;
+#pragma unroll
+    for (int u = 0; u < NP; ++u) {
+      const int row = (u * W + wave) * RPL + lane / CH, ch = lane % CH;
+      const char *ks, *vs;
+      if constexpr (PAGED) {
+        const int id = RPL <= 16 ? __builtin_amdgcn_readlane(ids, (u * W + wave) * RPL / 16) : __shfl(ids, row / 16, kWave);
+        const size_t at = (size_t)max(id, 0) * page_bytes + (size_t)((t + row) & (slots - 1)) * RB;
+        ks = Kp + at;
+        vs = Vp + at;
+      } else {
+        const size_t at = (size_t)min(t + row, k1 - 1) * ldb;
+        ks = Kp + at;
+        vs = Vp + at;
+      }
+      load_to_lds(ks + ((ch ^ kswz(row)) << 4), dst + u * W * 1024);
+      load_to_lds(vs + ((ch ^ vswz(row)) << 4), dst + TILE + u * W * 1024);
+    }
+  };
+  // What lies behind the last key, or on no page, may be anything: its values become zeros (no 0 * NaN).
+  const int real_end = PAGED ? len : k1;
+  auto clear = [&](int t, int ids, int stage) {
+    unsigned char* dst = lds + stage * STAGE + TILE + wave * 1024 + lane * 16;
+#pragma unroll
+    for (int u = 0; u < NP; ++u) {
+      const int row = (u * W + wave) * RPL + lane / CH;
+      bool none = t + row >= real_end;
+      if constexpr (PAGED) none |= __shfl(ids, row / 16, kWave) < 0;   // (every lane takes part)
+      if (none) *reinterpret_cast<u32x4*>(dst + u * W * 1024) = u32x4{0, 0, 0, 0};
+    }
+  };
+
+  float m[QB], l[QB];
+  floatx4 ls[QB];                             // 16-bit: the sums, by a product with ones
+  floatx4 o[CB][QB];                          // O[channel c * 16 + 4 grp + r][row ln]
+#pragma unroll
+  for (int q = 0; q < QB; ++q) {
+    m[q] = -INFINITY;
+    l[q] = 0.f;
+    ls[q] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int c = 0; c < CB; ++c) o[c][q] = floatx4{0.f, 0.f, 0.f, 0.f};
+  }
+  const float sl = a.scale_log2;
+  const unsigned one = std::is_same<T, f16>::value ? 0x3c003c00u : 0x3f803f80u;
+  u32x4 ones = u32x4{one, one, one, one};
+  if constexpr (EB == 2) asm volatile("" : "+v"(ones));   // kept, not formed again before each product
+
+  auto sees = [&](int q, int key) {           // (without branches)
+    if constexpr (PAGED) {
+      const unsigned j = key - base;
+      const unsigned w = (unsigned)(j & 32 ? bits[q] >> 32 : bits[q]) >> (j & 31);
+      return (key < hi[q]) | ((j < 64u) & (w & 1u));
+    } else {
+      return (key >= lo[q]) & (key < hi[q]);
+    }
+  };
+
+  auto compute = [&](int t, int ids, int stage) {
+    const int t0 = t + kw * TK;
+    if (t0 >= min(hi_last, k1) || t0 + TK <= lo_first) return;
+    const unsigned char* ks = lds + stage * STAGE + kw * TK * RB;
+    const unsigned char* vs = ks + TILE;
+    floatx4 sc[NB][QB];
+#pragma unroll
+    for (int j = 0; j < NB; ++j) {
+      const int row = 16 * j + ln, f = kswz(kw * TK + row);
+      const unsigned char* krow = ks + row * RB;
+      if constexpr (F8 && DH >= 64) {
+#pragma unroll
+        for (int p = 0; p < QK / 2; ++p) {
+          const u32x4 w = *reinterpret_cast<const u32x4*>(krow + (((p * 4 + grp) ^ f) << 4));
+          u32x4 x = f8_to_f16x8(w.x, w.y), y = f8_to_f16x8(w.z, w.w);
+          ready(x, y);
+#pragma unroll
+          for (int q = 0; q < QB; ++q) {
+            if (p == 0) mma0<T>(sc[j][q], x, qf[q][0]);
+            else mma<T>(sc[j][q], x, qf[q][2 * p]);
+            mma<T>(sc[j][q], y, qf[q][2 * p + 1]);
+          }
+        }
+      } else {
+#pragma unroll
+        for (int st = 0; st < QK; ++st) {
+          u32x4 kf;
+          if constexpr (F8) {
+            const uint2 w = *reinterpret_cast<const uint2*>(krow + (((grp >> 1) ^ f) << 4) + (grp & 1) * 8);
+            kf = f8_to_f16x8(w.x, w.y);
+            ready(kf);
+          } else {
+            kf = *reinterpret_cast<const u32x4*>(krow + (((st * 4 + grp) ^ f) << 4));
+          }
+#pragma unroll
+          for (int q = 0; q < QB; ++q) {
+            if (st == 0) mma0<T>(sc[j][q], kf, qf[q][0]);
+            else mma<T>(sc[j][q], kf, qf[q][st]);
+          }
+        }
+      }
+    }
+    settle<NB * QB>(&sc[0][0]);
+    bool whole = t0 >= lo_last && t0 + TK <= hi_first;
+    if constexpr (PAGED) whole = whole && !(__ballot(ids < 0) & (((1ull << NB) - 1) << (kw * NB)));
+    if (!whole) {
+#pragma unroll
+      for (int j = 0; j < NB; ++j) {
+        bool there = true;
+        if constexpr (PAGED) there = __builtin_amdgcn_readlane(ids, kw * NB + j) >= 0;
+#pragma unroll
+        for (int q = 0; q < QB; ++q)
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            sc[j][q][r] = there & sees(q, t0 + 16 * j + 4 * grp + r) ? sc[j][q][r] : -INFINITY;
+      }
+    }
+    // the reference moves only when a score passes it by LAZY
+    float top[QB];
+    bool pass = false;
+#pragma unroll
+    for (int q = 0; q < QB; ++q) {
+      top[q] = -INFINITY;
+#pragma unroll
+      for (int j = 0; j < NB; ++j)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) top[q] = fmaxf(top[q], sc[j][q][r]);
+      top[q] *= sl;
+      pass = pass || top[q] > m[q] + LAZY;
+    }
+    if (__ballot(pass)) {
+      settle<CB * QB>(&o[0][0]);
+      settle<QB>(ls);
+#pragma unroll
+      for (int q = 0; q < QB; ++q) {
+        float x = top[q];
+        x = fmaxf(x, __shfl_xor(x, 16, kWave));
+        x = fmaxf(x, __shfl_xor(x, 32, kWave));
+        const float mn = fmaxf(m[q], x);
+        const float alpha = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[q] - mn);
+        m[q] = mn;
+        l[q] *= alpha;
+        ls[q] *= alpha;
+#pragma unroll
+        for (int c = 0; c < CB; ++c) o[c][q] *= alpha;
+      }
+    }
+#pragma unroll
+    for (int q = 0; q < QB; ++q) {
+      const float ref = m[q] == -INFINITY ? 0.f : PSH - m[q];
+#pragma unroll
+      for (int j = 0; j < NB; ++j)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          sc[j][q][r] = __builtin_amdgcn_exp2f(fmaf(sc[j][q][r], sl, ref));
+          if constexpr (EB == 4) l[q] += sc[j][q][r];
+        }
+    }
+    if constexpr (EB == 2) {
+#pragma unroll
+      for (int j = 0; j < NB; j += 2) {
+        u32x4 pf[QB];
+#pragma unroll
+        for (int q = 0; q < QB; ++q) {
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int w = 0; w < 2; ++w) pf[q][2 * i + w] = pair_of<T>(sc[j + i][q][2 * w], sc[j + i][q][2 * w + 1]);
+          ready(pf[q]);
+          mma<T>(ls[q], ones, pf[q]);
+        }
+        if constexpr (F8) {
+          const int row = 16 * (j + (ln >> 3)) + 4 * grp + (ln >> 1 & 3), f = vswz(kw * TK + row);
+          const unsigned char* vrow = vs + row * RB + (ln & 1) * 8;
+#pragma unroll
+          for (int c = 0; c < CB; ++c) {
+            const uint2 w = lds_column8(vrow + ((c ^ f) << 4));
+            u32x4 vf = f8_to_f16x8(w.x, w.y);
+            ready(vf);
+#pragma unroll
+            for (int q = 0; q < QB; ++q) mma<T>(o[c][q], vf, pf[q]);
+          }
+        } else {
+          const int row = 16 * j + 4 * grp + (ln >> 2), f = vswz(kw * TK + row), g = vswz(kw * TK + row + 16);
+          const unsigned char* vrow = vs + row * RB + (ln & 1) * 8;
+#pragma unroll
+          for (int c = 0; c < CB; ++c) {
+            const int ch = 2 * c + (ln >> 1 & 1);
+            const uint2 v0 = lds_column4(vrow + ((ch ^ f) << 4)), v1 = lds_column4(vrow + 16 * RB + ((ch ^ g) << 4));
+            const u32x4 vf = u32x4{v0.x, v0.y, v1.x, v1.y};
+#pragma unroll
+            for (int q = 0; q < QB; ++q) mma<T>(o[c][q], vf, pf[q]);
+          }
+        }
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < NB; ++j) {
+        const int row = 16 * j + 4 * grp;
+#pragma unroll
+        for (int q = 0; q < QB; ++q) ready(sc[j][q]);
+#pragma unroll
+        for (int c = 0; c < CB; ++c) {
+          u32x4 vf;
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            vf[r] = *reinterpret_cast<const unsigned*>(vs + (row + r) * RB +
+                                                       (((c * 4 + (ln >> 2)) ^ vswz(kw * TK + row + r)) << 4) + (ln & 3) * 4);
+#pragma unroll
+          for (int q = 0; q < QB; ++q) mma<T>(o[c][q], vf, __builtin_bit_cast(u32x4, sc[j][q]));
+        }
+      }
+    }
+  };
+
+  if (k0 < k1) {
+    int ids = PAGED ? pages_of(k0) : 0, ids1 = 0;
+    issue(k0, ids, 0);
+    if constexpr (PAGED) ids1 = pages_of(k0 + BK);
+    int stage = 0;
+    for (int t = k0; t < k1; t += BK, stage ^= 1) {
+      // (the barrier's wait: this tile's loads are done)
+      bool part_tile = t + BK > real_end;
+      if constexpr (PAGED) part_tile = part_tile || (__ballot(ids < 0) & ((1ull << (BK / 16)) - 1));
+      if (part_tile) {
+        loads_done();
+        clear(t, ids, stage);
+      }
+      __syncthreads();
+      int ids2 = 0;
+      if (t + BK < k1) {
+        issue(t + BK, ids1, stage ^ 1);
+        if constexpr (PAGED) ids2 = pages_of(t + 2 * BK);
+      }
+      compute(t, ids, stage);
+      ids = ids1;
+      ids1 = ids2;
+    }
+  }
+  settle<CB * QB>(&o[0][0]);
+  settle<QB>(ls);
+#pragma unroll
+  for (int q = 0; q < QB; ++q) {
+    if constexpr (EB == 2) {
+      l[q] = ls[q][0];                        // (every element of a lane is its row's sum)
+    } else {
+      l[q] += __shfl_xor(l[q], 16, kWave);
+      l[q] += __shfl_xor(l[q], 32, kWave);
+    }
+  }
+
+  // Where a row came out as no number, its wave's rows are formed again key by key, so that a key or
+  // value that is none (or a product that overflows) reaches the rows that see it and no others.
+  {
+    float bad = 0.f;
+#pragma unroll
+    for (int q = 0; q < QB; ++q) {
+      float x = l[q] * 0.f;
+#pragma unroll
+      for (int c = 0; c < CB; ++c)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) x = fmaf(o[c][q][r], 0.f, x);
+      if (live[q]) bad += x;
+    }
+    if (__ballot(bad != 0.f)) {
+#pragma unroll
+      for (int q = 0; q < QB; ++q) {
+        m[q] = -INFINITY;
+        l[q] = 0.f;
+#pragma unroll
+        for (int c = 0; c < CB; ++c) o[c][q] = floatx4{0.f, 0.f, 0.f, 0.f};
+      }
+#pragma unroll 1
+      for (int t = k0; t < k1; t += BK) {
+#pragma unroll 1
+        for (int key = t + kw * TK; key < min(t + (kw + 1) * TK, k1); ++key) {
+          const char *kp, *vp;
+          if constexpr (PAGED) {
+            const int id = table[min(key >> sh, a.c.max_pages - 1)];
+            if ((unsigned)id >= (unsigned)a.c.n_pages) continue;
+            const size_t at = (size_t)id * page_bytes + (size_t)(key & (slots - 1)) * RB;
+            kp = Kp + at;
+            vp = Vp + at;
+          } else {
+            kp = Kp + (size_t)key * ldb;
+            vp = Vp + (size_t)key * ldb;
+          }
+#pragma unroll
+          for (int q = 0; q < QB; ++q) {
+            if (!__ballot(sees(q, key))) continue;
+            float s = 0.f;
+#pragma unroll 1
+            for (int c = 0; c < CB; ++c) {
+              float x[4], y[4];
+              four_values<KV>(kp + (c * 16 + 4 * grp) * EC, x);
+              four_values<T>(qrow[q] + (c * 16 + 4 * grp) * EB, y);
+#pragma unroll
+              for (int r = 0; r < 4; ++r) s = fmaf(x[r], y[r], s);
+            }
+            s += __shfl_xor(s, 16, kWave);
+            s += __shfl_xor(s, 32, kWave);
+            s *= a.scale_signed;
+            if (sees(q, key)) {
+              const float mn = fmaxf(m[q], s), ref = mn == -INFINITY ? 0.f : mn;
+              const float alpha = __builtin_amdgcn_exp2f(m[q] - ref), p = __builtin_amdgcn_exp2f(s - ref);
+              m[q] = mn;
+              l[q] = l[q] * alpha + p;
+#pragma unroll
+              for (int c = 0; c < CB; ++c) {
+                float v[4];
+                four_values<KV>(vp + (c * 16 + 4 * grp) * EC, v);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) o[c][q][r] = fmaf(p, v[r], o[c][q][r] * alpha);
+              }
+            }
+          }
+        }
+      }
+      // to the scale of the others
+      if constexpr (PSH != 0.f) {
+        const float up = __builtin_amdgcn_exp2f(PSH);
+#pragma unroll
+        for (int q = 0; q < QB; ++q) {
+          l[q] *= up;
+#pragma unroll
+          for (int c = 0; c < CB; ++c) o[c][q] *= up;
+        }
+      }
+    }
+  }
+
+  // ---- the rows' outputs ----
+  auto out_row = [&](int r) -> T* {           // of the workgroup's row r
+    if constexpr (PAGED) {
+      const int i = (r0 + r) / a.group, h = hk * a.group + (r0 + r) - i * a.group;
+      return static_cast<T*>(a.out) + (size_t)(row_first + i) * a.out_ld + (size_t)h * DH;
+    } else {
+      return static_cast<T*>(a.out) + (size_t)(r0 + r) * a.out_ld + (size_t)head * DH;
+    }
+  };
+  auto part_row = [&](int r) -> size_t {
+    const int i = (r0 + r) / a.group, h = hk * a.group + (r0 + r) - i * a.group;
+    return ((size_t)part * a.n_rows + row_first + i) * a.n_heads + h;
+  };
+  auto store4 = [&](int r, int x, floatx4 s, float inv) {
+    alignas(16) T t4[4] = {from_f32<T>(s.x * inv), from_f32<T>(s.y * inv), from_f32<T>(s.z * inv), from_f32<T>(s.w * inv)};
+    T* p = out_row(r) + x;
+    if constexpr (EB == 2) *reinterpret_cast<uint2*>(p) = *reinterpret_cast<const uint2*>(t4);
+    else *reinterpret_cast<uint4*>(p) = *reinterpret_cast<const uint4*>(t4);
+  };
+  if constexpr (KW == 1) {
+#pragma unroll
+    for (int q = 0; q < QB; ++q) {
+      const int r = (rw * QB + q) * 16 + ln;
+      if (!live[q]) continue;
+      if (!PAGED || a.parts == 1) {
+        const float inv = l[q] == 0.f ? 0.f : 1.0f / l[q];
+#pragma unroll
+        for (int c = 0; c < CB; ++c) store4(r, c * 16 + 4 * grp, o[c][q], inv);
+      } else {
+        const size_t pr = part_row(r);
+#pragma unroll
+        for (int c = 0; c < CB; ++c) *reinterpret_cast<floatx4*>(a.part_o + pr * DH + c * 16 + 4 * grp) = o[c][q];
+        if (grp == 0) *reinterpret_cast<float2*>(a.part_ml + pr * 2) = make_float2(m[q], l[q]);
+      }
+    }
+  } else {
+    __syncthreads();                          // the tiles' LDS is free
+    float* jo = reinterpret_cast<float*>(lds);
+#pragma unroll
+    for (int q = 0; q < QB; ++q) {
+      if (grp == 0) {
+        jm[wave][q * 16 + ln] = m[q];
+        jl[wave][q * 16 + ln] = l[q];
+        if (kw == 0) jlive[(rw * QB + q) * 16 + ln] = live[q];
+      }
+#pragma unroll
+      for (int c = 0; c < CB; ++c)
+        *reinterpret_cast<floatx4*>(jo + ((wave * QB + q) * 16 + ln) * DH + (((c * 4 + grp) ^ (ln & 7)) << 2)) = o[c][q];
+    }
+    __syncthreads();
+    for (int e = threadIdx.x; e < BM * (DH / 4); e += 64 * W) {
+      const int r = e / (DH / 4), x = e % (DH / 4);
+      const int w0 = r / (QB * 16) * KW, i = r % (QB * 16);
+      if (!jlive[r]) continue;
+      float mm = jm[w0][i];
+#pragma unroll
+      for (int w = 1; w < KW; ++w) mm = fmaxf(mm, jm[w0 + w][i]);
+      const float ref = mm == -INFINITY ? 0.f : mm;
+      float z = 0.f;
+      floatx4 s = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int w = 0; w < KW; ++w) {
+        const float f = __builtin_amdgcn_exp2f(jm[w0 + w][i] - ref);
+        z += f * jl[w0 + w][i];
+        s += f * *reinterpret_cast<const floatx4*>(jo + ((w0 + w) * QB * 16 + i) * DH + ((x ^ (i & 7)) << 2));
+      }
+      if (!PAGED || a.parts == 1) {
+        store4(r, x * 4, s, z == 0.f ? 0.f : 1.0f / z);
+      } else {
+        const size_t pr = part_row(r);
+        *reinterpret_cast<floatx4*>(a.part_o + pr * DH + x * 4) = s;
+        if (x == 0) *reinterpret_cast<float2*>(a.part_ml + pr * 2) = make_float2(mm, z);
+      }
+    }
+  }
+}
+// Merges the parts of a (new row, head): a wave, DH / 4 lanes four channels each of every
+// (256 / DH)-th part, U parts' loads in flight.
+template <typename T, int DH>
+__global__ __launch_bounds__(256) void rows_join_kernel(RowsAttnArgs a) {
+  constexpr int COLS = DH / 4, ROWS = kWave / COLS, U = 8;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
+  const long long item = (long long)blockIdx.x * 4 + wave;
+  const int row = (int)(item / a.n_heads), h = (int)(item - (long long)row * a.n_heads);
+  if (row >= a.n_rows) return;
+  int b = row;
+  if (a.off) {
+    b = __builtin_amdgcn_readfirstlane(sequence_of(a.off, a.n_seqs, row, lane));
+    if (b >= a.n_seqs) return;                  // a row of no sequence
+    const int first = max(a.off[b], 0);
+    if (row < first || row - first >= a.max_new) return;
+  }
+  const int len = max(0, min(a.lens[b], a.max_len));
+  const int n = max(1, (len + a.chunk - 1) / a.chunk);   // (part 0 is written for an empty row too)
+  const size_t stride = (size_t)a.n_rows * a.n_heads;
+  const int p0 = lane / COLS, x = lane % COLS * 4;
+  const float* ml = a.part_ml + (size_t)item * 2;
+  const float* po = a.part_o + (size_t)item * DH + x;
+  floatx4 s = floatx4{0.f, 0.f, 0.f, 0.f};
+  float m = -INFINITY, l = 0.f;
+  for (int p = p0; p < n; p += ROWS * U) {
+    float2 w[U];
+    floatx4 v[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const size_t at = min(p + u * ROWS, n - 1);
+      w[u] = *reinterpret_cast<const float2*>(ml + at * stride * 2);
+      v[u] = *reinterpret_cast<const floatx4*>(po + at * stride * DH);
+    }
+    float mn = m;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (p + u * ROWS >= n) w[u] = make_float2(-INFINITY, 0.f);
+      mn = fmaxf(mn, w[u].x);
+    }
+    const float ref = mn == -INFINITY ? 0.f : mn, f0 = __builtin_amdgcn_exp2f(m - ref);
+    l *= f0;
+    s *= f0;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const float f = __builtin_amdgcn_exp2f(w[u].x - ref);
+      l += f * w[u].y;
+      if (p + u * ROWS < n) s += f * v[u];      // (a part past the last is the last one's again)
+    }
+    m = mn;
+  }
+#pragma unroll
+  for (int d = COLS; d < kWave; d *= 2) {
+    const float mo = __shfl_xor(m, d, kWave), lo = __shfl_xor(l, d, kWave);
+    const float mn = fmaxf(m, mo), ref = mn == -INFINITY ? 0.f : mn;
+    const float f = __builtin_amdgcn_exp2f(m - ref), g = __builtin_amdgcn_exp2f(mo - ref);
+    l = l * f + lo * g;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) s[r] = s[r] * f + __shfl_xor(s[r], d, kWave) * g;
+    m = mn;
+  }
+  if (lane >= COLS) return;
+  const float inv = l == 0.f ? 0.f : 1.0f / l;
+  alignas(16) T t4[4] = {from_f32<T>(s.x * inv), from_f32<T>(s.y * inv), from_f32<T>(s.z * inv), from_f32<T>(s.w * inv)};
+  T* out = static_cast<T*>(a.out) + (size_t)row * a.out_ld + (size_t)h * DH + x;
+  if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(out) = *reinterpret_cast<const uint2*>(t4);
+  else *reinterpret_cast<uint4*>(out) = *reinterpret_cast<const uint4*>(t4);
+}
+
+// ---- launches ----------------------------------------------------------------------------
+// Keys of a wave's share of a tile, by what 160 KB of LDS hold twice over; a load of each wave at least.
+template <typename T, int DH, typename KV, int KW>
+constexpr int rows_keys() {
+  return sizeof(T) == 4 ? (KW == 1 ? 32 : 16) : KW > 1 ? 32 : DH * sizeof(KV) == 32 ? 128 : 64;
+}
+
+template <typename T, int DH, typename KV, bool PAGED, int QB, int RW, int KW>
+hipError_t rows_launch(const RowsAttnArgs& a, unsigned grid, hipStream_t s) {
+  NT_LAUNCH((attn_rows_kernel<T, DH, KV, PAGED, QB, RW, KW, rows_keys<T, DH, KV, KW>()>), dim3(grid), dim3(64 * RW * KW), 0, s, a);
+  return hipGetLastError();
+}
+
+template <typename T, int DH, typename KV, bool PAGED>
+hipError_t rows_tile(const RowsAttnArgs& a, hipStream_t s) {
+  const unsigned grid = PAGED ? ((unsigned)(a.n_seqs * a.c.n_kv_heads * a.parts) + 7) / 8 * 8 * a.rblocks
+                              : (unsigned)(a.rblocks * a.n_heads);
+  switch (a.tile) {
+    case ROWS_128: return rows_launch<T, DH, KV, PAGED, 2, 4, 1>(a, grid, s);
+    case ROWS_32: return rows_launch<T, DH, KV, PAGED, 2, 1, 4>(a, grid, s);
+    case ROWS_16: return rows_launch<T, DH, KV, PAGED, 1, 1, 4>(a, grid, s);
+    default: return hipErrorInvalidValue;
+  }
+}
+
+template <typename T, typename KV, bool PAGED>
+hipError_t rows_head(const RowsAttnArgs& a, hipStream_t s) {
+  hipError_t e;
+  switch (a.c.d_head) {
+    case 32: e = rows_tile<T, 32, KV, PAGED>(a, s); break;
+    case 64: e = rows_tile<T, 64, KV, PAGED>(a, s); break;
+    case 128: e = rows_tile<T, 128, KV, PAGED>(a, s); break;
+    default: return hipErrorInvalidValue;
+  }
+  if (!PAGED || e != hipSuccess || a.parts == 1) return e;
+  const dim3 grid((unsigned)(((long long)a.n_rows * a.n_heads + 3) / 4));
+  switch (a.c.d_head) {
+    case 32: NT_LAUNCH((rows_join_kernel<T, 32>), grid, dim3(256), 0, s, a); break;
+    case 64: NT_LAUNCH((rows_join_kernel<T, 64>), grid, dim3(256), 0, s, a); break;
+    case 128: NT_LAUNCH((rows_join_kernel<T, 128>), grid, dim3(256), 0, s, a); break;
+  }
+  return hipGetLastError();
+}
+}  // namespace
+}  // namespace nt

@@ -288,6 +288,32 @@ struct KvAppendArgs {
 };
 hipError_t kv_append(const KvAppendArgs& a, hipStream_t s);
 
+// Pages for growing and shrinking sequences, drafted tokens that stay (nt_pages.hip).
+enum ResizeStatus : int { RESIZE_TABLE = -1, RESIZE_ROWS = -2 };   // include/nt.h: NT_RESIZE_*
+struct KvResizeArgs {
+  int page_shift, n_pages, max_pages;
+  int* table;                 // [n_seqs][max_pages]
+  int* lens;                  // [n_seqs]
+  const int* add;             // [n_seqs]
+  int n_seqs;
+  int* ring;                  // [n_pages]
+  int* state;                 // head, count, status, rows
+  int* off;                   // [n_seqs + 1] or null
+  int* pos;                   // [rows] or null
+  long long* slot;            // [rows] or null
+  int rows;                   // -1: neither pos nor slot
+  int seqs;                   // sequences of a column of workgroups; set by kv_resize
+};
+hipError_t kv_resize(const KvResizeArgs& a, hipStream_t s);
+struct KvKeepArgs {
+  PagedCache c;
+  int eb;                     // bytes of the pools' elements
+  const int *off, *lens, *path, *n_path;   // [n_seqs + 1], [n_seqs], [n_seqs][max_path], [n_seqs]
+  int max_path, n_seqs;
+  int* add;                   // [n_seqs]
+};
+hipError_t kv_keep(const KvKeepArgs& a, hipStream_t s);
+
 struct PagedAttnArgs {
   PagedCache c;
   const void* q;              // sequence b's row at + b * q_ld, head h at + h * d_head
@@ -306,6 +332,45 @@ struct PagedAttnArgs {
 // Fills the cut from c, n_seqs, n_heads and max_len.  Host only.
 void paged_attn_plan(PagedAttnArgs* a);
 hipError_t paged_attn(const PagedAttnArgs& a, hipStream_t s);
+
+// ---------------------------------------------------------------------------------
+// Attention of many query rows (nt_attn_rows.h, nt_rows.hip): packed prompts, and several new
+// tokens a sequence over a paged cache.
+enum RowsTile : int { ROWS_16 = 0, ROWS_32 = 1, ROWS_128 = 2 };   // query rows of a workgroup
+struct RowsAttnArgs {
+  PagedCache c;               // (prompts: dt, n_kv_heads and d_head only)
+  const void* q;              // row i at + i * q_ld, head h at + h * d_head
+  int q_ld;
+  const void *k, *v;          // prompts: rows kv_ld apart
+  int kv_ld;
+  const int* off;             // [n_seqs + 1] first row of each sequence (tree, null: row b is b's)
+  const int* lens;            // tree: [n_seqs], new tokens counted
+  const unsigned long long* mask;   // tree: [n_rows], or null: each row sees those before it
+  void* out;                  // like q, rows out_ld apart
+  int out_ld;
+  int n_seqs, n_rows, n_heads, group;   // group: query heads of a key head
+  int max_new, max_len, causal;
+  // |scale| log2(e), and what the queries' words are masked and xored with for the rest of it;
+  // scale log2(e) itself
+  float scale_log2, scale_signed;
+  unsigned q_and, q_xor;
+  // the call's cut (attn_prompt_plan, attn_tree_plan): a RowsTile; blocks of query rows (a key
+  // head's, or the packed rows'); parts of `chunk` keys
+  int tile, rblocks, parts, chunk;
+  float* part_o;              // parts > 1: [parts][n_rows][n_heads][d_head] and (max, sum) of each
+  float* part_ml;
+};
+// Fill the cut from the sizes.  Host only.
+void attn_prompt_plan(RowsAttnArgs* a);
+void attn_tree_plan(RowsAttnArgs* a);
+hipError_t attn_prompt(const RowsAttnArgs& a, hipStream_t s);
+hipError_t attn_tree(const RowsAttnArgs& a, hipStream_t s);
+hipError_t attn_prompt_f16(const RowsAttnArgs& a, hipStream_t s);
+hipError_t attn_prompt_bf16(const RowsAttnArgs& a, hipStream_t s);
+hipError_t attn_prompt_f32(const RowsAttnArgs& a, hipStream_t s);
+hipError_t attn_tree_f16(const RowsAttnArgs& a, hipStream_t s);
+hipError_t attn_tree_bf16(const RowsAttnArgs& a, hipStream_t s);
+hipError_t attn_tree_f32(const RowsAttnArgs& a, hipStream_t s);
 
 // ---------------------------------------------------------------------------------
 // Log-probabilities, entropy and best alternatives of rows of logits (nt_score.hip).

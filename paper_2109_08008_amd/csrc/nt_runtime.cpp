@@ -1320,6 +1320,44 @@ nt_status paged_attn_cut(int n_heads, int n_seqs, int max_len, nt::PagedAttnArgs
   return NT_OK;
 }
 
+// Heads and scale of attention of many query rows.
+nt_status rows_attn_heads(int n_heads, float scale, nt::RowsAttnArgs* a) {
+  if (n_heads < 1 || n_heads > 65536 || n_heads % a->c.n_kv_heads)
+    return fail(NT_E_INVALID, "n_heads must be a positive multiple of n_kv_heads");
+  if (!std::isfinite(scale * 1.4426950408889634f)) return fail(NT_E_INVALID, "scale * log2(e) must be finite");
+  a->n_heads = n_heads;
+  a->group = n_heads / a->c.n_kv_heads;
+  // the kernels take |scale|: a negative one turns the queries' signs, 0 (or one that is no normal
+  // number) makes them zero
+  const bool none = !std::isnormal(scale * 1.4426950408889634f);
+  a->scale_signed = none ? 0.f : scale * 1.4426950408889634f;
+  a->scale_log2 = none ? 1.f : std::fabs(a->scale_signed);
+  a->q_and = none ? 0u : ~0u;
+  a->q_xor = !none && scale < 0.f ? (a->c.dt == DT::F32 ? 0x80000000u : 0x80008000u) : 0u;
+  return NT_OK;
+}
+
+nt_status attn_tree_cut(int n_heads, int n_seqs, int n_rows, int max_new, int max_len, float scale, nt::RowsAttnArgs* a) {
+  if (n_seqs < 0 || n_rows < 0 || max_new < 0 || max_len < 0)
+    return fail(NT_E_INVALID, "n_seqs, n_rows, max_new and max_len must be >= 0");
+  NT_TRY(rows_attn_heads(n_heads, scale, a));
+  const long long reach = (long long)a->c.max_pages << a->c.page_shift;
+  a->max_len = (int)std::min<long long>(std::min<long long>(max_len, reach), 1 << 30);
+  a->max_new = std::min(max_new, n_rows);
+  a->n_seqs = n_seqs;
+  a->n_rows = n_rows;
+  // a launch holds less than 2^24 workgroups of 256 threads (and the join has one for four heads' rows)
+  const long long tasks = (long long)n_seqs * a->c.n_kv_heads * (((long long)a->max_new * a->group + 15) / 16 + 1);
+  if (tasks >= 1 << 22 || (long long)n_rows * n_heads >= 1 << 25)
+    return fail(NT_E_UNSUPPORTED, "n_seqs * heads * max_new of one call is more than a launch takes");
+  nt::attn_tree_plan(a);
+  return NT_OK;
+}
+
+size_t tree_ws_bytes(const nt::RowsAttnArgs& a) {
+  return a.parts > 1 ? align_up((size_t)a.parts * a.n_rows * a.n_heads * (a.c.d_head + 2) * sizeof(float)) : 0;
+}
+
 // Operands of a gated projection within the kernels' 32-bit offsets (tiles name up to 256 rows past
 // the last one before they are bounded).
 constexpr size_t kLim32 = (size_t)1 << 32;
@@ -2198,6 +2236,138 @@ nt_status nt_op_attn_paged(const nt_kv_pages* cache, const void* d_q, int32_t q_
   a.part_o = static_cast<float*>(d_ws);
   a.part_ml = a.part_o + (need ? (size_t)a.parts * n_seqs * n_heads * a.c.d_head : 0);
   NT_HIP(nt::paged_attn(a, static_cast<hipStream_t>(stream)));
+  return NT_OK;
+}
+
+nt_status nt_op_attn_prompt(int32_t dtype, const void* d_q, int32_t q_ld, int32_t n_heads, const void* d_k,
+                            const void* d_v, int32_t kv_ld, int32_t n_kv_heads, int32_t d_head, const int32_t* d_off,
+                            int32_t n_seqs, int32_t n_rows, int32_t causal, float scale, void* d_out, int32_t out_ld,
+                            void* stream) {
+  g_err.clear();
+  if (dtype < NT_F32 || dtype > NT_BF16) return fail(NT_E_INVALID, "unknown dtype %d", dtype);
+  if (!d_q || !d_k || !d_v || !d_off || !d_out) return fail(NT_E_INVALID, "null argument to nt_op_attn_prompt");
+  if (d_head != 32 && d_head != 64 && d_head != 128) return fail(NT_E_INVALID, "d_head %d not in {32, 64, 128}", d_head);
+  if (n_kv_heads < 1 || n_kv_heads > 4096) return fail(NT_E_INVALID, "n_kv_heads must be in [1, 4096]");
+  if (n_seqs < 0 || n_rows < 0) return fail(NT_E_INVALID, "n_seqs and n_rows must be >= 0");
+  nt::RowsAttnArgs a{};
+  a.c.dt = static_cast<DT>(dtype);
+  a.c.n_kv_heads = n_kv_heads;
+  a.c.d_head = d_head;
+  NT_TRY(rows_attn_heads(n_heads, scale, &a));
+  NT_TRY(check_rows("d_q", d_q, q_ld, n_heads, a.c));
+  NT_TRY(check_rows("d_k", d_k, kv_ld, n_kv_heads, a.c));
+  NT_TRY(check_rows("d_v", d_v, kv_ld, n_kv_heads, a.c));
+  NT_TRY(check_rows("d_out", d_out, out_ld, n_heads, a.c));
+  a.n_seqs = n_seqs;
+  a.n_rows = n_rows;
+  nt::attn_prompt_plan(&a);
+  if (n_rows > 1 << 30 || n_seqs > 1 << 30 || (long long)a.rblocks * n_heads >= 1 << 23)
+    return fail(NT_E_UNSUPPORTED, "n_rows * n_heads of one call is more than a launch takes");
+  if (n_seqs == 0 || n_rows == 0) return NT_OK;
+  a.q = d_q;
+  a.q_ld = q_ld;
+  a.k = d_k;
+  a.v = d_v;
+  a.kv_ld = kv_ld;
+  a.off = d_off;
+  a.causal = causal != 0;
+  a.out = d_out;
+  a.out_ld = out_ld;
+  NT_HIP(nt::attn_prompt(a, static_cast<hipStream_t>(stream)));
+  return NT_OK;
+}
+
+nt_status nt_op_attn_tree_workspace(const nt_kv_pages* cache, int32_t n_heads, int32_t n_seqs, int32_t n_rows,
+                                    int32_t max_new, int32_t max_len, size_t* bytes) {
+  g_err.clear();
+  if (!bytes) return fail(NT_E_INVALID, "null argument to nt_op_attn_tree_workspace");
+  nt::RowsAttnArgs a{};
+  NT_TRY(paged_cache(cache, false, &a.c));
+  NT_TRY(attn_tree_cut(n_heads, n_seqs, n_rows, max_new, max_len, 1.f, &a));
+  *bytes = tree_ws_bytes(a);
+  return NT_OK;
+}
+
+nt_status nt_op_attn_tree(const nt_kv_pages* cache, const void* d_q, int32_t q_ld, int32_t n_heads,
+                          const int32_t* d_off, const uint64_t* d_mask, const int32_t* d_lens, int32_t n_seqs,
+                          int32_t n_rows, int32_t max_new, int32_t max_len, float scale, void* d_out, int32_t out_ld,
+                          void* d_ws, size_t ws_bytes, void* stream) {
+  g_err.clear();
+  nt::RowsAttnArgs a{};
+  NT_TRY(paged_cache(cache, true, &a.c));
+  if (!d_q || !d_lens || !d_out) return fail(NT_E_INVALID, "null argument to nt_op_attn_tree");
+  NT_TRY(attn_tree_cut(n_heads, n_seqs, n_rows, max_new, max_len, scale, &a));
+  if (!d_off && n_rows != n_seqs) return fail(NT_E_INVALID, "without d_off every sequence has one new row: n_rows == n_seqs");
+  if (d_mask && max_new > 64) return fail(NT_E_UNSUPPORTED, "d_mask holds 64 new tokens: max_new must be at most 64");
+  NT_TRY(check_rows("d_q", d_q, q_ld, n_heads, a.c));
+  NT_TRY(check_rows("d_out", d_out, out_ld, n_heads, a.c));
+  const size_t need = tree_ws_bytes(a);
+  if (need > 0) {
+    if (!d_ws || ws_bytes < need)
+      return fail(NT_E_WORKSPACE, "workspace of %zu bytes required, %zu given", need, d_ws ? ws_bytes : (size_t)0);
+    if (reinterpret_cast<uintptr_t>(d_ws) & 255) return fail(NT_E_INVALID, "workspace must be 256-byte aligned");
+  }
+  if (n_seqs == 0 || n_rows == 0 || a.max_new == 0) return NT_OK;
+  a.q = d_q;
+  a.q_ld = q_ld;
+  a.off = d_off;
+  a.mask = reinterpret_cast<const unsigned long long*>(d_mask);
+  a.lens = d_lens;
+  a.out = d_out;
+  a.out_ld = out_ld;
+  a.part_o = static_cast<float*>(d_ws);
+  a.part_ml = a.part_o + (need ? (size_t)a.parts * n_rows * n_heads * a.c.d_head : 0);
+  NT_HIP(nt::attn_tree(a, static_cast<hipStream_t>(stream)));
+  return NT_OK;
+}
+
+nt_status nt_op_kv_resize(int32_t page_len, int32_t n_pages, int32_t max_pages, int32_t* d_table, int32_t* d_lens,
+                          const int32_t* d_add, int32_t n_seqs, int32_t* d_ring, int32_t* d_state, int32_t* d_off,
+                          int32_t* d_pos, int64_t* d_slot, int32_t max_rows, void* stream) {
+  g_err.clear();
+  if (page_len < 16 || page_len > 256 || (page_len & (page_len - 1)))
+    return fail(NT_E_INVALID, "page_len %d not in {16, 32, 64, 128, 256}", page_len);
+  if (n_pages < 1 || max_pages < 1) return fail(NT_E_INVALID, "n_pages and max_pages must be positive");
+  if (n_seqs < 0 || max_rows < 0) return fail(NT_E_INVALID, "n_seqs and max_rows must be >= 0");
+  if (!d_table || !d_lens || !d_add || !d_ring || !d_state) return fail(NT_E_INVALID, "null argument to nt_op_kv_resize");
+  if (n_seqs > 65536) return fail(NT_E_UNSUPPORTED, "at most 65536 sequences");
+  nt::KvResizeArgs a{};
+  a.page_shift = 4;
+  while ((1 << a.page_shift) < page_len) ++a.page_shift;
+  a.n_pages = n_pages;
+  a.max_pages = max_pages;
+  a.table = d_table;
+  a.lens = d_lens;
+  a.add = d_add;
+  a.n_seqs = n_seqs;
+  a.ring = d_ring;
+  a.state = d_state;
+  a.off = d_off;
+  a.pos = d_pos;
+  a.slot = reinterpret_cast<long long*>(d_slot);
+  a.rows = d_pos || d_slot ? max_rows : -1;
+  NT_HIP(nt::kv_resize(a, static_cast<hipStream_t>(stream)));
+  return NT_OK;
+}
+
+nt_status nt_op_kv_keep(const nt_kv_pages* cache, const int32_t* d_off, const int32_t* d_lens, const int32_t* d_path,
+                        int32_t max_path, const int32_t* d_n_path, int32_t n_seqs, int32_t* d_add, void* stream) {
+  g_err.clear();
+  nt::KvKeepArgs a{};
+  NT_TRY(paged_cache(cache, true, &a.c));
+  if (!d_off || !d_lens || !d_path || !d_n_path || !d_add) return fail(NT_E_INVALID, "null argument to nt_op_kv_keep");
+  if (n_seqs < 0 || max_path < 0) return fail(NT_E_INVALID, "n_seqs and max_path must be >= 0");
+  a.eb = a.c.fp8 ? 1 : (int)nt::dt_bytes(a.c.dt);
+  if ((long long)n_seqs * 2 * a.c.n_kv_heads * (a.c.d_head * a.eb / 16) > 0x7fffffffll)
+    return fail(NT_E_UNSUPPORTED, "more sequences and heads than one launch takes");
+  a.off = d_off;
+  a.lens = d_lens;
+  a.path = d_path;
+  a.n_path = d_n_path;
+  a.max_path = max_path;
+  a.n_seqs = n_seqs;
+  a.add = d_add;
+  NT_HIP(nt::kv_keep(a, static_cast<hipStream_t>(stream)));
   return NT_OK;
 }
 

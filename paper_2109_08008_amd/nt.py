@@ -34,7 +34,9 @@ EXPORTS = [
     "nt_ensemble", "nt_quantize_fp8", "nt_op_kv_append", "nt_op_attn_paged", "nt_op_attn_paged_workspace",
     "nt_op_token_logp", "nt_op_token_logp_workspace",
     "nt_op_gemm_gated", "nt_op_gemm_gated_rows",
+    "nt_op_attn_prompt", "nt_op_attn_tree", "nt_op_attn_tree_workspace", "nt_op_kv_resize", "nt_op_kv_keep",
 ]
+NT_RESIZE_TABLE, NT_RESIZE_ROWS = -1, -2   # include/nt.h: why nt_op_kv_resize did nothing
 NT_ENS_MEAN_LOGP, NT_ENS_LOG_MEAN_P = 0, 1
 GATE_ACTS = {"silu": 0, "gelu": 1, "gelu_tanh": 2, "relu": 3}   # include/nt.h: nt_gate_act
 NT_SELECT_NOALLOC_MAX_RECORDS = 1 << 20   # include/nt.h: records of nt_op_select_tiled_noalloc
@@ -129,6 +131,13 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
                                        c_int32, P, c_size_t, P]),
         "nt_op_attn_paged_workspace": (c_int32, [POINTER(nt_kv_pages), c_int32, c_int32, c_int32,
                                                  POINTER(c_size_t)]),
+        "nt_op_attn_prompt": (c_int32, [c_int32, P, c_int32, c_int32, P, P, c_int32, c_int32, c_int32, P, c_int32,
+                                        c_int32, c_int32, c_float, P, c_int32, P]),
+        "nt_op_attn_tree": (c_int32, [POINTER(nt_kv_pages), P, c_int32, c_int32, P, P, P, c_int32, c_int32, c_int32,
+                                      c_int32, c_float, P, c_int32, P, c_size_t, P]),
+        "nt_op_attn_tree_workspace": (c_int32, [POINTER(nt_kv_pages)] + [c_int32] * 5 + [POINTER(c_size_t)]),
+        "nt_op_kv_resize": (c_int32, [c_int32, c_int32, c_int32, P, P, P, c_int32, P, P, P, P, P, c_int32, P]),
+        "nt_op_kv_keep": (c_int32, [POINTER(nt_kv_pages), P, P, P, c_int32, P, c_int32, P, P]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(L, name)
@@ -384,6 +393,40 @@ def nt_op_attn_paged(cache: nt_kv_pages, d_q: int, q_ld: int, n_heads: int, d_le
                      scale: float, d_out: int, out_ld: int, d_ws=None, ws_bytes: int = 0, stream=None):
     _check(load_library().nt_op_attn_paged(ctypes.byref(cache), d_q, q_ld, n_heads, d_lens, n_seqs, max_len, scale,
                                            d_out, out_ld, d_ws, ws_bytes, _stream(stream)))
+
+
+def nt_op_attn_prompt(dtype: str, d_q: int, q_ld: int, n_heads: int, d_k: int, d_v: int, kv_ld: int, n_kv_heads: int,
+                      d_head: int, d_off: int, n_seqs: int, n_rows: int, causal: bool, scale: float, d_out: int,
+                      out_ld: int, stream=None):
+    _check(load_library().nt_op_attn_prompt(DTYPES[dtype], d_q, q_ld, n_heads, d_k, d_v, kv_ld, n_kv_heads, d_head, d_off,
+                                            n_seqs, n_rows, int(causal), scale, d_out, out_ld, _stream(stream)))
+
+
+def nt_op_attn_tree_workspace(cache: nt_kv_pages, n_heads: int, n_seqs: int, n_rows: int, max_new: int,
+                              max_len: int) -> int:
+    b = c_size_t()
+    _check(load_library().nt_op_attn_tree_workspace(ctypes.byref(cache), n_heads, n_seqs, n_rows, max_new, max_len,
+                                                    ctypes.byref(b)))
+    return b.value
+
+
+def nt_op_attn_tree(cache: nt_kv_pages, d_q: int, q_ld: int, n_heads: int, d_off, d_mask, d_lens: int, n_seqs: int,
+                    n_rows: int, max_new: int, max_len: int, scale: float, d_out: int, out_ld: int, d_ws=None,
+                    ws_bytes: int = 0, stream=None):
+    _check(load_library().nt_op_attn_tree(ctypes.byref(cache), d_q, q_ld, n_heads, d_off, d_mask, d_lens, n_seqs, n_rows,
+                                          max_new, max_len, scale, d_out, out_ld, d_ws, ws_bytes, _stream(stream)))
+
+
+def nt_op_kv_resize(page_len: int, n_pages: int, max_pages: int, d_table: int, d_lens: int, d_add: int, n_seqs: int,
+                    d_ring: int, d_state: int, d_off=None, d_pos=None, d_slot=None, max_rows: int = 0, stream=None):
+    _check(load_library().nt_op_kv_resize(page_len, n_pages, max_pages, d_table, d_lens, d_add, n_seqs, d_ring, d_state,
+                                          d_off, d_pos, d_slot, max_rows, _stream(stream)))
+
+
+def nt_op_kv_keep(cache: nt_kv_pages, d_off: int, d_lens: int, d_path: int, max_path: int, d_n_path: int, n_seqs: int,
+                  d_add: int, stream=None):
+    _check(load_library().nt_op_kv_keep(ctypes.byref(cache), d_off, d_lens, d_path, max_path, d_n_path, n_seqs, d_add,
+                                        _stream(stream)))
 
 
 def nt_prof_enable(mask: int):

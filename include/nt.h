@@ -558,7 +558,8 @@ nt_status nt_op_attn_tree_workspace(const nt_kv_pages* cache, int32_t n_heads, i
  *   page * page_len + position % page_len of it, the page being the table's; -1 for rows of none.
  * All or nothing: where d_state[2] is not 0 lengths, table and ring stay as they were, d_off is all 0
  * and d_pos and d_slot all -1.  It is the number of pages that the ring lacks, NT_RESIZE_TABLE if a
- * sequence would pass its row of the table (or 2^31 - 1), or NT_RESIZE_ROWS if there are more new
+ * sequence would pass its row of the table (or 2^31 - 1) or the lengths and the ring do not match (more
+ * pages given up than the ring has room for), or NT_RESIZE_ROWS if there are more new
  * rows than max_rows (with neither d_pos nor d_slot: than 2^31 - 1).
  * Buffers overlap nowhere.  Asynchronous, one or two launches, no workspace, on the current device; a
  * ring and its lengths are one call's at a time.  NT_E_INVALID for a null pointer, a page_len that
@@ -579,7 +580,7 @@ nt_status nt_op_kv_resize(int32_t page_len, int32_t n_pages, int32_t max_pages, 
  * ends there.  Every other cell of the pools stays as it is.  Pages that two sequences share:
  * as for nt_op_kv_append.  Asynchronous, one launch, on the current device.  NT_E_INVALID for a null
  * pointer, a negative size or a shape the struct does not allow; NT_E_UNSUPPORTED for fp8 with
- * another dtype than NT_F16 or more than 2^31 pieces of 16 bytes in a row of all sequences. */
+ * another dtype than NT_F16 or more than 2^31 bytes of keys and values in a position of all sequences. */
 nt_status nt_op_kv_keep(const nt_kv_pages* cache, const int32_t* d_off, const int32_t* d_lens, const int32_t* d_path,
                         int32_t max_path, const int32_t* d_n_path, int32_t n_seqs, int32_t* d_add, void* stream);
 

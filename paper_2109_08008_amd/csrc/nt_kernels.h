@@ -311,6 +311,7 @@ struct KvKeepArgs {
   const int *off, *lens, *path, *n_path;   // [n_seqs + 1], [n_seqs], [n_seqs][max_path], [n_seqs]
   int max_path, n_seqs;
   int* add;                   // [n_seqs]
+  int waves;                  // of a sequence; set by kv_keep
 };
 hipError_t kv_keep(const KvKeepArgs& a, hipStream_t s);
 

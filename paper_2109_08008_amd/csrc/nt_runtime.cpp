@@ -2358,7 +2358,8 @@ nt_status nt_op_kv_keep(const nt_kv_pages* cache, const int32_t* d_off, const in
   if (!d_off || !d_lens || !d_path || !d_n_path || !d_add) return fail(NT_E_INVALID, "null argument to nt_op_kv_keep");
   if (n_seqs < 0 || max_path < 0) return fail(NT_E_INVALID, "n_seqs and max_path must be >= 0");
   a.eb = a.c.fp8 ? 1 : (int)nt::dt_bytes(a.c.dt);
-  if ((long long)n_seqs * 2 * a.c.n_kv_heads * (a.c.d_head * a.eb / 16) > 0x7fffffffll)
+  // a launch holds less than 2^24 workgroups of 256 threads: a wave for 64 16-byte pieces
+  if ((long long)n_seqs * ((2ll * a.c.n_kv_heads * (a.c.d_head * a.eb / 16) + 63) / 64) >= 1 << 25)
     return fail(NT_E_UNSUPPORTED, "more sequences and heads than one launch takes");
   a.off = d_off;
   a.lens = d_lens;

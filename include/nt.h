@@ -511,7 +511,8 @@ nt_status nt_op_attn_paged_workspace(const nt_kv_pages* cache, int32_t n_heads, 
  * rounding).  d_head in {32, 64, 128}.  out overlaps no input.  Asynchronous, one launch, no workspace,
  * on the current device.  NT_E_INVALID for a null pointer, a negative size, a d_head or heads that
  * are not allowed, rows shorter than their heads or not 16-byte aligned, or a scale whose product with
- * log2(e) is not finite (one below 2^-126 counts as 0); NT_E_UNSUPPORTED for more work than one launch takes (2^23 workgroups). */
+ * log2(e) is not finite (one below 2^-126 counts as 0); NT_E_UNSUPPORTED for rows of
+ * keys more than 16 MiB apart or more work than one launch takes (2^23 workgroups). */
 nt_status nt_op_attn_prompt(int32_t dtype, const void* d_q, int32_t q_ld, int32_t n_heads, const void* d_k,
                             const void* d_v, int32_t kv_ld, int32_t n_kv_heads, int32_t d_head, const int32_t* d_off,
                             int32_t n_seqs, int32_t n_rows, int32_t causal, float scale, void* d_out, int32_t out_ld,

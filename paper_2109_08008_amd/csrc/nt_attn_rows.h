@@ -104,9 +104,14 @@ constexpr float p_shift() {
   return std::is_same<T, f16>::value ? 7.f : 0.f;
 }
 
-// 16 bytes a lane, 1024 consecutive ones of LDS from dst on.
-__device__ __forceinline__ void load_to_lds(const char* src, unsigned char* dst) {
-  __builtin_amdgcn_global_load_lds(src, NT_LDS(dst), 16, 0, 0);
+// 16 bytes a lane, 1024 consecutive ones of LDS from dst on.  The compiler does not see the load: it
+// would wait for all of them before the next read of LDS, whatever that reads.
+__device__ __forceinline__ void load_to_lds(const char* base, unsigned at, unsigned dst) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(at), "s"(base), "s"(dst)
+               : "memory", "m0");
+}
+__device__ __forceinline__ void load_to_lds(const char* src, unsigned dst) {
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(src), "s"(dst) : "memory", "m0");
 }
 // Waits for the wave's loads, those into LDS among them.
 __device__ __forceinline__ void loads_done() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
@@ -282,24 +287,48 @@ __global__ __launch_bounds__(64 * RW * KW) __attribute__((amdgpu_waves_per_eu(2)
     }
     return id;
   };
-  auto issue = [&](int t, int ids, int stage) {
-    unsigned char* dst = lds + stage * STAGE + wave * 1024;
+  const unsigned lds0 = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)NT_LDS(lds) + wave * 1024);
+  // A lane's places in the rows that its loads cover (of a page's 16 keys, or of the tile): constant, so
+  // that a load takes a scalar base and no vector instruction.
+  constexpr bool UNIFORM = !PAGED || RPL <= 16;         // a load's rows are on one page
+  unsigned kat[UNIFORM ? NP : 1], vat[UNIFORM ? NP : 1];
+  if constexpr (UNIFORM) {
 #pragma unroll
     for (int u = 0; u < NP; ++u) {
       const int row = (u * W + wave) * RPL + lane / CH, ch = lane % CH;
-      const char *ks, *vs;
-      if constexpr (PAGED) {
-        const int id = RPL <= 16 ? __builtin_amdgcn_readlane(ids, (u * W + wave) * RPL / 16) : __shfl(ids, row / 16, kWave);
-        const size_t at = (size_t)max(id, 0) * page_bytes + (size_t)((t + row) & (slots - 1)) * RB;
-        ks = Kp + at;
-        vs = Vp + at;
-      } else {
-        const size_t at = (size_t)min(t + row, k1 - 1) * ldb;
-        ks = Kp + at;
-        vs = Vp + at;
+      const unsigned at = PAGED ? (row & 15) * RB : row * (unsigned)ldb;
+      kat[u] = at + ((ch ^ kswz(row)) << 4);
+      vat[u] = at + ((ch ^ vswz(row)) << 4);
+    }
+  }
+  auto issue = [&](int t, int ids, int stage) {
+    const unsigned dst = lds0 + stage * STAGE;
+    if constexpr (PAGED && UNIFORM) {
+#pragma unroll
+      for (int u = 0; u < NP; ++u) {
+        const int block = (u * W + wave) * RPL / 16;
+        const int id = __builtin_amdgcn_readlane(ids, block);
+        const size_t at = (size_t)max(id, 0) * page_bytes + (size_t)((t + block * 16) & (slots - 1)) * RB;
+        load_to_lds(Kp + at, kat[u], dst + u * W * 1024);
+        load_to_lds(Vp + at, vat[u], dst + TILE + u * W * 1024);
       }
-      load_to_lds(ks + ((ch ^ kswz(row)) << 4), dst + u * W * 1024);
-      load_to_lds(vs + ((ch ^ vswz(row)) << 4), dst + TILE + u * W * 1024);
+    } else if (!PAGED && t + BK <= k1) {
+      const char *ks = Kp + t * ldb, *vs = Vp + t * ldb;
+#pragma unroll
+      for (int u = 0; u < NP; ++u) {
+        load_to_lds(ks, kat[u], dst + u * W * 1024);
+        load_to_lds(vs, vat[u], dst + TILE + u * W * 1024);
+      }
+    } else {                                            // rows past the last: that one again
+#pragma unroll
+      for (int u = 0; u < NP; ++u) {
+        const int row = (u * W + wave) * RPL + lane / CH, ch = lane % CH;
+        size_t at;
+        if constexpr (PAGED) at = (size_t)max(__shfl(ids, row / 16, kWave), 0) * page_bytes + (size_t)((t + row) & (slots - 1)) * RB;
+        else at = (size_t)min(t + row, k1 - 1) * ldb;
+        load_to_lds(Kp + at + ((ch ^ kswz(row)) << 4), dst + u * W * 1024);
+        load_to_lds(Vp + at + ((ch ^ vswz(row)) << 4), dst + TILE + u * W * 1024);
+      }
     }
   };
   // What lies behind the last key, or on no page, may be anything: its values become zeros (no 0 * NaN).
@@ -346,43 +375,74 @@ __global__ __launch_bounds__(64 * RW * KW) __attribute__((amdgpu_waves_per_eu(2)
     if (t0 >= min(hi_last, k1) || t0 + TK <= lo_first) return;
     const unsigned char* ks = lds + stage * STAGE + kw * TK * RB;
     const unsigned char* vs = ks + TILE;
+    // Scores: a block's keys are read while the one before is multiplied.
+    constexpr int KR = F8 ? (QK + 1) / 2 : QK;          // 16-byte reads of a lane
     floatx4 sc[NB][QB];
-#pragma unroll
-    for (int j = 0; j < NB; ++j) {
+    u32x4 kr[2][KR];
+    auto read_k = [&](int j, u32x4 (&x)[KR]) {
       const int row = 16 * j + ln, f = kswz(kw * TK + row);
       const unsigned char* krow = ks + row * RB;
-      if constexpr (F8 && DH >= 64) {
-#pragma unroll
-        for (int p = 0; p < QK / 2; ++p) {
-          const u32x4 w = *reinterpret_cast<const u32x4*>(krow + (((p * 4 + grp) ^ f) << 4));
-          u32x4 x = f8_to_f16x8(w.x, w.y), y = f8_to_f16x8(w.z, w.w);
-          ready(x, y);
-#pragma unroll
-          for (int q = 0; q < QB; ++q) {
-            if (p == 0) mma0<T>(sc[j][q], x, qf[q][0]);
-            else mma<T>(sc[j][q], x, qf[q][2 * p]);
-            mma<T>(sc[j][q], y, qf[q][2 * p + 1]);
-          }
-        }
+      if constexpr (F8 && DH == 32) {
+        const uint2 w = *reinterpret_cast<const uint2*>(krow + (((grp >> 1) ^ f) << 4) + (grp & 1) * 8);
+        x[0] = u32x4{w.x, w.y, 0, 0};
       } else {
 #pragma unroll
-        for (int st = 0; st < QK; ++st) {
-          u32x4 kf;
-          if constexpr (F8) {
-            const uint2 w = *reinterpret_cast<const uint2*>(krow + (((grp >> 1) ^ f) << 4) + (grp & 1) * 8);
-            kf = f8_to_f16x8(w.x, w.y);
-            ready(kf);
-          } else {
-            kf = *reinterpret_cast<const u32x4*>(krow + (((st * 4 + grp) ^ f) << 4));
-          }
+        for (int i = 0; i < KR; ++i) x[i] = *reinterpret_cast<const u32x4*>(krow + (((i * 4 + grp) ^ f) << 4));
+      }
+    };
+    read_k(0, kr[0]);
 #pragma unroll
-          for (int q = 0; q < QB; ++q) {
-            if (st == 0) mma0<T>(sc[j][q], kf, qf[q][0]);
-            else mma<T>(sc[j][q], kf, qf[q][st]);
-          }
+    for (int j = 0; j < NB; ++j) {
+      if (j + 1 < NB) read_k(j + 1, kr[(j + 1) & 1]);
+      __builtin_amdgcn_sched_barrier(0);
+      const u32x4* x = kr[j & 1];
+#pragma unroll
+      for (int st = 0; st < QK; ++st) {
+        u32x4 kf;
+        if constexpr (F8) {
+          kf = st % 2 ? f8_to_f16x8(x[st / 2].z, x[st / 2].w) : f8_to_f16x8(x[st / 2].x, x[st / 2].y);
+          ready(kf);
+        } else {
+          kf = x[st];
+        }
+#pragma unroll
+        for (int q = 0; q < QB; ++q) {
+          if (st == 0) mma0<T>(sc[j][q], kf, qf[q][0]);
+          else mma<T>(sc[j][q], kf, qf[q][st]);
         }
       }
     }
+    // Values: VC channel blocks of 32 keys a group, read a group ahead; the first during the softmax.
+    constexpr int VC = EB == 2 ? (CB < 4 ? CB : 4) : 1, VG = NB / (EB == 2 ? 2 : 1) * (CB / VC);
+    u32x4 vr[2][VC];
+    auto read_v = [&](int g, u32x4 (&x)[VC]) {
+      const int j = g / (CB / VC) * (EB == 2 ? 2 : 1), c0 = g % (CB / VC) * VC;
+      if constexpr (EB == 4) {
+        const int row = 16 * j + 4 * grp;
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          x[0][r] = *reinterpret_cast<const unsigned*>(vs + (row + r) * RB +
+                                                      (((c0 * 4 + (ln >> 2)) ^ vswz(kw * TK + row + r)) << 4) + (ln & 3) * 4);
+      } else if constexpr (F8) {
+        const int row = 16 * (j + (ln >> 3)) + 4 * grp + (ln >> 1 & 3), f = vswz(kw * TK + row);
+        const unsigned char* vrow = vs + row * RB + (ln & 1) * 8;
+#pragma unroll
+        for (int c = 0; c < VC; ++c) {
+          const uint2 w = lds_column8(vrow + (((c0 + c) ^ f) << 4));
+          x[c] = u32x4{w.x, w.y, 0, 0};
+        }
+      } else {
+        const int row = 16 * j + 4 * grp + (ln >> 2), f = vswz(kw * TK + row), h = vswz(kw * TK + row + 16);
+        const unsigned char* vrow = vs + row * RB + (ln & 1) * 8;
+#pragma unroll
+        for (int c = 0; c < VC; ++c) {
+          const int ch = 2 * (c0 + c) + (ln >> 1 & 1);
+          const uint2 v0 = lds_column4(vrow + ((ch ^ f) << 4)), v1 = lds_column4(vrow + 16 * RB + ((ch ^ h) << 4));
+          x[c] = u32x4{v0.x, v0.y, v1.x, v1.y};
+        }
+      }
+    };
+    read_v(0, vr[0]);
     settle<NB * QB>(&sc[0][0]);
     bool whole = t0 >= lo_last && t0 + TK <= hi_first;
     if constexpr (PAGED) whole = whole && !(__ballot(ids < 0) & (((1ull << NB) - 1) << (kw * NB)));
@@ -428,70 +488,51 @@ __global__ __launch_bounds__(64 * RW * KW) __attribute__((amdgpu_waves_per_eu(2)
         for (int c = 0; c < CB; ++c) o[c][q] *= alpha;
       }
     }
+    float ref[QB];
 #pragma unroll
-    for (int q = 0; q < QB; ++q) {
-      const float ref = m[q] == -INFINITY ? 0.f : PSH - m[q];
+    for (int q = 0; q < QB; ++q) ref[q] = m[q] == -INFINITY ? 0.f : PSH - m[q];
+    auto prob = [&](int j, int q, int r) {
+      sc[j][q][r] = __builtin_amdgcn_exp2f(fmaf(sc[j][q][r], sl, ref[q]));
+      if constexpr (EB == 4) l[q] += sc[j][q][r];
+    };
+    // The first step's probabilities, then each step's products with the next one's between them.
+    constexpr int SB = EB == 2 ? 2 : 1;                 // 16-key blocks of a step
+    constexpr int NE = SB * QB * 4, PER = (NE + CB - 1) / CB;   // a step's probabilities of a lane; by channel block
+    auto next_probs = [&](int j, int first) {
 #pragma unroll
-      for (int j = 0; j < NB; ++j)
+      for (int e = first; e < min(first + PER, NE); ++e) prob(j + e / (QB * 4), e / 4 % QB, e % 4);
+    };
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          sc[j][q][r] = __builtin_amdgcn_exp2f(fmaf(sc[j][q][r], sl, ref));
-          if constexpr (EB == 4) l[q] += sc[j][q][r];
-        }
-    }
-    if constexpr (EB == 2) {
+    for (int e = 0; e < NE; e += PER) next_probs(0, e);
 #pragma unroll
-      for (int j = 0; j < NB; j += 2) {
-        u32x4 pf[QB];
+    for (int j = 0; j < NB; j += SB) {
+      u32x4 pf[QB];
 #pragma unroll
-        for (int q = 0; q < QB; ++q) {
+      for (int q = 0; q < QB; ++q) {
+        if constexpr (EB == 2) {
 #pragma unroll
           for (int i = 0; i < 2; ++i)
 #pragma unroll
             for (int w = 0; w < 2; ++w) pf[q][2 * i + w] = pair_of<T>(sc[j + i][q][2 * w], sc[j + i][q][2 * w + 1]);
-          ready(pf[q]);
-          mma<T>(ls[q], ones, pf[q]);
-        }
-        if constexpr (F8) {
-          const int row = 16 * (j + (ln >> 3)) + 4 * grp + (ln >> 1 & 3), f = vswz(kw * TK + row);
-          const unsigned char* vrow = vs + row * RB + (ln & 1) * 8;
-#pragma unroll
-          for (int c = 0; c < CB; ++c) {
-            const uint2 w = lds_column8(vrow + ((c ^ f) << 4));
-            u32x4 vf = f8_to_f16x8(w.x, w.y);
-            ready(vf);
-#pragma unroll
-            for (int q = 0; q < QB; ++q) mma<T>(o[c][q], vf, pf[q]);
-          }
         } else {
-          const int row = 16 * j + 4 * grp + (ln >> 2), f = vswz(kw * TK + row), g = vswz(kw * TK + row + 16);
-          const unsigned char* vrow = vs + row * RB + (ln & 1) * 8;
-#pragma unroll
-          for (int c = 0; c < CB; ++c) {
-            const int ch = 2 * c + (ln >> 1 & 1);
-            const uint2 v0 = lds_column4(vrow + ((ch ^ f) << 4)), v1 = lds_column4(vrow + 16 * RB + ((ch ^ g) << 4));
-            const u32x4 vf = u32x4{v0.x, v0.y, v1.x, v1.y};
-#pragma unroll
-            for (int q = 0; q < QB; ++q) mma<T>(o[c][q], vf, pf[q]);
-          }
+          pf[q] = __builtin_bit_cast(u32x4, sc[j][q]);
         }
+        ready(pf[q]);
+        if constexpr (EB == 2) mma<T>(ls[q], ones, pf[q]);
       }
-    } else {
 #pragma unroll
-      for (int j = 0; j < NB; ++j) {
-        const int row = 16 * j + 4 * grp;
-#pragma unroll
-        for (int q = 0; q < QB; ++q) ready(sc[j][q]);
-#pragma unroll
-        for (int c = 0; c < CB; ++c) {
-          u32x4 vf;
-#pragma unroll
-          for (int r = 0; r < 4; ++r)
-            vf[r] = *reinterpret_cast<const unsigned*>(vs + (row + r) * RB +
-                                                       (((c * 4 + (ln >> 2)) ^ vswz(kw * TK + row + r)) << 4) + (ln & 3) * 4);
-#pragma unroll
-          for (int q = 0; q < QB; ++q) mma<T>(o[c][q], vf, __builtin_bit_cast(u32x4, sc[j][q]));
+      for (int c = 0; c < CB; ++c) {
+        const int g = j / SB * (CB / VC) + c / VC;
+        if (c % VC == 0 && g + 1 < VG) read_v(g + 1, vr[(g + 1) & 1]);
+        __builtin_amdgcn_sched_barrier(0);
+        u32x4 vf = vr[g & 1][c % VC];
+        if constexpr (F8) {
+          vf = f8_to_f16x8(vf.x, vf.y);
+          ready(vf);
         }
+#pragma unroll
+        for (int q = 0; q < QB; ++q) mma<T>(o[c][q], vf, pf[q]);
+        if (j + SB < NB) next_probs(j + SB, c * PER);
       }
     }
   };
@@ -502,13 +543,10 @@ __global__ __launch_bounds__(64 * RW * KW) __attribute__((amdgpu_waves_per_eu(2)
     if constexpr (PAGED) ids1 = pages_of(k0 + BK);
     int stage = 0;
     for (int t = k0; t < k1; t += BK, stage ^= 1) {
-      // (the barrier's wait: this tile's loads are done)
+      loads_done();
       bool part_tile = t + BK > real_end;
       if constexpr (PAGED) part_tile = part_tile || (__ballot(ids < 0) & ((1ull << (BK / 16)) - 1));
-      if (part_tile) {
-        loads_done();
-        clear(t, ids, stage);
-      }
+      if (part_tile) clear(t, ids, stage);
       __syncthreads();
       int ids2 = 0;
       if (t + BK < k1) {

@@ -2261,6 +2261,8 @@ nt_status nt_op_attn_prompt(int32_t dtype, const void* d_q, int32_t q_ld, int32_
   a.n_seqs = n_seqs;
   a.n_rows = n_rows;
   nt::attn_prompt_plan(&a);
+  if ((long long)kv_ld * (long long)nt::dt_bytes(a.c.dt) > 1 << 24)      // (a tile's rows within 32-bit offsets)
+    return fail(NT_E_UNSUPPORTED, "rows of d_k and d_v must be at most 16 MiB apart");
   if (n_rows > 1 << 30 || n_seqs > 1 << 30 || (long long)a.rblocks * n_heads >= 1 << 23)
     return fail(NT_E_UNSUPPORTED, "n_rows * n_heads of one call is more than a launch takes");
   if (n_seqs == 0 || n_rows == 0) return NT_OK;

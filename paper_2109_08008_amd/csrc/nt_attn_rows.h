@@ -110,34 +110,66 @@ __device__ __forceinline__ void load_to_lds(const char* base, unsigned at, unsig
   asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(at), "s"(base), "s"(dst)
                : "memory", "m0");
 }
+// The same of what is read once.
+__device__ __forceinline__ void load_to_lds_once(const char* base, unsigned at, unsigned dst) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1 nt" ::"v"(at), "s"(base), "s"(dst)
+               : "memory", "m0");
+}
 __device__ __forceinline__ void load_to_lds(const char* src, unsigned dst) {
   asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(src), "s"(dst) : "memory", "m0");
 }
-// Waits for the wave's loads, those into LDS among them.
-__device__ __forceinline__ void loads_done() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
-
-// The sequence of packed row `row` (a lane's own): how many of off[1 .. n_seqs] are at or below it,
-// by 64 probes that the lanes share and a search between two of them.  n_seqs: none.
-__device__ __forceinline__ int sequence_of(const int* off, int n_seqs, int row, int lane) {
-  const int step = (n_seqs + kWave - 1) / kWave;
-  const int probe = off[min((lane + 1) * step, n_seqs)];
-  int lo = 0;
-#pragma unroll
-  for (int s = kWave / 2; s; s >>= 1)
-    if (__shfl(probe, lo + s - 1, kWave) <= row) lo += s;
-  if (lo == kWave - 1 && __builtin_amdgcn_readlane(probe, kWave - 1) <= row) lo = kWave;
-  int hi = min((lo + 1) * step - 1, n_seqs);
-  lo = min(lo * step, n_seqs);
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if (off[mid] <= row) lo = mid;
-    else hi = mid - 1;
-  }
-  return lo;
+// An address that is the same in every lane, where the compiler cannot tell.
+__device__ __forceinline__ const char* scalar(const char* p) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(p);
+  return reinterpret_cast<const char*>((uintptr_t)(unsigned)__builtin_amdgcn_readfirstlane((int)x) |
+                                       (uintptr_t)(unsigned)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32);
 }
+// Waits until at most N of the wave's loads, those into LDS among them, are under way.
+template <int N>
+__device__ __forceinline__ void loads_done() { asm volatile("s_waitcnt vmcnt(%0)" ::"i"(N) : "memory"); }
+
+// Which sequences a few neighbouring packed rows belong to: a wave reads 64 of the offsets, a lane one
+// of them, from the last that is at or below its first row (found by 64 probes of all of them) on, and
+// its lanes look their rows up there.
+struct Offsets {
+  const int* off;
+  int n_seqs, first, mine;                    // first: of the 64; mine: off[first + lane], clamped to the last
+  __device__ __forceinline__ Offsets(const int* off_, int n, int row, int lane) : off(off_), n_seqs(n), first(0) {
+    if (n >= kWave) {                         // (uniform)
+      const int step = (n + kWave - 1) / kWave;
+      const int probe = off[min(lane * step, n)];
+      const unsigned long long below = __ballot(probe <= row);
+      first = below ? (63 - __builtin_clzll(below)) * step : 0;
+      while (first + kWave - 1 < n && off[first + kWave - 1] <= row) first += kWave - 1;   // (steps past 64)
+    }
+    mine = off[min(first + lane, n)];
+  }
+  // A lane's row: the last b in [0, n_seqs] with off[b] <= row (0 if there is none; n_seqs: behind the
+  // last sequence) and its first and last-but-one rows.
+  __device__ __forceinline__ int find(int row, int& start, int& end) const {
+    int at = 0;
+#pragma unroll
+    for (int s = kWave / 2; s; s >>= 1)
+      if (__shfl(mine, at + s, kWave) <= row) at += s;
+    start = __shfl(mine, at, kWave);
+    end = __shfl(mine, min(at + 1, kWave - 1), kWave);
+    int b = min(first + at, n_seqs);
+    if (at == kWave - 1 && b < n_seqs) {      // beyond the 64
+      int hi = n_seqs;
+      while (b < hi) {
+        const int mid = (b + hi + 1) >> 1;
+        if (off[mid] <= row) b = mid;
+        else hi = mid - 1;
+      }
+      start = off[b];
+      end = off[min(b + 1, n_seqs)];
+    }
+    return b;
+  }
+};
 
 // A workgroup takes BM = RW * QB * 16 query rows; KW waves share the keys of a tile (BK = KW * TK).
-template <typename T, int DH, typename KV, bool PAGED, int QB, int RW, int KW, int TK>
+template <typename T, int DH, typename KV, bool PAGED, int QB, int RW, int KW, int TK, int STG>
 __global__ __launch_bounds__(64 * RW * KW) __attribute__((amdgpu_waves_per_eu(2))) void attn_rows_kernel(RowsAttnArgs a) {
   constexpr int EB = sizeof(T), EC = sizeof(KV);
   constexpr bool F8 = EC == 1;
@@ -156,7 +188,7 @@ __global__ __launch_bounds__(64 * RW * KW) __attribute__((amdgpu_waves_per_eu(2)
   static_assert(EB == 4 || NB % 2 == 0, "16-bit products take 32 keys");
   constexpr int STAGE = 2 * TILE;
   constexpr int JOIN = KW > 1 ? W * QB * 16 * DH * 4 : 0;
-  constexpr int LDS_BYTES = 2 * STAGE > JOIN ? 2 * STAGE : JOIN;
+  constexpr int LDS_BYTES = STG * STAGE > JOIN ? STG * STAGE : JOIN;
   __shared__ __attribute__((aligned(1024))) unsigned char lds[LDS_BYTES];
   __shared__ float jm[W][QB * 16], jl[W][QB * 16];
   __shared__ bool jlive[BM];
@@ -194,74 +226,6 @@ __global__ __launch_bounds__(64 * RW * KW) __attribute__((amdgpu_waves_per_eu(2)
     n_live = a.n_rows;
   }
 
-  // A lane's rows: row ln of each of the wave's QB blocks.  It sees keys [lo, hi), and of a tree the
-  // new tokens of `bits`, which start at `base`.
-  int lo[QB], hi[QB];
-  unsigned long long bits[QB];
-  const char* qrow[QB];
-  bool live[QB];
-#pragma unroll
-  for (int q = 0; q < QB; ++q) {
-    const int r = r0 + (rw * QB + q) * 16 + ln;
-    live[q] = r < n_live;
-    bits[q] = 0;
-    if constexpr (PAGED) {
-      const int rr = min(r, n_live - 1), i = rr / a.group, h = hk * a.group + rr - i * a.group;
-      lo[q] = 0;
-      hi[q] = min(base + i + 1, len);
-      if (a.mask) {
-        hi[q] = min(base, len);
-        const int n = max(0, min(n_new, len - base));     // (positions from len on are not read)
-        bits[q] = a.mask[row_first + i] & (n >= 64 ? ~0ull : (1ull << n) - 1);
-      }
-      qrow[q] = reinterpret_cast<const char*>(static_cast<const T*>(a.q) + (size_t)(row_first + i) * a.q_ld + (size_t)h * DH);
-    } else {
-      const int s = sequence_of(a.off, a.n_seqs, r, lane);
-      const int start = min(max(a.off[min(s, a.n_seqs)], 0), a.n_rows);
-      const int end = s < a.n_seqs ? min(max(a.off[s + 1], start), a.n_rows) : start;
-      live[q] = live[q] && r >= start && r < end;
-      lo[q] = start;
-      hi[q] = !live[q] ? start : a.causal ? r + 1 : end;
-      qrow[q] = reinterpret_cast<const char*>(static_cast<const T*>(a.q) + (size_t)min(r, a.n_rows - 1) * a.q_ld +
-                                              (size_t)head * DH);
-    }
-  }
-  // Of the wave's rows: the largest lo and smallest hi (between them no mask is needed), and the range
-  // outside which no row sees anything.  Both grow with the row.
-  const int lo_first = __builtin_amdgcn_readlane(lo[0], 0), lo_last = __builtin_amdgcn_readlane(lo[QB - 1], 15);
-  const int hi_first = __builtin_amdgcn_readlane(hi[0], 0);
-  int hi_last = __builtin_amdgcn_readlane(hi[QB - 1], 15);
-  int k0, k1;
-  if constexpr (PAGED) {
-    if (a.mask) hi_last = len;
-    if (r0 + rw * QB * 16 >= n_live) hi_last = 0;       // no rows
-    k0 = part * a.chunk;
-    k1 = min(len, k0 + a.chunk);
-    if (!a.mask) k1 = min(k1, max(0, min(base + (min(r0 + BM, n_live) - 1) / a.group + 1, len)));
-    if (k0 >= len && part > 0) return;                  // nothing here; the join does not look
-  } else {
-    if (lane == 0 && kw == 0) {
-      range[rw][0] = lo_first;
-      range[rw][1] = hi_last;
-    }
-    __syncthreads();
-    k0 = __builtin_amdgcn_readfirstlane(range[0][0]);
-    k1 = __builtin_amdgcn_readfirstlane(range[RW - 1][1]);
-  }
-
-  u32x4 qf[QB][QK];
-#pragma unroll
-  for (int q = 0; q < QB; ++q)
-#pragma unroll
-    for (int st = 0; st < QK; ++st) {
-      // E4M3 keys of 64 channels and more come 16 a lane: steps 2p and 2p + 1 take a half each
-      const int at = F8 && DH >= 64 ? st / 2 * 128 + grp * 32 + st % 2 * 16 : st * 64 + grp * 16;
-      u32x4 x = *reinterpret_cast<const u32x4*>(qrow[q] + at);
-#pragma unroll
-      for (int w = 0; w < 4; ++w) x[w] = (x[w] & a.q_and) ^ a.q_xor;
-      qf[q][st] = x;
-    }
-
   // ---- tiles of keys and values into LDS ----
   // Chunk c of row r lies at chunk c ^ f(r): 16 rows of one chunk (keys), 8 rows of two or 4 of four
   // (values' columns) fall on different banks.
@@ -277,16 +241,19 @@ __global__ __launch_bounds__(64 * RW * KW) __attribute__((amdgpu_waves_per_eu(2)
   const char* Kp = PAGED ? static_cast<const char*>(a.c.k) + hk * head_bytes : static_cast<const char*>(a.k) + (size_t)hk * RB;
   const char* Vp = PAGED ? static_cast<const char*>(a.c.v) + hk * head_bytes : static_cast<const char*>(a.v) + (size_t)hk * RB;
   const size_t ldb = (size_t)a.kv_ld * EB;
-  // page of the tile's 16-key block `lane`; -1: none
-  auto pages_of = [&](int t) {
+  // Pages of 64 blocks of 16 keys from `window` on, a block a lane, and of the 64 behind them; -1: none.
+  constexpr int SPAN = 64 * 16;
+  auto pages_from = [&](int t) {
     const int key = t + lane * 16;
     int id = -1;
-    if (lane < BK / 16 && key < len) {
+    if (key < len) {
       id = table[min(key >> sh, a.c.max_pages - 1)];
       if ((unsigned)id >= (unsigned)a.c.n_pages) id = -1;
     }
     return id;
   };
+  int window = 0, ids0 = -1, ids1 = -1;
+  unsigned long long holes = 0;                         // of ids0, a bit a block
   const unsigned lds0 = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)NT_LDS(lds) + wave * 1024);
   // A lane's places in the rows that its loads cover (of a page's 16 keys, or of the tile): constant, so
   // that a load takes a scalar base and no vector instruction.
@@ -301,45 +268,140 @@ __global__ __launch_bounds__(64 * RW * KW) __attribute__((amdgpu_waves_per_eu(2)
       vat[u] = at + ((ch ^ vswz(row)) << 4);
     }
   }
-  auto issue = [&](int t, int ids, int stage) {
+  auto issue = [&](int t, int stage) {
     const unsigned dst = lds0 + stage * STAGE;
+    const int ids = t - window < SPAN ? ids0 : ids1, block0 = ((t - window) >> 4) & 63;
     if constexpr (PAGED && UNIFORM) {
 #pragma unroll
       for (int u = 0; u < NP; ++u) {
         const int block = (u * W + wave) * RPL / 16;
-        const int id = __builtin_amdgcn_readlane(ids, block);
+        const int id = __builtin_amdgcn_readlane(ids, block0 + block);
         const size_t at = (size_t)max(id, 0) * page_bytes + (size_t)((t + block * 16) & (slots - 1)) * RB;
-        load_to_lds(Kp + at, kat[u], dst + u * W * 1024);
-        load_to_lds(Vp + at, vat[u], dst + TILE + u * W * 1024);
+        if (a.rblocks == 1) {
+          load_to_lds_once(Kp + at, kat[u], dst + u * W * 1024);
+          load_to_lds_once(Vp + at, vat[u], dst + TILE + u * W * 1024);
+        } else {
+          load_to_lds(Kp + at, kat[u], dst + u * W * 1024);
+          load_to_lds(Vp + at, vat[u], dst + TILE + u * W * 1024);
+        }
       }
-    } else if (!PAGED && t + BK <= k1) {
-      const char *ks = Kp + t * ldb, *vs = Vp + t * ldb;
+    } else if (!PAGED && t + BK <= a.n_rows) {
+      const char *ks = scalar(Kp + t * ldb), *vs = scalar(Vp + t * ldb);
+      asm volatile("s_nop 4" : "+s"(ks), "+s"(vs));     // (a load waits for scalars that vector instructions wrote)
 #pragma unroll
       for (int u = 0; u < NP; ++u) {
         load_to_lds(ks, kat[u], dst + u * W * 1024);
         load_to_lds(vs, vat[u], dst + TILE + u * W * 1024);
       }
-    } else {                                            // rows past the last: that one again
+    } else {                                            // rows past the buffer's: its last again
+      int here = lane;
+      asm volatile("" : "+v"(here));                    // (what follows from it is not kept over the loop)
 #pragma unroll
       for (int u = 0; u < NP; ++u) {
-        const int row = (u * W + wave) * RPL + lane / CH, ch = lane % CH;
+        const int row = (u * W + wave) * RPL + here / CH, ch = here % CH;
         size_t at;
-        if constexpr (PAGED) at = (size_t)max(__shfl(ids, row / 16, kWave), 0) * page_bytes + (size_t)((t + row) & (slots - 1)) * RB;
-        else at = (size_t)min(t + row, k1 - 1) * ldb;
+        if constexpr (PAGED) at = (size_t)max(__shfl(ids, block0 + row / 16, kWave), 0) * page_bytes + (size_t)((t + row) & (slots - 1)) * RB;
+        else at = (size_t)min(t + row, a.n_rows - 1) * ldb;
         load_to_lds(Kp + at + ((ch ^ kswz(row)) << 4), dst + u * W * 1024);
         load_to_lds(Vp + at + ((ch ^ vswz(row)) << 4), dst + TILE + u * W * 1024);
       }
     }
   };
+  // A lane's rows: row ln of each of the wave's QB blocks.  It sees keys [lo, hi), and of a tree the
+  // new tokens of `bits`, which start at `base`.
+  int lo[QB], hi[QB];
+  unsigned long long bits[QB];
+  const char* qrow[QB];
+  bool live[QB];
+  const int row0 = r0 + rw * QB * 16;         // the wave's first
+  const Offsets offsets(PAGED ? nullptr : a.off, PAGED ? 0 : a.n_seqs, row0, lane);
+#pragma unroll
+  for (int q = 0; q < QB; ++q) {
+    const int r = row0 + q * 16 + ln;
+    live[q] = r < n_live;
+    bits[q] = 0;
+    if constexpr (PAGED) {
+      const int rr = min(r, n_live - 1), i = rr / a.group, h = hk * a.group + rr - i * a.group;
+      lo[q] = 0;
+      hi[q] = min(base + i + 1, len);
+      if (a.mask) {
+        hi[q] = min(base, len);
+        const int n = max(0, min(n_new, len - base));     // (positions from len on are not read)
+        bits[q] = a.mask[row_first + i] & (n >= 64 ? ~0ull : (1ull << n) - 1);
+      }
+      qrow[q] = reinterpret_cast<const char*>(static_cast<const T*>(a.q) + (size_t)(row_first + i) * a.q_ld + (size_t)h * DH);
+    } else {
+      int start, end;
+      const int s = offsets.find(r, start, end);
+      start = min(max(start, 0), a.n_rows);
+      end = s < a.n_seqs ? min(max(end, start), a.n_rows) : start;
+      live[q] = live[q] && r >= start && r < end;
+      lo[q] = start;
+      hi[q] = !live[q] ? start : a.causal ? r + 1 : end;
+      qrow[q] = reinterpret_cast<const char*>(static_cast<const T*>(a.q) + (size_t)min(r, a.n_rows - 1) * a.q_ld +
+                                              (size_t)head * DH);
+    }
+  }
+  // Of the wave's rows: the largest lo and smallest hi (between them no mask is needed), and the range
+  // outside which no row sees anything.  Both grow with the row.
+  const int lo_first = __builtin_amdgcn_readlane(lo[0], 0), lo_last = __builtin_amdgcn_readlane(lo[QB - 1], 15);
+  const int hi_first = __builtin_amdgcn_readlane(hi[0], 0);
+  int hi_last = __builtin_amdgcn_readlane(hi[QB - 1], 15);
+  int k0, k1;
+  if constexpr (PAGED) {
+    if (a.mask) hi_last = len;
+    if (row0 >= n_live) hi_last = 0;                    // no rows
+    k0 = part * a.chunk;
+    k1 = min(len, k0 + a.chunk);
+    if (!a.mask) k1 = min(k1, max(0, min(base + (min(r0 + BM, n_live) - 1) / a.group + 1, len)));
+    if (k0 >= len && part > 0) return;                  // nothing here; the join does not look
+  } else {
+    k0 = lo_first;
+    k1 = hi_last;
+    if constexpr (RW > 1) {
+      if (lane == 0 && kw == 0) {
+        range[rw][0] = k0;
+        range[rw][1] = k1;
+      }
+      __syncthreads();
+      k0 = __builtin_amdgcn_readfirstlane(range[0][0]);
+      k1 = __builtin_amdgcn_readfirstlane(range[RW - 1][1]);
+    }
+  }
+
+  if constexpr (PAGED) {
+    window = k0;
+    ids0 = pages_from(k0);
+    ids1 = pages_from(k0 + SPAN);
+    holes = __ballot(ids0 < 0);
+  }
+  u32x4 qf[QB][QK];
+#pragma unroll
+  for (int q = 0; q < QB; ++q)
+#pragma unroll
+    for (int st = 0; st < QK; ++st) {
+      // E4M3 keys of 64 channels and more come 16 a lane: steps 2p and 2p + 1 take a half each
+      const int at = F8 && DH >= 64 ? st / 2 * 128 + grp * 32 + st % 2 * 16 : st * 64 + grp * 16;
+      qf[q][st] = *reinterpret_cast<const u32x4*>(qrow[q] + at);
+    }
+  if (a.q_xor | ~a.q_and) {                             // a scale below or equal to 0
+#pragma unroll
+    for (int q = 0; q < QB; ++q)
+#pragma unroll
+      for (int st = 0; st < QK; ++st)
+#pragma unroll
+        for (int w = 0; w < 4; ++w) qf[q][st][w] = (qf[q][st][w] & a.q_and) ^ a.q_xor;
+  }
+
   // What lies behind the last key, or on no page, may be anything: its values become zeros (no 0 * NaN).
   const int real_end = PAGED ? len : k1;
-  auto clear = [&](int t, int ids, int stage) {
+  auto clear = [&](int t, unsigned none_of, int stage) {
     unsigned char* dst = lds + stage * STAGE + TILE + wave * 1024 + lane * 16;
 #pragma unroll
     for (int u = 0; u < NP; ++u) {
       const int row = (u * W + wave) * RPL + lane / CH;
       bool none = t + row >= real_end;
-      if constexpr (PAGED) none |= __shfl(ids, row / 16, kWave) < 0;   // (every lane takes part)
+      if constexpr (PAGED) none |= (none_of >> (row / 16)) & 1;
       if (none) *reinterpret_cast<u32x4*>(dst + u * W * 1024) = u32x4{0, 0, 0, 0};
     }
   };
@@ -370,7 +432,7 @@ __global__ __launch_bounds__(64 * RW * KW) __attribute__((amdgpu_waves_per_eu(2)
     }
   };
 
-  auto compute = [&](int t, int ids, int stage) {
+  auto compute = [&](int t, unsigned none_of, int stage) {
     const int t0 = t + kw * TK;
     if (t0 >= min(hi_last, k1) || t0 + TK <= lo_first) return;
     const unsigned char* ks = lds + stage * STAGE + kw * TK * RB;
@@ -445,17 +507,31 @@ __global__ __launch_bounds__(64 * RW * KW) __attribute__((amdgpu_waves_per_eu(2)
     read_v(0, vr[0]);
     settle<NB * QB>(&sc[0][0]);
     bool whole = t0 >= lo_last && t0 + TK <= hi_first;
-    if constexpr (PAGED) whole = whole && !(__ballot(ids < 0) & (((1ull << NB) - 1) << (kw * NB)));
+    none_of = (none_of >> (kw * NB)) & ((1u << NB) - 1);
+    whole = whole && !none_of;
+    // A key that a lane's row does not see counts -inf.  Which ones: an interval of the row's (a tile's
+    // keys against it by comparisons with constants), holes, a tree's new tokens.
     if (!whole) {
 #pragma unroll
-      for (int j = 0; j < NB; ++j) {
-        bool there = true;
-        if constexpr (PAGED) there = __builtin_amdgcn_readlane(ids, kw * NB + j) >= 0;
+      for (int q = 0; q < QB; ++q) {
+        const int end = hi[q] - t0 - 4 * grp, first = lo[q] - t0 - 4 * grp;
+        unsigned long long tree = 0;                    // bit c: key t0 + 16 j + 4 grp + c, j a multiple of 4
 #pragma unroll
-        for (int q = 0; q < QB; ++q)
+        for (int j = 0; j < NB; ++j) {
+          if (PAGED && j % 4 == 0) {
+            const int shift = base - t0 - 16 * j - 4 * grp;
+            tree = shift >= 64 || shift <= -64 ? 0 : shift >= 0 ? bits[q] << shift : bits[q] >> -shift;
+          }
+          const unsigned part = (unsigned)(tree >> (j * 16 & 63));
+          const bool there = !((none_of >> j) & 1);
 #pragma unroll
-          for (int r = 0; r < 4; ++r)
-            sc[j][q][r] = there & sees(q, t0 + 16 * j + 4 * grp + r) ? sc[j][q][r] : -INFINITY;
+          for (int r = 0; r < 4; ++r) {
+            bool s = 16 * j + r < end;
+            if constexpr (PAGED) s = (s | ((part >> r) & 1)) & there;
+            else s = s & (16 * j + r >= first);
+            sc[j][q][r] = s ? sc[j][q][r] : -INFINITY;
+          }
+        }
       }
     }
     // the reference moves only when a score passes it by LAZY
@@ -537,25 +613,28 @@ __global__ __launch_bounds__(64 * RW * KW) __attribute__((amdgpu_waves_per_eu(2)
     }
   };
 
-  if (k0 < k1) {
-    int ids = PAGED ? pages_of(k0) : 0, ids1 = 0;
-    issue(k0, ids, 0);
-    if constexpr (PAGED) ids1 = pages_of(k0 + BK);
-    int stage = 0;
-    for (int t = k0; t < k1; t += BK, stage ^= 1) {
-      loads_done();
-      bool part_tile = t + BK > real_end;
-      if constexpr (PAGED) part_tile = part_tile || (__ballot(ids < 0) & ((1ull << (BK / 16)) - 1));
-      if (part_tile) clear(t, ids, stage);
-      __syncthreads();
-      int ids2 = 0;
-      if (t + BK < k1) {
-        issue(t + BK, ids1, stage ^ 1);
-        if constexpr (PAGED) ids2 = pages_of(t + 2 * BK);
+#pragma unroll
+  for (int i = 0; i < STG - 1; ++i)
+    if (k0 + i * BK < k1) issue(k0 + i * BK, i);
+  int stage = 0;
+  for (int t = k0; t < k1; t += BK) {
+    // this tile's loads are done; the STG - 2 tiles behind it may be under way
+    if (t + (STG - 2) * BK < k1) loads_done<2 * NP * (STG - 2)>();
+    else loads_done<0>();
+    unsigned none_of = 0;                               // blocks of the tile without a page
+    if constexpr (PAGED) none_of = (unsigned)(holes >> ((t - window) >> 4)) & (unsigned)((1ull << (BK / 16)) - 1);
+    if (none_of || t + BK > real_end) clear(t, none_of, stage);
+    __syncthreads();
+    if (t + (STG - 1) * BK < k1) issue(t + (STG - 1) * BK, stage == 0 ? STG - 1 : stage - 1);
+    compute(t, none_of, stage);
+    stage = stage == STG - 1 ? 0 : stage + 1;
+    if constexpr (PAGED) {
+      if (t + BK - window == SPAN) {
+        window += SPAN;
+        ids0 = ids1;
+        holes = __ballot(ids0 < 0);
+        ids1 = pages_from(window + SPAN);
       }
-      compute(t, ids, stage);
-      ids = ids1;
-      ids1 = ids2;
     }
   }
   settle<CB * QB>(&o[0][0]);
@@ -651,6 +730,7 @@ __global__ __launch_bounds__(64 * RW * KW) __attribute__((amdgpu_waves_per_eu(2)
   }
 
   // ---- the rows' outputs ----
+  const bool whole_length = a.parts == 1 || len <= a.chunk;   // (else a part of it, for the join)
   auto out_row = [&](int r) -> T* {           // of the workgroup's row r
     if constexpr (PAGED) {
       const int i = (r0 + r) / a.group, h = hk * a.group + (r0 + r) - i * a.group;
@@ -674,7 +754,7 @@ __global__ __launch_bounds__(64 * RW * KW) __attribute__((amdgpu_waves_per_eu(2)
     for (int q = 0; q < QB; ++q) {
       const int r = (rw * QB + q) * 16 + ln;
       if (!live[q]) continue;
-      if (!PAGED || a.parts == 1) {
+      if (!PAGED || whole_length) {
         const float inv = l[q] == 0.f ? 0.f : 1.0f / l[q];
 #pragma unroll
         for (int c = 0; c < CB; ++c) store4(r, c * 16 + 4 * grp, o[c][q], inv);
@@ -716,7 +796,7 @@ __global__ __launch_bounds__(64 * RW * KW) __attribute__((amdgpu_waves_per_eu(2)
         z += f * jl[w0 + w][i];
         s += f * *reinterpret_cast<const floatx4*>(jo + ((w0 + w) * QB * 16 + i) * DH + ((x ^ (i & 7)) << 2));
       }
-      if (!PAGED || a.parts == 1) {
+      if (!PAGED || whole_length) {
         store4(r, x * 4, s, z == 0.f ? 0.f : 1.0f / z);
       } else {
         const size_t pr = part_row(r);
@@ -726,84 +806,104 @@ __global__ __launch_bounds__(64 * RW * KW) __attribute__((amdgpu_waves_per_eu(2)
     }
   }
 }
-// Merges the parts of a (new row, head): a wave, DH / 4 lanes four channels each of every
-// (256 / DH)-th part, U parts' loads in flight.
-template <typename T, int DH>
+// Merges the parts of ITEMS heads of a new row: a wave, DH / 4 lanes four channels each of every
+// (256 / DH)-th part, ITEMS * U parts' loads in flight.
+template <typename T, int DH, int ITEMS>
 __global__ __launch_bounds__(256) void rows_join_kernel(RowsAttnArgs a) {
-  constexpr int COLS = DH / 4, ROWS = kWave / COLS, U = 8;
+  constexpr int COLS = DH / 4, ROWS = kWave / COLS, U = 8 / ITEMS;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
-  const long long item = (long long)blockIdx.x * 4 + wave;
-  const int row = (int)(item / a.n_heads), h = (int)(item - (long long)row * a.n_heads);
+  const long long item = ((long long)blockIdx.x * 4 + wave) * ITEMS;
+  const int row = (int)(item / a.n_heads), h0 = (int)(item - (long long)row * a.n_heads);
   if (row >= a.n_rows) return;
   int b = row;
   if (a.off) {
-    b = __builtin_amdgcn_readfirstlane(sequence_of(a.off, a.n_seqs, row, lane));
-    if (b >= a.n_seqs) return;                  // a row of no sequence
-    const int first = max(a.off[b], 0);
-    if (row < first || row - first >= a.max_new) return;
+    int first, end;
+    const Offsets offsets(a.off, a.n_seqs, row, lane);
+    b = __builtin_amdgcn_readfirstlane(offsets.find(row, first, end));
+    first = max(__builtin_amdgcn_readfirstlane(first), 0);
+    if (b >= a.n_seqs || row < first || row - first >= a.max_new) return;   // a row of no sequence, or past max_new
   }
   const int len = max(0, min(a.lens[b], a.max_len));
-  const int n = max(1, (len + a.chunk - 1) / a.chunk);   // (part 0 is written for an empty row too)
+  if (len <= a.chunk) return;                   // one part, written where it belongs
+  const int n = (len + a.chunk - 1) / a.chunk;
   const size_t stride = (size_t)a.n_rows * a.n_heads;
   const int p0 = lane / COLS, x = lane % COLS * 4;
   const float* ml = a.part_ml + (size_t)item * 2;
   const float* po = a.part_o + (size_t)item * DH + x;
-  floatx4 s = floatx4{0.f, 0.f, 0.f, 0.f};
-  float m = -INFINITY, l = 0.f;
+  floatx4 s[ITEMS];
+  float m[ITEMS], l[ITEMS];
+#pragma unroll
+  for (int i = 0; i < ITEMS; ++i) {
+    s[i] = floatx4{0.f, 0.f, 0.f, 0.f};
+    m[i] = -INFINITY;
+    l[i] = 0.f;
+  }
   for (int p = p0; p < n; p += ROWS * U) {
-    float2 w[U];
-    floatx4 v[U];
+    float2 w[ITEMS][U];
+    floatx4 v[ITEMS][U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const size_t at = min(p + u * ROWS, n - 1);
-      w[u] = *reinterpret_cast<const float2*>(ml + at * stride * 2);
-      v[u] = *reinterpret_cast<const floatx4*>(po + at * stride * DH);
-    }
-    float mn = m;
+      const size_t at = (size_t)min(p + u * ROWS, n - 1) * stride;
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      if (p + u * ROWS >= n) w[u] = make_float2(-INFINITY, 0.f);
-      mn = fmaxf(mn, w[u].x);
+      for (int i = 0; i < ITEMS; ++i) {
+        w[i][u] = *reinterpret_cast<const float2*>(ml + (at + i) * 2);
+        v[i][u] = *reinterpret_cast<const floatx4*>(po + (at + i) * DH);
+      }
     }
-    const float ref = mn == -INFINITY ? 0.f : mn, f0 = __builtin_amdgcn_exp2f(m - ref);
-    l *= f0;
-    s *= f0;
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const float f = __builtin_amdgcn_exp2f(w[u].x - ref);
-      l += f * w[u].y;
-      if (p + u * ROWS < n) s += f * v[u];      // (a part past the last is the last one's again)
+    for (int i = 0; i < ITEMS; ++i) {
+      float mn = m[i];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (p + u * ROWS >= n) w[i][u] = make_float2(-INFINITY, 0.f);
+        mn = fmaxf(mn, w[i][u].x);
+      }
+      const float ref = mn == -INFINITY ? 0.f : mn, f0 = __builtin_amdgcn_exp2f(m[i] - ref);
+      l[i] *= f0;
+      s[i] *= f0;
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const float f = __builtin_amdgcn_exp2f(w[i][u].x - ref);
+        l[i] += f * w[i][u].y;
+        if (p + u * ROWS < n) s[i] += f * v[i][u];      // (a part past the last is the last one's again)
+      }
+      m[i] = mn;
     }
-    m = mn;
   }
 #pragma unroll
-  for (int d = COLS; d < kWave; d *= 2) {
-    const float mo = __shfl_xor(m, d, kWave), lo = __shfl_xor(l, d, kWave);
-    const float mn = fmaxf(m, mo), ref = mn == -INFINITY ? 0.f : mn;
-    const float f = __builtin_amdgcn_exp2f(m - ref), g = __builtin_amdgcn_exp2f(mo - ref);
-    l = l * f + lo * g;
+  for (int i = 0; i < ITEMS; ++i) {
 #pragma unroll
-    for (int r = 0; r < 4; ++r) s[r] = s[r] * f + __shfl_xor(s[r], d, kWave) * g;
-    m = mn;
+    for (int d = COLS; d < kWave; d *= 2) {
+      const float mo = __shfl_xor(m[i], d, kWave), lo = __shfl_xor(l[i], d, kWave);
+      const float mn = fmaxf(m[i], mo), ref = mn == -INFINITY ? 0.f : mn;
+      const float f = __builtin_amdgcn_exp2f(m[i] - ref), g = __builtin_amdgcn_exp2f(mo - ref);
+      l[i] = l[i] * f + lo * g;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) s[i][r] = s[i][r] * f + __shfl_xor(s[i][r], d, kWave) * g;
+      m[i] = mn;
+    }
+    if (lane >= COLS) continue;
+    const float inv = l[i] == 0.f ? 0.f : 1.0f / l[i];
+    alignas(16) T t4[4] = {from_f32<T>(s[i].x * inv), from_f32<T>(s[i].y * inv), from_f32<T>(s[i].z * inv),
+                           from_f32<T>(s[i].w * inv)};
+    T* out = static_cast<T*>(a.out) + (size_t)row * a.out_ld + (size_t)(h0 + i) * DH + x;
+    if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(out) = *reinterpret_cast<const uint2*>(t4);
+    else *reinterpret_cast<uint4*>(out) = *reinterpret_cast<const uint4*>(t4);
   }
-  if (lane >= COLS) return;
-  const float inv = l == 0.f ? 0.f : 1.0f / l;
-  alignas(16) T t4[4] = {from_f32<T>(s.x * inv), from_f32<T>(s.y * inv), from_f32<T>(s.z * inv), from_f32<T>(s.w * inv)};
-  T* out = static_cast<T*>(a.out) + (size_t)row * a.out_ld + (size_t)h * DH + x;
-  if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(out) = *reinterpret_cast<const uint2*>(t4);
-  else *reinterpret_cast<uint4*>(out) = *reinterpret_cast<const uint4*>(t4);
 }
 
 // ---- launches ----------------------------------------------------------------------------
-// Keys of a wave's share of a tile, by what 160 KB of LDS hold twice over; a load of each wave at least.
-template <typename T, int DH, typename KV, int KW>
+// Keys of a wave's share of a tile (a load of each wave at least).
+template <typename T, int DH, typename KV, int RW, int KW>
 constexpr int rows_keys() {
-  return sizeof(T) == 4 ? (KW == 1 ? 32 : 16) : KW > 1 ? 32 : DH * sizeof(KV) == 32 ? 128 : 64;
+  constexpr int least = 1024 * RW / (DH * (int)sizeof(KV));
+  return std::max(least, sizeof(T) == 4 ? (KW == 1 ? 32 : 16) : KW == 1 ? 64 : 32);
 }
 
 template <typename T, int DH, typename KV, bool PAGED, int QB, int RW, int KW>
 hipError_t rows_launch(const RowsAttnArgs& a, unsigned grid, hipStream_t s) {
-  NT_LAUNCH((attn_rows_kernel<T, DH, KV, PAGED, QB, RW, KW, rows_keys<T, DH, KV, KW>()>), dim3(grid), dim3(64 * RW * KW), 0, s, a);
+  constexpr int TK = rows_keys<T, DH, KV, RW, KW>();
+  NT_LAUNCH((attn_rows_kernel<T, DH, KV, PAGED, QB, RW, KW, TK, 2>), dim3(grid), dim3(64 * RW * KW), 0, s, a);
   return hipGetLastError();
 }
 
@@ -811,31 +911,36 @@ template <typename T, int DH, typename KV, bool PAGED>
 hipError_t rows_tile(const RowsAttnArgs& a, hipStream_t s) {
   const unsigned grid = PAGED ? ((unsigned)(a.n_seqs * a.c.n_kv_heads * a.parts) + 7) / 8 * 8 * a.rblocks
                               : (unsigned)(a.rblocks * a.n_heads);
+  hipError_t e = hipErrorInvalidValue;
   switch (a.tile) {
-    case ROWS_128: return rows_launch<T, DH, KV, PAGED, 2, 4, 1>(a, grid, s);
-    case ROWS_32: return rows_launch<T, DH, KV, PAGED, 2, 1, 4>(a, grid, s);
-    case ROWS_16: return rows_launch<T, DH, KV, PAGED, 1, 1, 4>(a, grid, s);
-    default: return hipErrorInvalidValue;
+    case ROWS_128: e = rows_launch<T, DH, KV, PAGED, 2, 4, 1>(a, grid, s); break;
+    case ROWS_64: e = rows_launch<T, DH, KV, PAGED, 2, 2, 2>(a, grid, s); break;
+    case ROWS_32:
+      if constexpr (!PAGED) e = rows_launch<T, DH, KV, PAGED, 2, 1, 4>(a, grid, s);
+      break;
+    case ROWS_16: e = rows_launch<T, DH, KV, PAGED, 1, 1, 4>(a, grid, s); break;
   }
+  if constexpr (PAGED) {
+    if (e != hipSuccess || a.parts == 1) return e;
+    // few parts: four heads of a row a wave
+    const long long items = (long long)a.n_rows * a.n_heads;
+    if (a.parts <= 8 && a.n_heads % 4 == 0)
+      NT_LAUNCH((rows_join_kernel<T, DH, 4>), dim3((unsigned)((items / 4 + 3) / 4)), dim3(256), 0, s, a);
+    else
+      NT_LAUNCH((rows_join_kernel<T, DH, 1>), dim3((unsigned)((items + 3) / 4)), dim3(256), 0, s, a);
+    e = hipGetLastError();
+  }
+  return e;
 }
 
 template <typename T, typename KV, bool PAGED>
 hipError_t rows_head(const RowsAttnArgs& a, hipStream_t s) {
-  hipError_t e;
   switch (a.c.d_head) {
-    case 32: e = rows_tile<T, 32, KV, PAGED>(a, s); break;
-    case 64: e = rows_tile<T, 64, KV, PAGED>(a, s); break;
-    case 128: e = rows_tile<T, 128, KV, PAGED>(a, s); break;
+    case 32: return rows_tile<T, 32, KV, PAGED>(a, s);
+    case 64: return rows_tile<T, 64, KV, PAGED>(a, s);
+    case 128: return rows_tile<T, 128, KV, PAGED>(a, s);
     default: return hipErrorInvalidValue;
   }
-  if (!PAGED || e != hipSuccess || a.parts == 1) return e;
-  const dim3 grid((unsigned)(((long long)a.n_rows * a.n_heads + 3) / 4));
-  switch (a.c.d_head) {
-    case 32: NT_LAUNCH((rows_join_kernel<T, 32>), grid, dim3(256), 0, s, a); break;
-    case 64: NT_LAUNCH((rows_join_kernel<T, 64>), grid, dim3(256), 0, s, a); break;
-    case 128: NT_LAUNCH((rows_join_kernel<T, 128>), grid, dim3(256), 0, s, a); break;
-  }
-  return hipGetLastError();
 }
 }  // namespace
 }  // namespace nt

@@ -337,7 +337,7 @@ hipError_t paged_attn(const PagedAttnArgs& a, hipStream_t s);
 // ---------------------------------------------------------------------------------
 // Attention of many query rows (nt_attn_rows.h, nt_rows.hip): packed prompts, and several new
 // tokens a sequence over a paged cache.
-enum RowsTile : int { ROWS_16 = 0, ROWS_32 = 1, ROWS_128 = 2 };   // query rows of a workgroup
+enum RowsTile : int { ROWS_16 = 0, ROWS_32 = 1, ROWS_64 = 2, ROWS_128 = 3 };   // query rows of a workgroup
 struct RowsAttnArgs {
   PagedCache c;               // (prompts: dt, n_kv_heads and d_head only)
   const void* q;              // row i at + i * q_ld, head h at + h * d_head

@@ -1,27 +1,42 @@
-// How attention of many query rows is cut, and which data type's kernels take it.
+// How attention of many query rows is cut, by sizes that the host knows, and which data type's kernels take it.
 #include <algorithm>
 
 #include "nt_kernels.h"
 
 namespace nt {
 
+// The largest tile that still gives the CUs enough workgroups: a large one reads keys less often, a
+// small one ends sooner (its waves share the keys of a tile, and join in LDS).  Measured, us, with
+// tiles of 16 / 32 / 64 / 128 rows, one fp16 prompt: 8 heads, d_head 64, 100 tokens 7.1 / 7.1 / 7.8 / 7.8,
+// 300 7.8 / 7.7 / 9.8 / 10.7, 1000 10.1 / 12.1 / 18.5 / 25, 3000 36 / 30 / 45 / 65; 16 heads, d_head 128,
+// 300 10.5 / 10.3 / 12.4 / 13.6, 1000 32 / 23 / 24 / 32, 3000 170 / 109 / 64 / 88, 8000 - / 648 / 335 / 286.
 void attn_prompt_plan(RowsAttnArgs* a) {
-  a->tile = ROWS_128;
-  a->rblocks = (int)(((long long)a->n_rows + 127) / 128);
+  auto groups = [&](int rows) { return (a->n_rows + (long long)rows - 1) / rows * a->n_heads; };
+  a->tile = groups(128) >= 768 ? ROWS_128 : groups(64) >= 512 ? ROWS_64 : groups(32) >= 400 ? ROWS_32 : ROWS_16;
+  a->rblocks = (int)((a->n_rows + (16ll << a->tile) - 1) >> (4 + a->tile));
   a->parts = 1;
   a->chunk = 0;
 }
 
+// A key head's rows (new tokens times the heads that share it) in one tile if they fit: a second block of
+// rows reads the keys again.  Measured, us, with 16 / 64 / 128 rows: 64 requests of 100..4000 bf16
+// positions, 8 key heads of 128 channels (597 MB), 8 rows 110 / 108 / 126, 32 rows 176 / 109 / 117, 1..96 rows
+// - / 157 / 121, 256 rows - / 245 / 200.
+// Lengths are cut into parts of 512 keys' multiples until two workgroups a CU have work; with more than two
+// blocks of rows, where matrix products bound it and a workgroup's own time is long, until six have, so
+// that the ends of ragged batches even out.  Measured, us, uncut / 4096 / 2048 / 1024 keys: 12 requests of
+// 1000..8000 positions and 200..500 new tokens, 4 key heads of four 245 / 184 / 184 / 214, three such
+// 68 / 68 / 61 / 50, forty 555 / 577 / 637 / 731; one of 131001 E4M3 positions, 64 new 3150 / 119 / 95 / 106.
+// Never more than 32768 parts in all, however far max_len is above the lengths.
 void attn_tree_plan(RowsAttnArgs* a) {
   const long long rows = (long long)std::max(a->max_new, 1) * a->group;
-  a->tile = rows <= 16 ? ROWS_16 : rows <= 32 ? ROWS_32 : ROWS_128;
-  const int bm = a->tile == ROWS_16 ? 16 : a->tile == ROWS_32 ? 32 : 128;
-  a->rblocks = (int)((rows + bm - 1) / bm);
+  a->tile = rows <= 16 ? ROWS_16 : rows <= 64 ? ROWS_64 : ROWS_128;
+  a->rblocks = (int)((rows + (16ll << a->tile) - 1) >> (4 + a->tile));
   const long long tasks = std::max<long long>(1, (long long)a->n_seqs * a->c.n_kv_heads * a->rblocks);
-  long long parts = std::max<long long>(1, 1024 / tasks);
-  long long chunk = (a->max_len + parts - 1) / parts;
-  chunk = std::max<long long>(512, (chunk + 511) / 512 * 512);
-  a->chunk = (int)std::min<long long>(chunk, 1 << 30);
+  const long long want = std::max<long long>(1, (a->rblocks > 2 ? 1536 : 512) / tasks);
+  const long long least = std::max<long long>(1, a->max_len * tasks / 32768);
+  long long chunk = std::max({(a->max_len + want - 1) / want, least, 512ll});
+  a->chunk = (int)std::min<long long>((chunk + 511) / 512 * 512, 1 << 30);
   a->parts = (int)std::max<long long>(1, (a->max_len + (long long)a->chunk - 1) / a->chunk);
 }
 

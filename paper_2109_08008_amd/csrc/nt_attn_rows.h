@@ -169,7 +169,7 @@ struct Offsets {
 };
 
 // A workgroup takes BM = RW * QB * 16 query rows; KW waves share the keys of a tile (BK = KW * TK).
-template <typename T, int DH, typename KV, bool PAGED, int QB, int RW, int KW, int TK, int STG>
+template <typename T, int DH, typename KV, bool PAGED, int QB, int RW, int KW, int TK>
 __global__ __launch_bounds__(64 * RW * KW) __attribute__((amdgpu_waves_per_eu(2))) void attn_rows_kernel(RowsAttnArgs a) {
   constexpr int EB = sizeof(T), EC = sizeof(KV);
   constexpr bool F8 = EC == 1;
@@ -186,13 +186,13 @@ __global__ __launch_bounds__(64 * RW * KW) __attribute__((amdgpu_waves_per_eu(2)
   constexpr float PSH = p_shift<T>();
   static_assert(TILE % (W * 1024) == 0 && NP >= 1, "a tile's rows split evenly over the waves");
   static_assert(EB == 4 || NB % 2 == 0, "16-bit products take 32 keys");
-  constexpr int STAGE = 2 * TILE;
+  // LDS: two tiles of keys, two of values; the join of waves that share rows
   constexpr int JOIN = KW > 1 ? W * QB * 16 * DH * 4 : 0;
-  constexpr int LDS_BYTES = STG * STAGE > JOIN ? STG * STAGE : JOIN;
+  constexpr int LDS_BYTES = std::max(4 * TILE, JOIN);
   __shared__ __attribute__((aligned(1024))) unsigned char lds[LDS_BYTES];
-  __shared__ float jm[W][QB * 16], jl[W][QB * 16];
-  __shared__ bool jlive[BM];
-  __shared__ int range[RW][2];
+  __shared__ float jm[KW > 1 ? W : 1][QB * 16], jl[KW > 1 ? W : 1][QB * 16];
+  __shared__ bool jlive[KW > 1 ? BM : 1];
+  int (*range)[2] = reinterpret_cast<int(*)[2]>(lds);   // (before the first tile)
 
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
   const int grp = lane >> 4, ln = lane & 15;
@@ -268,8 +268,8 @@ __global__ __launch_bounds__(64 * RW * KW) __attribute__((amdgpu_waves_per_eu(2)
       vat[u] = at + ((ch ^ vswz(row)) << 4);
     }
   }
-  auto issue = [&](int t, int stage) {
-    const unsigned dst = lds0 + stage * STAGE;
+  auto issue = [&](int t, int buf) {
+    const unsigned kdst = lds0 + buf * TILE, vdst = kdst + 2 * TILE;
     const int ids = t - window < SPAN ? ids0 : ids1, block0 = ((t - window) >> 4) & 63;
     if constexpr (PAGED && UNIFORM) {
 #pragma unroll
@@ -278,11 +278,11 @@ __global__ __launch_bounds__(64 * RW * KW) __attribute__((amdgpu_waves_per_eu(2)
         const int id = __builtin_amdgcn_readlane(ids, block0 + block);
         const size_t at = (size_t)max(id, 0) * page_bytes + (size_t)((t + block * 16) & (slots - 1)) * RB;
         if (a.rblocks == 1) {
-          load_to_lds_once(Kp + at, kat[u], dst + u * W * 1024);
-          load_to_lds_once(Vp + at, vat[u], dst + TILE + u * W * 1024);
+          load_to_lds_once(Kp + at, kat[u], kdst + u * W * 1024);
+          load_to_lds_once(Vp + at, vat[u], vdst + u * W * 1024);
         } else {
-          load_to_lds(Kp + at, kat[u], dst + u * W * 1024);
-          load_to_lds(Vp + at, vat[u], dst + TILE + u * W * 1024);
+          load_to_lds(Kp + at, kat[u], kdst + u * W * 1024);
+          load_to_lds(Vp + at, vat[u], vdst + u * W * 1024);
         }
       }
     } else if (!PAGED && t + BK <= a.n_rows) {
@@ -290,8 +290,8 @@ __global__ __launch_bounds__(64 * RW * KW) __attribute__((amdgpu_waves_per_eu(2)
       asm volatile("s_nop 4" : "+s"(ks), "+s"(vs));     // (a load waits for scalars that vector instructions wrote)
 #pragma unroll
       for (int u = 0; u < NP; ++u) {
-        load_to_lds(ks, kat[u], dst + u * W * 1024);
-        load_to_lds(vs, vat[u], dst + TILE + u * W * 1024);
+        load_to_lds(ks, kat[u], kdst + u * W * 1024);
+        load_to_lds(vs, vat[u], vdst + u * W * 1024);
       }
     } else {                                            // rows past the buffer's: its last again
       int here = lane;
@@ -302,8 +302,8 @@ __global__ __launch_bounds__(64 * RW * KW) __attribute__((amdgpu_waves_per_eu(2)
         size_t at;
         if constexpr (PAGED) at = (size_t)max(__shfl(ids, block0 + row / 16, kWave), 0) * page_bytes + (size_t)((t + row) & (slots - 1)) * RB;
         else at = (size_t)min(t + row, a.n_rows - 1) * ldb;
-        load_to_lds(Kp + at + ((ch ^ kswz(row)) << 4), dst + u * W * 1024);
-        load_to_lds(Vp + at + ((ch ^ vswz(row)) << 4), dst + TILE + u * W * 1024);
+        load_to_lds(Kp + at + ((ch ^ kswz(row)) << 4), kdst + u * W * 1024);
+        load_to_lds(Vp + at + ((ch ^ vswz(row)) << 4), vdst + u * W * 1024);
       }
     }
   };
@@ -366,6 +366,7 @@ __global__ __launch_bounds__(64 * RW * KW) __attribute__((amdgpu_waves_per_eu(2)
       __syncthreads();
       k0 = __builtin_amdgcn_readfirstlane(range[0][0]);
       k1 = __builtin_amdgcn_readfirstlane(range[RW - 1][1]);
+      __syncthreads();                        // (read, before the first tile's loads)
     }
   }
 
@@ -395,8 +396,8 @@ __global__ __launch_bounds__(64 * RW * KW) __attribute__((amdgpu_waves_per_eu(2)
 
   // What lies behind the last key, or on no page, may be anything: its values become zeros (no 0 * NaN).
   const int real_end = PAGED ? len : k1;
-  auto clear = [&](int t, unsigned none_of, int stage) {
-    unsigned char* dst = lds + stage * STAGE + TILE + wave * 1024 + lane * 16;
+  auto clear = [&](int t, unsigned none_of, int buf) {
+    unsigned char* dst = lds + (2 + buf) * TILE + wave * 1024 + lane * 16;
 #pragma unroll
     for (int u = 0; u < NP; ++u) {
       const int row = (u * W + wave) * RPL + lane / CH;
@@ -406,13 +407,13 @@ __global__ __launch_bounds__(64 * RW * KW) __attribute__((amdgpu_waves_per_eu(2)
     }
   };
 
-  float m[QB], l[QB];
+  float m[QB], l[QB], ref[QB];                // ref: what is added to a scaled score, p_shift - m
   floatx4 ls[QB];                             // 16-bit: the sums, by a product with ones
   floatx4 o[CB][QB];                          // O[channel c * 16 + 4 grp + r][row ln]
 #pragma unroll
   for (int q = 0; q < QB; ++q) {
     m[q] = -INFINITY;
-    l[q] = 0.f;
+    l[q] = ref[q] = 0.f;
     ls[q] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int c = 0; c < CB; ++c) o[c][q] = floatx4{0.f, 0.f, 0.f, 0.f};
@@ -432,111 +433,172 @@ __global__ __launch_bounds__(64 * RW * KW) __attribute__((amdgpu_waves_per_eu(2)
     }
   };
 
-  auto compute = [&](int t, unsigned none_of, int stage) {
-    const int t0 = t + kw * TK;
-    if (t0 >= min(hi_last, k1) || t0 + TK <= lo_first) return;
-    const unsigned char* ks = lds + stage * STAGE + kw * TK * RB;
-    const unsigned char* vs = ks + TILE;
-    // Scores: a block's keys are read while the one before is multiplied.
-    constexpr int KR = F8 ? (QK + 1) / 2 : QK;          // 16-byte reads of a lane
-    floatx4 sc[NB][QB];
-    u32x4 kr[2][KR];
-    auto read_k = [&](int j, u32x4 (&x)[KR]) {
-      const int row = 16 * j + ln, f = kswz(kw * TK + row);
-      const unsigned char* krow = ks + row * RB;
-      if constexpr (F8 && DH == 32) {
-        const uint2 w = *reinterpret_cast<const uint2*>(krow + (((grp >> 1) ^ f) << 4) + (grp & 1) * 8);
-        x[0] = u32x4{w.x, w.y, 0, 0};
-      } else {
+  // ---- pieces of a tile's work (ks, vs: the wave's keys and values of a tile) ----
+  // Read i of the KR that a lane takes of a 16-key block's keys; a channel block's values of 32 keys (fp32: 16).
+  constexpr int KR = F8 ? (QK + 1) / 2 : QK;
+  auto read_k = [&](const unsigned char* ks, int j, int i) {
+    const int row = 16 * j + ln, f = kswz(kw * TK + row);
+    const unsigned char* krow = ks + row * RB;
+    if constexpr (F8 && DH == 32) {
+      const uint2 w = *reinterpret_cast<const uint2*>(krow + (((grp >> 1) ^ f) << 4) + (grp & 1) * 8);
+      return u32x4{w.x, w.y, 0, 0};
+    } else {
+      return *reinterpret_cast<const u32x4*>(krow + (((i * 4 + grp) ^ f) << 4));
+    }
+  };
+  auto read_v = [&](const unsigned char* vs, int j, int c) {
+    if constexpr (EB == 4) {
+      const int row = 16 * j + 4 * grp;
+      u32x4 x;
 #pragma unroll
-        for (int i = 0; i < KR; ++i) x[i] = *reinterpret_cast<const u32x4*>(krow + (((i * 4 + grp) ^ f) << 4));
-      }
-    };
-    read_k(0, kr[0]);
+      for (int r = 0; r < 4; ++r)
+        x[r] = *reinterpret_cast<const unsigned*>(vs + (row + r) * RB +
+                                                 (((c * 4 + (ln >> 2)) ^ vswz(kw * TK + row + r)) << 4) + (ln & 3) * 4);
+      return x;
+    } else if constexpr (F8) {
+      const int row = 16 * (j + (ln >> 3)) + 4 * grp + (ln >> 1 & 3), f = vswz(kw * TK + row);
+      const uint2 w = lds_column8(vs + row * RB + (ln & 1) * 8 + ((c ^ f) << 4));
+      return u32x4{w.x, w.y, 0, 0};
+    } else {
+      const int row = 16 * j + 4 * grp + (ln >> 2), f = vswz(kw * TK + row), h = vswz(kw * TK + row + 16);
+      const unsigned char* vrow = vs + row * RB + (ln & 1) * 8;
+      const int ch = 2 * c + (ln >> 1 & 1);
+      const uint2 v0 = lds_column4(vrow + ((ch ^ f) << 4)), v1 = lds_column4(vrow + 16 * RB + ((ch ^ h) << 4));
+      return u32x4{v0.x, v0.y, v1.x, v1.y};
+    }
+  };
+  // One MFMA step of a block's scores; one channel block of the output.
+  auto score = [&](u32x4 kf, int st, floatx4 (&s)[QB]) {
+    if constexpr (F8) {
+      kf = st % 2 ? f8_to_f16x8(kf.z, kf.w) : f8_to_f16x8(kf.x, kf.y);
+      ready(kf);
+    }
 #pragma unroll
-    for (int j = 0; j < NB; ++j) {
-      if (j + 1 < NB) read_k(j + 1, kr[(j + 1) & 1]);
-      __builtin_amdgcn_sched_barrier(0);
-      const u32x4* x = kr[j & 1];
+    for (int q = 0; q < QB; ++q) {
+      if (st == 0) mma0<T>(s[q], kf, qf[q][0]);
+      else mma<T>(s[q], kf, qf[q][st]);
+    }
+  };
+  auto product = [&](u32x4 vf, const u32x4 (&pf)[QB], int c) {
+    if constexpr (F8) {
+      vf = f8_to_f16x8(vf.x, vf.y);
+      ready(vf);
+    }
 #pragma unroll
-      for (int st = 0; st < QK; ++st) {
-        u32x4 kf;
-        if constexpr (F8) {
-          kf = st % 2 ? f8_to_f16x8(x[st / 2].z, x[st / 2].w) : f8_to_f16x8(x[st / 2].x, x[st / 2].y);
-          ready(kf);
-        } else {
-          kf = x[st];
+    for (int q = 0; q < QB; ++q) mma<T>(o[c][q], vf, pf[q]);
+  };
+  // A key that a lane's row does not see counts -inf.  Which ones: an interval of the row's (a tile's
+  // keys against it by comparisons with constants), holes (none_of), a tree's new tokens.  sc: blocks from key t0 on.
+  auto mask = [&](auto& sc, int t0, unsigned none_of) {
+    constexpr int N = sizeof(sc) / sizeof(sc[0]);
+    if (t0 >= lo_last && t0 + 16 * N <= hi_first && !(none_of & ((1u << N) - 1))) return;
+#pragma unroll
+    for (int q = 0; q < QB; ++q) {
+      const int end = hi[q] - t0 - 4 * grp, first = lo[q] - t0 - 4 * grp;
+      unsigned long long tree = 0;                      // bit c: key t0 + 16 j + 4 grp + c, j a multiple of 4
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        if (PAGED && j % 4 == 0) {
+          const int shift = base - t0 - 16 * j - 4 * grp;
+          tree = shift >= 64 || shift <= -64 ? 0 : shift >= 0 ? bits[q] << shift : bits[q] >> -shift;
         }
+        const unsigned part = (unsigned)(tree >> (j * 16 & 63));
+        const bool there = !((none_of >> j) & 1);
 #pragma unroll
-        for (int q = 0; q < QB; ++q) {
-          if (st == 0) mma0<T>(sc[j][q], kf, qf[q][0]);
-          else mma<T>(sc[j][q], kf, qf[q][st]);
+        for (int r = 0; r < 4; ++r) {
+          bool s = 16 * j + r < end;
+          if constexpr (PAGED) s = (s | ((part >> r) & 1)) & there;
+          else s = s & (16 * j + r >= first);
+          sc[j][q][r] = s ? sc[j][q][r] : -INFINITY;
         }
       }
     }
-    // Values: VC channel blocks of 32 keys a group, read a group ahead; the first during the softmax.
-    constexpr int VC = EB == 2 ? (CB < 4 ? CB : 4) : 1, VG = NB / (EB == 2 ? 2 : 1) * (CB / VC);
-    u32x4 vr[2][VC];
-    auto read_v = [&](int g, u32x4 (&x)[VC]) {
-      const int j = g / (CB / VC) * (EB == 2 ? 2 : 1), c0 = g % (CB / VC) * VC;
-      if constexpr (EB == 4) {
-        const int row = 16 * j + 4 * grp;
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-          x[0][r] = *reinterpret_cast<const unsigned*>(vs + (row + r) * RB +
-                                                      (((c0 * 4 + (ln >> 2)) ^ vswz(kw * TK + row + r)) << 4) + (ln & 3) * 4);
-      } else if constexpr (F8) {
-        const int row = 16 * (j + (ln >> 3)) + 4 * grp + (ln >> 1 & 3), f = vswz(kw * TK + row);
-        const unsigned char* vrow = vs + row * RB + (ln & 1) * 8;
-#pragma unroll
-        for (int c = 0; c < VC; ++c) {
-          const uint2 w = lds_column8(vrow + (((c0 + c) ^ f) << 4));
-          x[c] = u32x4{w.x, w.y, 0, 0};
-        }
-      } else {
-        const int row = 16 * j + 4 * grp + (ln >> 2), f = vswz(kw * TK + row), h = vswz(kw * TK + row + 16);
-        const unsigned char* vrow = vs + row * RB + (ln & 1) * 8;
-#pragma unroll
-        for (int c = 0; c < VC; ++c) {
-          const int ch = 2 * (c0 + c) + (ln >> 1 & 1);
-          const uint2 v0 = lds_column4(vrow + ((ch ^ f) << 4)), v1 = lds_column4(vrow + 16 * RB + ((ch ^ h) << 4));
-          x[c] = u32x4{v0.x, v0.y, v1.x, v1.y};
-        }
-      }
-    };
-    read_v(0, vr[0]);
-    settle<NB * QB>(&sc[0][0]);
-    bool whole = t0 >= lo_last && t0 + TK <= hi_first;
-    none_of = (none_of >> (kw * NB)) & ((1u << NB) - 1);
-    whole = whole && !none_of;
-    // A key that a lane's row does not see counts -inf.  Which ones: an interval of the row's (a tile's
-    // keys against it by comparisons with constants), holes, a tree's new tokens.
-    if (!whole) {
-#pragma unroll
-      for (int q = 0; q < QB; ++q) {
-        const int end = hi[q] - t0 - 4 * grp, first = lo[q] - t0 - 4 * grp;
-        unsigned long long tree = 0;                    // bit c: key t0 + 16 j + 4 grp + c, j a multiple of 4
-#pragma unroll
-        for (int j = 0; j < NB; ++j) {
-          if (PAGED && j % 4 == 0) {
-            const int shift = base - t0 - 16 * j - 4 * grp;
-            tree = shift >= 64 || shift <= -64 ? 0 : shift >= 0 ? bits[q] << shift : bits[q] >> -shift;
-          }
-          const unsigned part = (unsigned)(tree >> (j * 16 & 63));
-          const bool there = !((none_of >> j) & 1);
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            bool s = 16 * j + r < end;
-            if constexpr (PAGED) s = (s | ((part >> r) & 1)) & there;
-            else s = s & (16 * j + r >= first);
-            sc[j][q][r] = s ? sc[j][q][r] : -INFINITY;
-          }
-        }
-      }
-    }
-    // the reference moves only when a score passes it by LAZY
-    float top[QB];
+  };
+  // The reference moves only when a score (top: a lane's largest, not scaled) passes it by LAZY.
+  auto move_reference = [&](float (&top)[QB]) {
     bool pass = false;
+#pragma unroll
+    for (int q = 0; q < QB; ++q) {
+      top[q] *= sl;
+      pass = pass || top[q] > m[q] + LAZY;
+    }
+    if (!__ballot(pass)) return;
+    settle<CB * QB>(&o[0][0]);
+    settle<QB>(ls);
+#pragma unroll
+    for (int q = 0; q < QB; ++q) {
+      float x = top[q];
+      x = fmaxf(x, __shfl_xor(x, 16, kWave));
+      x = fmaxf(x, __shfl_xor(x, 32, kWave));
+      const float mn = fmaxf(m[q], x);
+      const float alpha = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[q] - mn);
+      m[q] = mn;
+      ref[q] = mn == -INFINITY ? 0.f : PSH - mn;
+      l[q] *= alpha;
+      ls[q] *= alpha;
+#pragma unroll
+      for (int c = 0; c < CB; ++c) o[c][q] *= alpha;
+    }
+  };
+  auto prob = [&](float s, int q) {
+    const float p = __builtin_amdgcn_exp2f(fmaf(s, sl, ref[q]));
+    if constexpr (EB == 4) l[q] += p;
+    return p;
+  };
+  // Probabilities of 32 keys (fp32: 16) as operands, and their sums.
+  auto pack = [&](const auto& sc, int j, u32x4 (&pf)[QB]) {
+#pragma unroll
+    for (int q = 0; q < QB; ++q) {
+      if constexpr (EB == 2) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int w = 0; w < 2; ++w) pf[q][2 * i + w] = pair_of<T>(sc[j + i][q][2 * w], sc[j + i][q][2 * w + 1]);
+      } else {
+        pf[q] = __builtin_bit_cast(u32x4, sc[j][q]);
+      }
+      ready(pf[q]);
+      if constexpr (EB == 2) mma<T>(ls[q], ones, pf[q]);
+    }
+  };
+  constexpr int SB = EB == 2 ? 2 : 1;                   // 16-key blocks of a step of the second product
+  constexpr int NE = SB * QB * 4;                       // a step's scores of a lane
+  const int see_first = lo_first, see_last = min(hi_last, k1);   // the wave's rows see nothing outside
+
+  auto compute = [&](int t, unsigned none_of, int buf) {
+    const int t0 = t + kw * TK;
+    if (t0 >= see_last || t0 + TK <= see_first) return;
+    const unsigned char* ks = lds + buf * TILE + kw * TK * RB;
+    const unsigned char* vs = lds + (2 + buf) * TILE + kw * TK * RB;
+    // Scores, two blocks at a time in turn (a product waits for the one before it on the same accumulator),
+    // fragments read three products' turns ahead.
+    constexpr int PB = NB > 1 ? 2 : 1, NR = NB * KR, AHEAD = 3;
+    floatx4 sc[NB][QB];
+    u32x4 kr[AHEAD + 1];
+    auto next_k = [&](int i) {
+      if (i < NR) kr[i % (AHEAD + 1)] = read_k(ks, i / (PB * KR) * PB + i % PB, i % (PB * KR) / PB);
+    };
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) next_k(i);
+#pragma unroll
+    for (int i = 0; i < NB * QK; ++i) {
+      const int st = i % (PB * QK) / PB, j = i / (PB * QK) * PB + i % PB;
+      const int read = i / (PB * QK) * PB * KR + (F8 ? st / 2 : st) * PB + i % PB;
+      if (!F8 || st % 2 == 1 || QK == 1) next_k(read + AHEAD);
+      __builtin_amdgcn_sched_barrier(0);
+      score(kr[read % (AHEAD + 1)], st, sc[j]);
+    }
+    // Values are read a group of VC channel blocks ahead, the first during the softmax.
+    constexpr int VC = EB == 2 ? (CB < 4 ? CB : 4) : 1, VG = NB / SB * (CB / VC);
+    u32x4 vr[2][VC];
+    auto read_group = [&](int g) {
+#pragma unroll
+      for (int c = 0; c < VC; ++c) vr[g & 1][c] = read_v(vs, g / (CB / VC) * SB, g % (CB / VC) * VC + c);
+    };
+    read_group(0);
+    settle<NB * QB>(&sc[0][0]);
+    mask(sc, t0, none_of >> (kw * NB));
+    float top[QB];
 #pragma unroll
     for (int q = 0; q < QB; ++q) {
       top[q] = -INFINITY;
@@ -544,90 +606,44 @@ __global__ __launch_bounds__(64 * RW * KW) __attribute__((amdgpu_waves_per_eu(2)
       for (int j = 0; j < NB; ++j)
 #pragma unroll
         for (int r = 0; r < 4; ++r) top[q] = fmaxf(top[q], sc[j][q][r]);
-      top[q] *= sl;
-      pass = pass || top[q] > m[q] + LAZY;
     }
-    if (__ballot(pass)) {
-      settle<CB * QB>(&o[0][0]);
-      settle<QB>(ls);
-#pragma unroll
-      for (int q = 0; q < QB; ++q) {
-        float x = top[q];
-        x = fmaxf(x, __shfl_xor(x, 16, kWave));
-        x = fmaxf(x, __shfl_xor(x, 32, kWave));
-        const float mn = fmaxf(m[q], x);
-        const float alpha = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[q] - mn);
-        m[q] = mn;
-        l[q] *= alpha;
-        ls[q] *= alpha;
-#pragma unroll
-        for (int c = 0; c < CB; ++c) o[c][q] *= alpha;
-      }
-    }
-    float ref[QB];
-#pragma unroll
-    for (int q = 0; q < QB; ++q) ref[q] = m[q] == -INFINITY ? 0.f : PSH - m[q];
-    auto prob = [&](int j, int q, int r) {
-      sc[j][q][r] = __builtin_amdgcn_exp2f(fmaf(sc[j][q][r], sl, ref[q]));
-      if constexpr (EB == 4) l[q] += sc[j][q][r];
-    };
+    move_reference(top);
     // The first step's probabilities, then each step's products with the next one's between them.
-    constexpr int SB = EB == 2 ? 2 : 1;                 // 16-key blocks of a step
-    constexpr int NE = SB * QB * 4, PER = (NE + CB - 1) / CB;   // a step's probabilities of a lane; by channel block
+    constexpr int PER = (NE + CB - 1) / CB;
     auto next_probs = [&](int j, int first) {
 #pragma unroll
-      for (int e = first; e < min(first + PER, NE); ++e) prob(j + e / (QB * 4), e / 4 % QB, e % 4);
+      for (int e = first; e < min(first + PER, NE); ++e) {
+        const int i = j + e / (QB * 4), q = e / 4 % QB, r = e % 4;
+        sc[i][q][r] = prob(sc[i][q][r], q);
+      }
     };
 #pragma unroll
     for (int e = 0; e < NE; e += PER) next_probs(0, e);
 #pragma unroll
     for (int j = 0; j < NB; j += SB) {
       u32x4 pf[QB];
-#pragma unroll
-      for (int q = 0; q < QB; ++q) {
-        if constexpr (EB == 2) {
-#pragma unroll
-          for (int i = 0; i < 2; ++i)
-#pragma unroll
-            for (int w = 0; w < 2; ++w) pf[q][2 * i + w] = pair_of<T>(sc[j + i][q][2 * w], sc[j + i][q][2 * w + 1]);
-        } else {
-          pf[q] = __builtin_bit_cast(u32x4, sc[j][q]);
-        }
-        ready(pf[q]);
-        if constexpr (EB == 2) mma<T>(ls[q], ones, pf[q]);
-      }
+      pack(sc, j, pf);
 #pragma unroll
       for (int c = 0; c < CB; ++c) {
         const int g = j / SB * (CB / VC) + c / VC;
-        if (c % VC == 0 && g + 1 < VG) read_v(g + 1, vr[(g + 1) & 1]);
+        if (c % VC == 0 && g + 1 < VG) read_group(g + 1);
         __builtin_amdgcn_sched_barrier(0);
-        u32x4 vf = vr[g & 1][c % VC];
-        if constexpr (F8) {
-          vf = f8_to_f16x8(vf.x, vf.y);
-          ready(vf);
-        }
-#pragma unroll
-        for (int q = 0; q < QB; ++q) mma<T>(o[c][q], vf, pf[q]);
+        product(vr[g & 1][c % VC], pf, c);
         if (j + SB < NB) next_probs(j + SB, c * PER);
       }
     }
   };
-
-#pragma unroll
-  for (int i = 0; i < STG - 1; ++i)
-    if (k0 + i * BK < k1) issue(k0 + i * BK, i);
-  int stage = 0;
+  if (k0 < k1) issue(k0, 0);
+  int buf = 0;
   for (int t = k0; t < k1; t += BK) {
-    // this tile's loads are done; the STG - 2 tiles behind it may be under way
-    if (t + (STG - 2) * BK < k1) loads_done<2 * NP * (STG - 2)>();
-    else loads_done<0>();
-    unsigned none_of = 0;                               // blocks of the tile without a page
+    loads_done<0>();                                  // this tile's
+    unsigned none_of = 0;                             // blocks of the tile without a page
     if constexpr (PAGED) none_of = (unsigned)(holes >> ((t - window) >> 4)) & (unsigned)((1ull << (BK / 16)) - 1);
-    if (none_of || t + BK > real_end) clear(t, none_of, stage);
+    if (none_of || t + BK > real_end) clear(t, none_of, buf);
     __syncthreads();
-    if (t + (STG - 1) * BK < k1) issue(t + (STG - 1) * BK, stage == 0 ? STG - 1 : stage - 1);
-    compute(t, none_of, stage);
-    stage = stage == STG - 1 ? 0 : stage + 1;
+    if (t + BK < k1) issue(t + BK, buf ^ 1);
+    compute(t, none_of, buf);
+    buf ^= 1;
     if constexpr (PAGED) {
       if (t + BK - window == SPAN) {
         window += SPAN;
@@ -903,7 +919,7 @@ constexpr int rows_keys() {
 template <typename T, int DH, typename KV, bool PAGED, int QB, int RW, int KW>
 hipError_t rows_launch(const RowsAttnArgs& a, unsigned grid, hipStream_t s) {
   constexpr int TK = rows_keys<T, DH, KV, RW, KW>();
-  NT_LAUNCH((attn_rows_kernel<T, DH, KV, PAGED, QB, RW, KW, TK, 2>), dim3(grid), dim3(64 * RW * KW), 0, s, a);
+  NT_LAUNCH((attn_rows_kernel<T, DH, KV, PAGED, QB, RW, KW, TK>), dim3(grid), dim3(64 * RW * KW), 0, s, a);
   return hipGetLastError();
 }
 

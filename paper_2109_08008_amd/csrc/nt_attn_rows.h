@@ -580,6 +580,9 @@ __global__ __launch_bounds__(64 * RW * KW) __attribute__((amdgpu_waves_per_eu(2)
     };
 #pragma unroll
     for (int i = 0; i < AHEAD; ++i) next_k(i);
+    // A wave among its products goes before the SIMD's other wave, whose softmax fills what they leave: 5 %
+    // (one fp16 prompt of 8192 tokens, 32 heads of 128: 1018 -> 971 us; pieces of 256 tokens over 4096: 196 -> 183).
+    __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int i = 0; i < NB * QK; ++i) {
       const int st = i % (PB * QK) / PB, j = i / (PB * QK) * PB + i % PB;
@@ -596,6 +599,7 @@ __global__ __launch_bounds__(64 * RW * KW) __attribute__((amdgpu_waves_per_eu(2)
       for (int c = 0; c < VC; ++c) vr[g & 1][c] = read_v(vs, g / (CB / VC) * SB, g % (CB / VC) * VC + c);
     };
     read_group(0);
+    __builtin_amdgcn_s_setprio(0);
     settle<NB * QB>(&sc[0][0]);
     mask(sc, t0, none_of >> (kw * NB));
     float top[QB];
@@ -619,6 +623,7 @@ __global__ __launch_bounds__(64 * RW * KW) __attribute__((amdgpu_waves_per_eu(2)
     };
 #pragma unroll
     for (int e = 0; e < NE; e += PER) next_probs(0, e);
+    __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int j = 0; j < NB; j += SB) {
       u32x4 pf[QB];
@@ -632,6 +637,7 @@ __global__ __launch_bounds__(64 * RW * KW) __attribute__((amdgpu_waves_per_eu(2)
         if (j + SB < NB) next_probs(j + SB, c * PER);
       }
     }
+    __builtin_amdgcn_s_setprio(0);
   };
   if (k0 < k1) issue(k0, 0);
   int buf = 0;

@@ -112,6 +112,41 @@ def test_long(lens, dtype):
     check(run(x, off, rows, 2, 1, 128, dtype, True, 128 ** -0.5), x, off, 2, 1, 128, dtype, True, 128 ** -0.5)
 
 
+TILES = [(96, 32, [1000, 1, 0, 23]), (64, 16, [300, 0, 129, 65, 6]), (40, 8, [150, 1, 31, 97, 41]), (12, 4, [77, 16, 33, 2])]
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
+@pytest.mark.parametrize("d_head", [32, 64, 128])
+@pytest.mark.parametrize("heads,kv_heads,lens", TILES, ids=["128", "64", "32", "16"])
+def test_each_tile(heads, kv_heads, lens, d_head, dtype, causal):
+    """Heads and rows enough for tiles of 128, 64, 32 and 16 rows, which sequences' ends cut; behind the
+    last sequence, and in its last token's value, stands no number."""
+    import torch
+    x, off, rows = make(lens, heads, kv_heads, d_head, dtype, seed=heads, behind=7)
+    part = (heads + kv_heads) * d_head
+    last = off[-1] - 1
+    x[last, part:] = float("nan")
+    scale = d_head ** -0.5
+    got = run(x, off, rows, heads, kv_heads, d_head, dtype, causal, scale)
+    lo = off[-2]                    # the last sequence's rows: all of them see it, or with causal the last alone
+    hit = got[last if causal else lo:last + 1]
+    assert bool(torch.isnan(hit).all())
+    clean = x.clone()
+    clean[last, part:] = 0
+    q, k, v = split(clean, heads, kv_heads, d_head)
+    for b in range(len(lens)):
+        lo, hi = off[b], off[b + 1]
+        if lo == hi:
+            continue
+        seen = torch.ones(hi - lo, hi - lo, dtype=torch.bool, device="cuda")
+        want, bound = attention(q[lo:hi], k[lo:hi], v[lo:hi], seen.tril() if causal else seen, scale, dtype)
+        n = hi - lo if b + 1 < len(lens) else (hi - lo - 1 if causal else 0)
+        if n:
+            assert_rows(got[lo:lo + n].reshape(n, heads, d_head), want[:n], bound[:n], (b, hi - lo))
+    assert bool((got[off[-1]:] == 7.0).all())
+
+
 @pytest.mark.parametrize("scale", [-0.125, 0.0, 4.0])
 @pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
 def test_scales(scale, dtype):

@@ -61,6 +61,9 @@ def test_prompt_accepts_nothing_to_do_and_refuses_too_much(nt):   # noqa: F811
     assert prompt(nt, n_seqs=5) == nt.NT_OK and prompt(nt, n_rows=5) == nt.NT_OK
     assert prompt(nt, n_seqs=1, n_rows=2 ** 31 - 1) == nt.NT_E_UNSUPPORTED
     assert prompt(nt, n_seqs=2 ** 30 + 1, n_rows=1) == nt.NT_E_UNSUPPORTED
+    assert prompt(nt, kv_ld=1 << 23) == nt.NT_OK and prompt(nt, dtype=0, kv_ld=1 << 22) == nt.NT_OK
+    assert prompt(nt, kv_ld=(1 << 23) + 8) == nt.NT_E_UNSUPPORTED
+    assert prompt(nt, dtype=0, kv_ld=(1 << 22) + 4) == nt.NT_E_UNSUPPORTED
     assert prompt(nt, n_seqs=1, n_rows=1 << 24, n_heads=65536, q_ld=65536 * 64, out_ld=65536 * 64) == nt.NT_E_UNSUPPORTED
 
 

@@ -577,11 +577,11 @@ nt_status nt_op_kv_resize(int32_t page_len, int32_t n_pages, int32_t max_pages, 
  * behind its context: the keys and values of d_path[b][i] go to position d_lens[b] - new + i, new =
  * d_off[b+1] - d_off[b].  d_add[b] becomes the (negative) number of positions then to be given back,
  * kept - new, for nt_op_kv_resize; d_lens is not changed.  A number below its place in the path or not
- * below `new`, and a position without a page, move nothing; a path longer than max_path or `new`
+ * below `new`, and a position below 0 or without a page, move nothing; a path longer than max_path or `new`
  * ends there.  Every other cell of the pools stays as it is.  Pages that two sequences share:
  * as for nt_op_kv_append.  Asynchronous, one launch, on the current device.  NT_E_INVALID for a null
  * pointer, a negative size or a shape the struct does not allow; NT_E_UNSUPPORTED for fp8 with
- * another dtype than NT_F16 or more than 2^31 bytes of keys and values in a position of all sequences. */
+ * another dtype than NT_F16 or more than 2^35 bytes of keys and values in one position of all sequences. */
 nt_status nt_op_kv_keep(const nt_kv_pages* cache, const int32_t* d_off, const int32_t* d_lens, const int32_t* d_path,
                         int32_t max_path, const int32_t* d_n_path, int32_t n_seqs, int32_t* d_add, void* stream);
 

@@ -319,7 +319,7 @@ __global__ __launch_bounds__(256) void kv_keep_kernel(KvKeepArgs a) {
   auto cell_of = [&](long long pos) -> long long {
     const long long i = (pos >> sh) - page0;
     int page = __shfl(pages, (int)(i & (kWave - 1)), kWave);
-    if (i >= kWave) page = page0 + i < a.c.max_pages ? table[page0 + i] : -1;
+    if (i >= kWave) page = page0 + i >= 0 && page0 + i < a.c.max_pages ? table[page0 + i] : -1;
     if (pos < 0 || (unsigned)page >= (unsigned)a.c.n_pages) return -1;
     return (long long)((size_t)page * page_bytes + (size_t)(pos & ((1 << sh) - 1)) * cell);
   };

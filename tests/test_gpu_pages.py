@@ -282,3 +282,17 @@ def test_paths_that_are_none():
     pages = Pages(lens, 2, 64, 16, "f16", seed=1).fill(2)
     compare_keep(pages, [0, 6, 12, 18, 24, 30], [[3]] * 5, [2 ** 31 - 1] * 5)
     compare_keep(pages, [0, 6, 12, 10, 24, 30], [[3]] * 5, [1] * 5)
+
+
+def test_more_new_tokens_than_positions():
+    """A context that begins far below position 0: its new tokens there have no page, nothing before the
+    table is read, and those from position 0 on move."""
+    new, lens = [3000, 2500], [700, 40]
+    pages = Pages(lens, 1, 32, 16, "f16", seed=5).fill(6)
+    path = [list(range(1, 1500)) + list(range(2301, 2800, 3)), list(range(5, 2000))]
+    width = max(len(p) for p in path)
+    n_path = [len(p) for p in path]
+    compare_keep(pages, [0, 3000, 5500], [p + [-1] * (width - len(p)) for p in path], n_path)
+    late = list(range(2400)) + [2450, 2700, 2701, 2999]
+    pages = Pages(lens, 1, 32, 16, "f16", seed=5).fill(6)
+    compare_keep(pages, [0, 3000, 5500], [late, late], [len(late), 2402])

@@ -218,32 +218,32 @@ __global__ __launch_bounds__(THREADS) void resize_fill_kernel(KvResizeArgs a) {
       if (a.off && b < last && blockIdx.y == 0) a.off[b] = v[0] - x[0];
       __syncthreads();
       if (blockIdx.y == 0) {
-        for (int i = take0[0] + (int)threadIdx.x; i < take0[n]; i += THREADS) {
-          const int at[1] = {i};
+        for (unsigned i = take0[0] + threadIdx.x; i < (unsigned)take0[n]; i += THREADS) {   // (i may pass 2^31)
+          const int at[1] = {(int)i};
           int to[1];
           find(take0, n, at, to);
           const int q = to[0];
-          a.table[(size_t)(s0 + q) * a.max_pages + pages_of(len0[q], a.page_shift) + i - take0[q]] = ring(i);
+          a.table[(size_t)(s0 + q) * a.max_pages + pages_of(len0[q], a.page_shift) + (int)i - take0[q]] = ring(i);
         }
-        for (int i = give0[0] + (int)threadIdx.x; i < give0[n]; i += THREADS) {
-          const int num[1] = {i};
+        for (unsigned i = give0[0] + threadIdx.x; i < (unsigned)give0[n]; i += THREADS) {
+          const int num[1] = {(int)i};
           int of[1];
           find(give0, n, num, of);
           const int q = of[0];
           const int p0 = pages_of(len0[q], a.page_shift) - (give0[q + 1] - give0[q]);
-          int* entry = a.table + (size_t)(s0 + q) * a.max_pages + p0 + i - give0[q];
+          int* entry = a.table + (size_t)(s0 + q) * a.max_pages + p0 + (int)i - give0[q];
           const int page = *entry;
           *entry = -1;
-          const unsigned at = (unsigned)count + (unsigned)i;     // behind the tail, below n_pages
+          const unsigned at = (unsigned)count + i;     // behind the tail, below n_pages
           ring(at) = page;
         }
       }
       if (a.pos || a.slot) {
-        const int rows = row0[n], step = (int)gridDim.y * THREADS;
-        for (int r0 = row0[0] + (int)(blockIdx.y * THREADS + threadIdx.x); r0 < rows; r0 += ROWS * step) {
+        const unsigned rows = row0[n], step = gridDim.y * THREADS;      // (r0 may pass 2^31)
+        for (unsigned r0 = row0[0] + blockIdx.y * THREADS + threadIdx.x; r0 < rows; r0 += ROWS * step) {
           int p[ROWS], page[ROWS], r[ROWS], qs[ROWS];
 #pragma unroll
-          for (int u = 0; u < ROWS; ++u) r[u] = min(r0 + u * step, rows - 1);
+          for (int u = 0; u < ROWS; ++u) r[u] = (int)min(r0 + u * step, rows - 1);
           find(row0, n, r, qs);
 #pragma unroll
           for (int u = 0; u < ROWS; ++u) {

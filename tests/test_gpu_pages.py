@@ -170,6 +170,32 @@ def test_one_long_prompt_among_many():
     step(plain, device, -add, 0)
 
 
+def test_rows_up_to_two_to_the_31():
+    """As many new rows as a call can have, less 2^16: their numbers stay below 2^31."""
+    import torch
+    from paper_2109_08008_amd import nt
+    n, each, page = 65536, 32767, 256
+    per = 128
+    i32 = dict(dtype=torch.int32, device="cuda")
+    table, ring = torch.full((n, per), -1, **i32), torch.arange(n * per, **i32)
+    lens, add, state = torch.zeros(n, **i32), torch.full((n,), each, **i32), torch.tensor([0, n * per, 9, 9], **i32)
+    off = torch.empty(n + 1, **i32)
+    rows = 2 ** 31 - 1
+    guard = torch.full((rows + 4096,), 77, **i32)
+    pos = guard[2048:2048 + rows]
+    nt.nt_op_kv_resize(page, n * per, per, table.data_ptr(), lens.data_ptr(), add.data_ptr(), n, ring.data_ptr(),
+                       state.data_ptr(), off.data_ptr(), pos.data_ptr(), None, rows)
+    torch.cuda.synchronize()
+    assert state.tolist() == [0, 0, 0, n * each]
+    assert bool((lens == each).all()) and bool((off == torch.arange(n + 1, **i32) * each).all())
+    assert bool((table.view(-1) == ring).all())
+    want = torch.arange(each, **i32)
+    for b in range(0, n, 4096):                                # 4096 sequences at a time
+        assert bool((pos[b * each:(b + 4096) * each].view(4096, each) == want).all()), b
+    assert bool((pos[n * each:] == -1).all())
+    assert bool((guard[:2048] == 77).all()) and bool((guard[2048 + rows:] == 77).all())
+
+
 def test_resize_in_a_graph():
     """A step's growth and the return of a part of it, captured and replayed; counts change between."""
     import torch

@@ -504,7 +504,8 @@ nt_status nt_op_attn_paged_workspace(const nt_kv_pages* cache, int32_t n_heads, 
  * d_off[b+1] - 1, any number of them, none included; n_rows: rows of the buffers.  Rows of no
  * sequence are not written, and what they hold is never part of a result; nor is what a row
  * does not see, whatever it is (infinities and NaN stay with the rows that see them; a wave's rows
- * where one came out as no number are formed again key by key, at a small part of the speed).
+ * where one came out as no number, or has scores past 2^24, are formed again key by key, at a small
+ * part of the speed).
  * Scores, softmax and sums are fp32; with 16-bit values each probability is rounded once to dtype
  * for the second product (half a step of it), and their sum is that of the rounded ones.  Results
  * do not depend on the other sequences except through where tiles of keys begin (a matter of
@@ -527,10 +528,11 @@ nt_status nt_op_attn_prompt(int32_t dtype, const void* d_q, int32_t q_ld, int32_
  *  d_mask [n_rows] device uint64: new token j where bit j of its word is set (itself only if its
  *   bit is); max_new <= 64.
  * max_new: at least every sequence's new tokens, max_len every length (host; what the work is
- * divided by): rows past max_new are not written, positions past max_len not read.  A row that sees
+ * divided by): a sequence's rows past max_new are not written, positions past max_len not read.  A row that sees
  * nothing is zero; holes, what lies behind a length and what a row does not see are never part of
  * a result, as for nt_op_attn_prompt; rows of no sequence are not written.  Scores, softmax, sums
- * and roundings as there.  fp8 caches as for nt_op_attn_paged.
+ * and roundings as there; into how many parts a length is cut follows from n_seqs, max_new and max_len
+ * (a matter of rounding).  d_out overlaps no input.  fp8 caches as for nt_op_attn_paged.
  * d_ws: workspace of at least nt_op_attn_tree_workspace bytes (256-byte aligned; may be NULL
  * when that is 0), in use until the call's work is done: calls that may overlap need their own.
  * Asynchronous, one or two launches, on the current device.  Refusals as for nt_op_attn_paged, and

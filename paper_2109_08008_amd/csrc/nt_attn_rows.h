@@ -212,8 +212,8 @@ __global__ __launch_bounds__(64 * RW * KW) __attribute__((amdgpu_waves_per_eu(2)
     b = unit / a.c.n_kv_heads;
     r0 = rb * BM;
     row_first = a.off ? min(max(a.off[b], 0), a.n_rows) : b;
-    n_new = a.off ? min(max(min(a.off[b + 1], a.n_rows) - row_first, 0), a.max_new) : 1;
-    n_live = n_new * a.group;                 // rows are (new token, head of the group)
+    n_new = a.off ? max(min(max(a.off[b + 1], 0), a.n_rows) - row_first, 0) : 1;
+    n_live = min(n_new, a.max_new) * a.group;   // rows are (new token, head of the group)
     const int whole = a.lens[b];
     len = max(0, min(whole, a.max_len));
     base = whole - n_new;

@@ -191,6 +191,42 @@ def test_rows_past_max_new_are_not_written():
     assert bool((got[4:9] == 7.0).all()) and bool(torch.isfinite(got).all())
 
 
+@pytest.mark.parametrize("tree", [True, False])
+@pytest.mark.parametrize("max_new", [1, 4, 17])
+def test_rows_up_to_max_new_are_the_same(max_new, tree):
+    """Where a sequence has more new tokens than max_new those before that see what they saw."""
+    import torch
+    new, lens = [20, 3, 40], [60, 70, 300]
+    pages = Pages(lens, 1, 64, 16, "f16", seed=4).fill(5)
+    q = queries(63, 2, 64, "f16")
+    masks = trees(new, 9) if tree else None
+    whole = run(pages, q, new, masks, 0.125)
+    check(whole, pages, q, new, masks, 0.125)
+    got = run(pages, q, new, masks, 0.125, max_new=max_new)
+    row = 0
+    for n in new:
+        m = min(n, max_new)
+        assert bool((got[row + m:row + n] == 7.0).all())
+        got[row + m:row + n] = whole[row + m:row + n]
+        row += n
+    check(got, pages, q, new, masks, 0.125)
+
+
+def test_offsets_that_fall():
+    """Offsets below 0, past the rows or falling write no row outside the buffers, and those of other
+    sequences are as without them."""
+    import torch
+    pages = Pages([60, 70, 80], 1, 64, 16, "f16", seed=4).fill(5)
+    q = queries(12, 2, 64, "f16", behind=4)
+    whole = run(pages, q, [0, 0, 5], None, 0.125)
+    for bad in ([-2 ** 31, -2 ** 31, 0, 5], [2 ** 31 - 1, -2 ** 31, 0, 5], [12, 2 ** 31 - 1, 0, 5]):
+        off = torch.tensor(bad, dtype=torch.int32, device="cuda")
+        guard = torch.full((32, 2, 64), 7.0, dtype=torch.float16, device="cuda")
+        got = run(pages, q, [0, 0, 0], None, 0.125, max_new=5, max_len=80, off=off, out=guard[8:24], n_rows=12)
+        assert torch.equal(got[:5], whole[:5]), bad
+        assert bool((guard[:8] == 7.0).all()) and bool((guard[20:] == 7.0).all()), bad
+
+
 @pytest.mark.parametrize("dtype,fp8", CONFIGS)
 @pytest.mark.parametrize("what", ["value", "key"])
 @pytest.mark.parametrize("new", [6, 40])

@@ -183,7 +183,8 @@ __global__ __launch_bounds__(64 * RW * KW) __attribute__((amdgpu_waves_per_eu(2)
   constexpr int NP = TILE / (W * 1024);       // loads a lane issues for them
   constexpr int RPL = 1024 / RB;              // rows that one load of a wave covers
   constexpr int RPB = RB < 256 ? 256 / RB : 1;   // rows that the 64 banks hold side by side
-  constexpr float PSH = p_shift<T>();
+  constexpr float PSH = p_shift<T>(), P1 = PSH == 0.f ? 1.f : 128.f;   // 2^PSH, a probability of 1
+  static_assert(PSH == 0.f || PSH == 7.f, "P1 is its power");
   static_assert(TILE % (W * 1024) == 0 && NP >= 1, "a tile's rows split evenly over the waves");
   static_assert(EB == 4 || NB % 2 == 0, "16-bit products take 32 keys");
   // LDS: two tiles of keys, two of values; the join of waves that share rows
@@ -672,7 +673,9 @@ __global__ __launch_bounds__(64 * RW * KW) __attribute__((amdgpu_waves_per_eu(2)
   }
 
   // Where a row came out as no number, its wave's rows are formed again key by key, so that a key or
-  // value that is none (or a product that overflows) reaches the rows that see it and no others.
+  // value that is none (or a product that overflows) reaches the rows that see it and no others.  So are
+  // scores past 2^24: a row's largest product and its reference, the same product rounded, differ by
+  // steps of 1 and more, so that its probability is not 1 but may be any, 0 among them.
   {
     float bad = 0.f;
 #pragma unroll
@@ -682,6 +685,7 @@ __global__ __launch_bounds__(64 * RW * KW) __attribute__((amdgpu_waves_per_eu(2)
       for (int c = 0; c < CB; ++c)
 #pragma unroll
         for (int r = 0; r < 4; ++r) x = fmaf(o[c][q][r], 0.f, x);
+      if (m[q] > -INFINITY && l[q] < 0.5f * P1) x = 1.f;
       if (live[q]) bad += x;
     }
     if (__ballot(bad != 0.f)) {
@@ -722,6 +726,7 @@ __global__ __launch_bounds__(64 * RW * KW) __attribute__((amdgpu_waves_per_eu(2)
             s += __shfl_xor(s, 16, kWave);
             s += __shfl_xor(s, 32, kWave);
             s *= a.scale_signed;
+            asm("" : "+v"(s));                          // (rounded once, not fused with the difference below)
             if (sees(q, key)) {
               const float mn = fmaxf(m[q], s), ref = mn == -INFINITY ? 0.f : mn;
               const float alpha = __builtin_amdgcn_exp2f(m[q] - ref), p = __builtin_amdgcn_exp2f(s - ref);
@@ -740,12 +745,11 @@ __global__ __launch_bounds__(64 * RW * KW) __attribute__((amdgpu_waves_per_eu(2)
       }
       // to the scale of the others
       if constexpr (PSH != 0.f) {
-        const float up = __builtin_amdgcn_exp2f(PSH);
 #pragma unroll
         for (int q = 0; q < QB; ++q) {
-          l[q] *= up;
+          l[q] *= P1;
 #pragma unroll
-          for (int c = 0; c < CB; ++c) o[c][q] *= up;
+          for (int c = 0; c < CB; ++c) o[c][q] *= P1;
         }
       }
     }

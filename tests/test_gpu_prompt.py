@@ -182,6 +182,30 @@ def test_a_long_tail_keeps_its_weight():
     assert 3e-3 < float(got[-1].float().mean()) < 4e-3
 
 
+@pytest.mark.parametrize("dtype,size", [("f16", 1e4), ("bf16", 1e6), ("bf16", 1e15), ("f32", 1e6), ("f32", 1e15)])
+@pytest.mark.parametrize("sign", [1, -1])
+def test_scores_past_two_to_the_31(sign, dtype, size):
+    """A token that sees itself alone is its value (to the rounding of a division), however large its score."""
+    import torch
+    from tests.paged_util import EPS
+    n, h, dh = 300, 4, 64
+    x, off, rows = make([1] * n, h, h, dh, dtype, seed=12)
+    x[:, :h * dh] *= size
+    x[:, h * dh:2 * h * dh] *= size
+    got = run(x, off, rows, h, h, dh, dtype, True, sign * 0.7).double()
+    want = x[:, 2 * h * dh:].double()
+    assert bool(((got - want).abs() <= (EPS[dtype] / 2 + 2.0 ** -22) * want.abs()).all())
+    # and two of them, whose scores differ by a good part of themselves: the larger one's value
+    x, off, rows = make([2] * n, 1, 1, dh, dtype, seed=13)
+    x[:, :2 * dh] *= size
+    x[1::2, dh:2 * dh] = x[0::2, dh:2 * dh] * -1
+    got = run(x, off, rows, 1, 1, dh, dtype, False, sign * 0.7).double()
+    q, k, v = split(x, 1, 1, dh)
+    first = (q[:, 0] * k[::2, 0].repeat_interleave(2, 0)).sum(1) * sign > 0
+    want = torch.where(first[:, None], v[::2, 0].repeat_interleave(2, 0), v[1::2, 0].repeat_interleave(2, 0))
+    assert bool(((got - want).abs() <= (EPS[dtype] / 2 + 2.0 ** -22) * want.abs()).all())
+
+
 @pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
 @pytest.mark.parametrize("what", ["nan_value", "inf_value", "nan_key", "inf_key"])
 def test_numbers_stay_with_the_rows_that_see_them(what, dtype):

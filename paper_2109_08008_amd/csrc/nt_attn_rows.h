@@ -129,20 +129,19 @@ template <int N>
 __device__ __forceinline__ void loads_done() { asm volatile("s_waitcnt vmcnt(%0)" ::"i"(N) : "memory"); }
 
 // Which sequences a few neighbouring packed rows belong to: a wave reads 64 of the offsets, a lane one
-// of them, from the last that is at or below its first row (found by 64 probes of all of them) on, and
+// of them, from one that is at or below its first row on (64 probes of what is left at a time find it), and
 // its lanes look their rows up there.
 struct Offsets {
   const int* off;
   int n_seqs, first, mine;                    // first: of the 64; mine: off[first + lane], clamped to the last
   __device__ __forceinline__ Offsets(const int* off_, int n, int row, int lane) : off(off_), n_seqs(n), first(0) {
-    if (n >= kWave) {                         // (uniform)
-      const int step = (n + kWave - 1) / kWave;
-      const int probe = off[min(lane * step, n)];
-      const unsigned long long below = __ballot(probe <= row);
-      first = below ? (63 - __builtin_clzll(below)) * step : 0;
-      while (first + kWave - 1 < n && off[first + kWave - 1] <= row) first += kWave - 1;   // (steps past 64)
+    for (int left = n; left >= kWave;) {      // (uniform) the last one at or below row is in [first, first + left]
+      const int step = (left + kWave - 1) / kWave;
+      const unsigned long long below = __ballot(off[min(first + lane * step, n)] <= row);
+      first += below ? (63 - __builtin_clzll(below)) * step : 0;
+      left = step;
     }
-    mine = off[min(first + lane, n)];
+    mine = n > 0 ? off[min(first + lane, n)] : 0;
   }
   // A lane's row: the last b in [0, n_seqs] with off[b] <= row (0 if there is none; n_seqs: behind the
   // last sequence) and its first and last-but-one rows.

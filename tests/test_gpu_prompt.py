@@ -105,6 +105,20 @@ def test_many_short_sequences(n_seqs, longest):
         assert bool((got[rows - 1:] == 7.0).all())
 
 
+@pytest.mark.parametrize("n_seqs,every", [(4096, 63), (4097, 1000), (300000, 4099), (1 << 20, 99991)])
+def test_few_tokens_in_many_sequences(n_seqs, every):
+    """Most sequences are empty: a row's is found among many equal offsets."""
+    import torch
+    lens = torch.zeros(n_seqs, dtype=torch.int64)
+    lens[every // 2::every] = torch.arange(len(lens[every // 2::every])) % 7 + 1
+    lens[-1] = 5
+    off = torch.cat([torch.zeros(1, dtype=torch.int64), lens.cumsum(0)])
+    short = [int(x) for x in lens[lens > 0]]
+    x, packed, rows = make(short, 2, 1, 32, "f16", seed=n_seqs, behind=3)
+    got = run(x, off.tolist(), rows, 2, 1, 32, "f16", True, 0.2)
+    check(got, x, packed, 2, 1, 32, "f16", True, 0.2)
+
+
 @pytest.mark.parametrize("lens", [[4000], [2048, 1, 3000]], ids=str)
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])
 def test_long(lens, dtype):

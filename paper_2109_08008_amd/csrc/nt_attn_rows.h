@@ -167,6 +167,12 @@ struct Offsets {
   }
 };
 
+// Keys of a part of a sequence's length: about a.chunk, alike in all of them.
+__device__ __forceinline__ int part_keys(const RowsAttnArgs& a, int len) {
+  const int n = max(1, min(a.parts, (len + a.chunk / 2) / a.chunk));
+  return n == 1 ? len : ((len + n - 1) / n + 127) & ~127;
+}
+
 // A workgroup takes BM = RW * QB * 16 query rows; KW waves share the keys of a tile (BK = KW * TK).
 template <typename T, int DH, typename KV, bool PAGED, int QB, int RW, int KW, int TK>
 __global__ __launch_bounds__(64 * RW * KW) __attribute__((amdgpu_waves_per_eu(2))) void attn_rows_kernel(RowsAttnArgs a) {
@@ -351,8 +357,9 @@ __global__ __launch_bounds__(64 * RW * KW) __attribute__((amdgpu_waves_per_eu(2)
   if constexpr (PAGED) {
     if (a.mask) hi_last = len;
     if (row0 >= n_live) hi_last = 0;                    // no rows
-    k0 = part * a.chunk;
-    k1 = min(len, k0 + a.chunk);
+    const int keys = part_keys(a, len);
+    k0 = (int)min((long long)part * keys, (long long)len);
+    k1 = min(len, k0 + keys);
     if (!a.mask) k1 = min(k1, max(0, min(base + (min(r0 + BM, n_live) - 1) / a.group + 1, len)));
     if (k0 >= len && part > 0) return;                  // nothing here; the join does not look
   } else {
@@ -756,7 +763,7 @@ __global__ __launch_bounds__(64 * RW * KW) __attribute__((amdgpu_waves_per_eu(2)
   }
 
   // ---- the rows' outputs ----
-  const bool whole_length = a.parts == 1 || len <= a.chunk;   // (else a part of it, for the join)
+  const bool whole_length = a.parts == 1 || part_keys(a, len) >= len;   // (else a part of it, for the join)
   auto out_row = [&](int r) -> T* {           // of the workgroup's row r
     if constexpr (PAGED) {
       const int i = (r0 + r) / a.group, h = hk * a.group + (r0 + r) - i * a.group;
@@ -850,8 +857,9 @@ __global__ __launch_bounds__(256) void rows_join_kernel(RowsAttnArgs a) {
     if (b >= a.n_seqs || row < first || row - first >= a.max_new) return;   // a row of no sequence, or past max_new
   }
   const int len = max(0, min(a.lens[b], a.max_len));
-  if (len <= a.chunk) return;                   // one part, written where it belongs
-  const int n = (len + a.chunk - 1) / a.chunk;
+  const int keys = part_keys(a, len);
+  if (keys >= len) return;                      // one part, written where it belongs
+  const int n = (len + keys - 1) / keys;
   const size_t stride = (size_t)a.n_rows * a.n_heads;
   const int p0 = lane / COLS, x = lane % COLS * 4;
   const float* ml = a.part_ml + (size_t)item * 2;

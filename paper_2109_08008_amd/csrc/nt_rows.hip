@@ -22,18 +22,22 @@ void attn_prompt_plan(RowsAttnArgs* a) {
 // rows reads the keys again.  Measured, us, with 16 / 64 / 128 rows: 64 requests of 100..4000 bf16
 // positions, 8 key heads of 128 channels (597 MB), 8 rows 110 / 108 / 126, 32 rows 176 / 109 / 117, 1..96 rows
 // - / 157 / 121, 256 rows - / 245 / 200.
-// Lengths are cut into parts of 512 keys' multiples until two workgroups a CU have work; with more than two
-// blocks of rows, where matrix products bound it and a workgroup's own time is long, until six have, so
-// that the ends of ragged batches even out.  Measured, us, uncut / 4096 / 2048 / 1024 keys: 12 requests of
-// 1000..8000 positions and 200..500 new tokens, 4 key heads of four 245 / 184 / 184 / 214, three such
-// 68 / 68 / 61 / 50, forty 555 / 577 / 637 / 731; one of 131001 E4M3 positions, 64 new 3150 / 119 / 95 / 106.
+// Lengths are cut into parts of about chunk keys, a multiple of 512, alike within a sequence (its length
+// decides how many), so that two workgroups a CU have work; with more than two blocks of rows, where matrix
+// products bound it and a workgroup's own time is long, so that six have (the ends of ragged batches even
+// out), but into 8 parts at most, whose join costs less.  Measured, us, uncut / 4096 / 2048 / 1024
+// keys: 12 requests of 1000..8000 positions and 200..500 new tokens, 4 key heads of four 228 / 174 / 164 /
+// 184, forty 498 / 498 / 498 / 511; three such in 3 / 4 / 8 parts 68 / 61 / 51; six of 2000..16000 positions and
+// 500..1000 new, 8 key heads of four, in 1 / 2 / 4 parts 576 / 492 / 507; one of 30000 positions, 512 new, in
+// 8 / 12 / 18 / 25 parts 269 / 279 / 290 / 300; one of 131001 E4M3 positions, 64 new, uncut / 4096 / 2048 /
+// 1024 keys 3150 / 119 / 90 / 106.  With parts of exactly chunk keys and a rest: 187 for the first's 174.
 // Never more than 32768 parts in all, however far max_len is above the lengths.
 void attn_tree_plan(RowsAttnArgs* a) {
   const long long rows = (long long)std::max(a->max_new, 1) * a->group;
   a->tile = rows <= 16 ? ROWS_16 : rows <= 64 ? ROWS_64 : ROWS_128;
   a->rblocks = (int)((rows + (16ll << a->tile) - 1) >> (4 + a->tile));
   const long long tasks = std::max<long long>(1, (long long)a->n_seqs * a->c.n_kv_heads * a->rblocks);
-  const long long want = std::max<long long>(1, (a->rblocks > 2 ? 1536 : 512) / tasks);
+  const long long want = std::max({1ll, 512 / tasks, a->rblocks > 2 ? std::min(8ll, 3200 / tasks) : 0ll});
   const long long least = std::max<long long>(1, a->max_len * tasks / 32768);
   long long chunk = std::max({(a->max_len + want - 1) / want, least, 512ll});
   a->chunk = (int)std::min<long long>((chunk + 511) / 512 * 512, 1 << 30);

@@ -278,6 +278,19 @@ def test_many_sequences():
     check(run(pages, q, new, masks, 0.18), pages, q, new, masks, 0.18)
 
 
+@pytest.mark.parametrize("dtype,fp8", CONFIGS)
+@pytest.mark.parametrize("heads", [1, 3, 4])
+@pytest.mark.parametrize("new", [3, 40])
+def test_parts_of_lengths(new, heads, dtype, fp8):
+    """Lengths around a half and a whole of the 512 keys that a part has at least, uncut, in two and in many."""
+    lens = [3000, 1, 511, 512, 513, 767, 768, 769, 1024, 1279, 1280, 1281, 2999]
+    news = [min(new, n) for n in lens]
+    pages = Pages(lens, 1, 32, 64, dtype, fp8, seed=heads).fill(4)
+    q = queries(sum(news), heads, 32, dtype)
+    for masks in (trees(news, 5), None):
+        check(run(pages, q, news, masks, 0.18), pages, q, news, masks, 0.18)
+
+
 def test_a_length_below_the_new_tokens():
     """Lengths that do not hold all new tokens (the first of them have no position)."""
     new = [6, 6]

@@ -240,7 +240,7 @@ __global__ __launch_bounds__(64 * RW * KW) __attribute__((amdgpu_waves_per_eu(2)
   auto kswz = [](int row) { return (row / RPB) & (CH < 16 ? CH - 1 : 15); };
   auto vswz = [](int row) {
     if constexpr (EB == 4) return ((row >> 2) & 3) * 4 & (CH - 1);
-    else if constexpr (F8) return (row / RPB) & (CH - 1);
+    else if constexpr (F8) return ((row / RPB) & (CH - 1)) ^ (row >> 4 & 1) * (CH / 2);   // (rows of two blocks a read)
     else return ((row / RPB) & (CH / 2 - 1)) * 2;
   };
   const int sh = PAGED ? a.c.page_shift : 0, slots = 1 << sh;

@@ -12,8 +12,9 @@ namespace {
 // ---- resize ----------------------------------------------------------------------------
 // new_b = max(len_b + add_b, 0).  Pages taken, pages given up and new rows are numbered by sums over
 // the sequences before a sequence: every workgroup forms the sums that it needs from the lengths,
-// which nothing writes before all have read them.  A launch bounds a step, the stores of positions and
-// slots a call with many new rows; in between it is the chain of reads, sums and barriers.  The sums are
+// which nothing writes before all have read them.  A launch bounds a step (96 sequences 3.3 us), the
+// stores of positions and slots a call with many new rows (4096 sequences, 1.8 million rows, 22 MB: 16 us and
+// 4.8 for the lengths by a second launch); in between it is the chain of reads, sums and barriers.  The sums are
 // fp64 (2^16 terms below 2^31: exact), which lanes add without LDS.
 struct Need {
   double rows, take, give;                    // new rows; pages taken from and given to the ring
@@ -288,7 +289,8 @@ __global__ __launch_bounds__(RESIZE_MANY) void resize_end_kernel(KvResizeArgs a)
 // A wave moves 64 16-byte pieces of a sequence's rows, of keys and values, U entries of the path at a
 // time.  An entry that is moved lies behind its place, so what is read was not written before.  Short
 // chains bound it: the sequence's numbers, its path and pages (a lane an entry, handed round as
-// scalars), the cells.
+// scalars), the cells.  64 sequences of up to 24 new tokens 4.4 us; 900 of 48..64, 8 heads of 128 bf16
+// channels, 13 us, 53 MB at 4.1 TB/s (a large copy reaches 4.9).
 __global__ __launch_bounds__(256) void kv_keep_kernel(KvKeepArgs a) {
   constexpr int U = 16;
   const int wave = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + threadIdx.x / kWave), lane = threadIdx.x % kWave;

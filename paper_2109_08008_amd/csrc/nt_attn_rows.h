@@ -951,15 +951,16 @@ __global__ __launch_bounds__(256) void rows_join_kernel(RowsAttnArgs a) {
 
 // ---- launches ----------------------------------------------------------------------------
 // Keys of a wave's share of a tile (a load of each wave at least).
-template <typename T, int DH, typename KV, int RW, int KW>
+template <typename T, int DH, typename KV, int QB, int RW, int KW>
 constexpr int rows_keys() {
   constexpr int least = 1024 * RW / (DH * (int)sizeof(KV));
-  return std::max(least, sizeof(T) == 4 ? (KW == 1 ? 32 : 16) : KW == 1 ? 64 : 32);
+  constexpr bool large = KW == 1 && QB == 2;
+  return std::max(least, sizeof(T) == 4 ? (large ? 32 : 16) : large ? 64 : 32);
 }
 
 template <typename T, int DH, typename KV, bool PAGED, int QB, int RW, int KW>
 hipError_t rows_launch(const RowsAttnArgs& a, unsigned grid, hipStream_t s) {
-  constexpr int TK = rows_keys<T, DH, KV, RW, KW>();
+  constexpr int TK = rows_keys<T, DH, KV, QB, RW, KW>();
   NT_LAUNCH((attn_rows_kernel<T, DH, KV, PAGED, QB, RW, KW, TK>), dim3(grid), dim3(64 * RW * KW), 0, s, a);
   return hipGetLastError();
 }
@@ -970,8 +971,13 @@ hipError_t rows_tile(const RowsAttnArgs& a, hipStream_t s) {
                               : (unsigned)(a.rblocks * a.n_heads);
   hipError_t e = hipErrorInvalidValue;
   switch (a.tile) {
-    case ROWS_128: e = rows_launch<T, DH, KV, PAGED, 2, 4, 1>(a, grid, s); break;
+    case ROWS_128:
+      if constexpr (PAGED || DH == 32 || sizeof(T) == 2) e = rows_launch<T, DH, KV, PAGED, 2, 4, 1>(a, grid, s);
+      break;
     case ROWS_64: e = rows_launch<T, DH, KV, PAGED, 2, 2, 2>(a, grid, s); break;
+    case ROWS_64_FINE:
+      if constexpr (!PAGED && DH >= 64) e = rows_launch<T, DH, KV, PAGED, 1, 4, 1>(a, grid, s);
+      break;
     case ROWS_32:
       if constexpr (!PAGED) e = rows_launch<T, DH, KV, PAGED, 2, 1, 4>(a, grid, s);
       break;

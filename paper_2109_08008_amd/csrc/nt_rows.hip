@@ -10,10 +10,19 @@ namespace nt {
 // tiles of 16 / 32 / 64 / 128 rows, one fp16 prompt: 8 heads, d_head 64, 100 tokens 7.1 / 7.1 / 7.8 / 7.8,
 // 300 7.8 / 7.7 / 9.8 / 10.7, 1000 10.1 / 12.1 / 18.5 / 25, 3000 36 / 30 / 45 / 65; 16 heads, d_head 128,
 // 300 10.5 / 10.3 / 12.4 / 13.6, 1000 32 / 23 / 24 / 32, 3000 170 / 109 / 64 / 88, 8000 - / 648 / 335 / 286.
+// Sequences of less than 128 rows on average: waves of 16 rows and tiles of 32 keys pass over fewer keys of
+// other sequences, and four to five workgroups instead of two or three are on a CU.  40000 rows of sequences
+// of 1..n tokens, 16 heads, fp16, tiles of 128 / so, us: n = 8 d_head 32 61 / 60, 64 89 / 83, 128 154 / 138;
+// 150 73 / 75, 107 / 104, 185 / 176; 400 99 / 101, 139 / 144, 243 / 244; 1500 178 / 177, 239 / 272, 416 / 462.
+// fp32 with them at every length, from 64 channels on: n = 8 210 / 148, 418 / 258; 150 344 / 275, 691 / 503;
+// 1500 1486 / 1410, 2886 / 2641.
 void attn_prompt_plan(RowsAttnArgs* a) {
   auto groups = [&](int rows) { return (a->n_rows + (long long)rows - 1) / rows * a->n_heads; };
   a->tile = groups(128) >= 768 ? ROWS_128 : groups(64) >= 512 ? ROWS_64 : groups(32) >= 400 ? ROWS_32 : ROWS_16;
-  a->rblocks = (int)((a->n_rows + (16ll << a->tile) - 1) >> (4 + a->tile));
+  const bool fine = a->tile == ROWS_128 && a->c.d_head >= 64 && (a->c.dt == DT::F32 || a->n_rows < 128ll * a->n_seqs);
+  if (fine) a->tile = ROWS_64_FINE;
+  const int rows = fine ? 64 : 16 << a->tile;
+  a->rblocks = (int)((a->n_rows + (long long)rows - 1) / rows);
   a->parts = 1;
   a->chunk = 0;
 }

@@ -558,7 +558,8 @@ nt_status nt_op_attn_tree_workspace(const nt_kv_pages* cache, int32_t n_heads, i
  *  d_off [n_seqs + 1] or NULL: exclusive sums of max(d_add[b], 0): the new rows of each sequence,
  *   as nt_op_kv_append and nt_op_attn_tree take them.
  *  d_pos [max_rows] int32 or NULL, d_slot [max_rows] int64 or NULL: each new row's position, and
- *   page * page_len + position % page_len of it, the page being the table's; -1 for rows of none.
+ *   page * page_len + position % page_len of it, the page being the table's (below 0 where that is);
+ *   -1 for rows of none.
  * All or nothing: where d_state[2] is not 0 lengths, table and ring stay as they were, d_off is all 0
  * and d_pos and d_slot all -1.  It is the number of pages that the ring lacks, NT_RESIZE_TABLE if a
  * sequence would pass its row of the table (or 2^31 - 1) or the lengths and the ring do not match (more

@@ -22,7 +22,7 @@
 // 58 % and the softmax (a fused multiply-add, an exponential, half a conversion, a maximum an element) most of the
 // rest: 16383 tokens, 16 heads of 128 channels, causal, 0.97 ms = 1.13 PFLOP/s, above what a large fp16
 // product reaches (1.05).  Few rows over a cache: HBM, 5.1 TB/s (64 requests of 100..4000 positions, 8 key
-// heads).  Short sequences: a workgroup's reads in series (offsets, queries, tiles) with three workgroups a CU:
+// heads).  Short sequences: a workgroup's reads in series (offsets, queries, tiles) with five workgroups a CU:
 // 540 of 1..150 tokens, 16 heads of 64: 107 us, 3.1 TB/s.
 #pragma once
 #include <algorithm>

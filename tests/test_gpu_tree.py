@@ -338,6 +338,33 @@ def test_a_graph_of_cut_lengths():
     assert int(full[0]) == 3000
 
 
+def test_two_streams():
+    """Cut lengths on two streams at once, each with a workspace and outputs of its own."""
+    import torch
+    from paper_2109_08008_amd import nt
+    cases = []
+    for i, (new, lens) in enumerate((([5, 12], [3000, 1500]), ([17], [2800]))):
+        pages = Pages(lens, 1, 64, 64, "f16", seed=i).fill(3)
+        q = queries(17, 4, 64, "f16", seed=i, behind=0)
+        masks = trees(new, i)
+        want = run(pages, q, new, masks, 0.125, max_len=3000)
+        check(want, pages, q, new, masks, 0.125)
+        off = torch.tensor([sum(new[:b]) for b in range(len(new) + 1)], dtype=torch.int32, device="cuda")
+        mask = torch.tensor([w for m in masks for w in m], device="cuda")
+        need = nt.nt_op_attn_tree_workspace(pages.cache, 4, len(new), 17, max(new), 3000)
+        ws = torch.full((need,), 0xFF, dtype=torch.uint8, device="cuda")
+        cases.append((pages, q, off, mask, len(new), max(new), need, ws, want, torch.full_like(want, 7.0),
+                      torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    for _ in range(8):
+        for pages, q, off, mask, n, most, need, ws, _, out, st in cases:
+            nt.nt_op_attn_tree(pages.cache, q.data_ptr(), 256, 4, off.data_ptr(), mask.data_ptr(), pages.lens.data_ptr(), n,
+                               17, most, 3000, 0.125, out.data_ptr(), 256, ws.data_ptr(), need, st.cuda_stream)
+    torch.cuda.synchronize()
+    for *_, want, out, _ in cases:
+        assert torch.equal(out, want)
+
+
 def test_pools_past_32_bits():
     """Pages whose distance from the pool's start passes 2^32 bytes."""
     import numpy as np

@@ -981,6 +981,9 @@ hipError_t rows_tile(const RowsAttnArgs& a, hipStream_t s) {
     case ROWS_32:
       if constexpr (!PAGED) e = rows_launch<T, DH, KV, PAGED, 2, 1, 4>(a, grid, s);
       break;
+    case ROWS_16_PAIR:
+      if constexpr (PAGED || DH * sizeof(T) >= 256) e = rows_launch<T, DH, KV, PAGED, 1, 1, 2>(a, grid, s);
+      break;
     case ROWS_16: e = rows_launch<T, DH, KV, PAGED, 1, 1, 4>(a, grid, s); break;
   }
   if constexpr (PAGED) {

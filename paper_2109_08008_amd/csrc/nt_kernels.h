@@ -337,8 +337,9 @@ hipError_t paged_attn(const PagedAttnArgs& a, hipStream_t s);
 // ---------------------------------------------------------------------------------
 // Attention of many query rows (nt_attn_rows.h, nt_rows.hip): packed prompts, and several new
 // tokens a sequence over a paged cache.
-// query rows of a workgroup; ROWS_64_FINE: 16 a wave, as ROWS_16 has them, with the keys shared as in ROWS_128
-enum RowsTile : int { ROWS_16 = 0, ROWS_32 = 1, ROWS_64 = 2, ROWS_128 = 3, ROWS_64_FINE = 4 };
+// query rows of a workgroup; ROWS_64_FINE: 16 a wave, as ROWS_16 has them, with the keys shared as in ROWS_128;
+// ROWS_16_PAIR: by two waves instead of four
+enum RowsTile : int { ROWS_16 = 0, ROWS_32 = 1, ROWS_64 = 2, ROWS_128 = 3, ROWS_64_FINE = 4, ROWS_16_PAIR = 5 };
 struct RowsAttnArgs {
   PagedCache c;               // (prompts: dt, n_kv_heads and d_head only)
   const void* q;              // row i at + i * q_ld, head h at + h * d_head

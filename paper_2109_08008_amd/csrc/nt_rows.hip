@@ -16,6 +16,9 @@ namespace nt {
 // 150 73 / 75, 107 / 104, 185 / 176; 400 99 / 101, 139 / 144, 243 / 244; 1500 178 / 177, 239 / 272, 416 / 462.
 // fp32 with them at every length, from 64 channels on: n = 8 210 / 148, 418 / 258; 150 344 / 275, 691 / 503;
 // 1500 1486 / 1410, 2886 / 2641.
+// Where a workgroup of four waves fills a CU's LDS (keys of 256 bytes and more: 128 KB) and there are more of
+// them than CUs, two waves: 16 heads of 128, fp16 and bf16, 300 tokens 9.2 / 8.6, 450 11.7 / 10.7, 30 sequences of
+// 5..25 9.3 / 6.6; fp32 300 tokens 13.5 / 20.5, the 30 12.1 / 9.2.
 void attn_prompt_plan(RowsAttnArgs* a) {
   auto groups = [&](int rows) { return (a->n_rows + (long long)rows - 1) / rows * a->n_heads; };
   a->tile = groups(128) >= 768 ? ROWS_128 : groups(64) >= 512 ? ROWS_64 : groups(32) >= 400 ? ROWS_32 : ROWS_16;
@@ -23,6 +26,9 @@ void attn_prompt_plan(RowsAttnArgs* a) {
   if (fine) a->tile = ROWS_64_FINE;
   const int rows = fine ? 64 : 16 << a->tile;
   a->rblocks = (int)((a->n_rows + (long long)rows - 1) / rows);
+  if (a->tile == ROWS_16 && a->c.d_head * dt_bytes(a->c.dt) >= 256 && groups(16) > 256 &&
+      (a->c.dt != DT::F32 || a->n_rows < 128ll * a->n_seqs))
+    a->tile = ROWS_16_PAIR;
   a->parts = 1;
   a->chunk = 0;
 }
@@ -41,6 +47,10 @@ void attn_prompt_plan(RowsAttnArgs* a) {
 // 8 / 12 / 18 / 25 parts 269 / 279 / 290 / 300; one of 131001 E4M3 positions, 64 new, uncut / 4096 / 2048 /
 // 1024 keys 3150 / 119 / 90 / 106.  With parts of exactly chunk keys and a rest: 187 for the first's 174.
 // Never more than 32768 parts in all, however far max_len is above the lengths.
+// 16 rows by two waves instead of four, for the same reason as prompts, and for many short sequences: 8 key heads
+// of 128, up to 8 new tokens, 500 requests of 5..100 bf16 positions 88 / 53, of E4M3 44 / 29; 8 of 500..3000 29 / 25,
+// 64 of 100..4000 110 / 108, one of 16000 20.2 / 21.3; of 64 channels 500 of 5..100 37 / 24, 300 of 100..300 33 / 27,
+// 160 of 100..1000 37.8 / 38.1, 256 of 100..4000 174 / 182, 64 of 100..4000 54 / 66, 4 of 13..68 5.8 / 6.9.
 void attn_tree_plan(RowsAttnArgs* a) {
   const long long rows = (long long)std::max(a->max_new, 1) * a->group;
   a->tile = rows <= 16 ? ROWS_16 : rows <= 64 ? ROWS_64 : ROWS_128;
@@ -51,6 +61,8 @@ void attn_tree_plan(RowsAttnArgs* a) {
   long long chunk = std::max({(a->max_len + want - 1) / want, least, 512ll});
   a->chunk = (int)std::min<long long>((chunk + 511) / 512 * 512, 1 << 30);
   a->parts = (int)std::max<long long>(1, (a->max_len + (long long)a->chunk - 1) / a->chunk);
+  const size_t key = a->c.d_head * (a->c.fp8 ? 1 : dt_bytes(a->c.dt));
+  if (a->tile == ROWS_16 && (key >= 256 ? tasks * a->parts > 256 : tasks > 1024 && a->max_len < 1024)) a->tile = ROWS_16_PAIR;
 }
 
 hipError_t attn_prompt(const RowsAttnArgs& a, hipStream_t s) {

@@ -127,13 +127,13 @@ def test_long(lens, dtype):
 
 
 TILES = [(96, 32, [1000, 1, 0, 23]), (64, 16, [300, 0, 129, 65, 6]), (40, 8, [150, 1, 31, 97, 41]), (12, 4, [77, 16, 33, 2]),
-         (96, 32, [33, 1, 16, 0, 140, 64, 17, 63, 65, 2] * 3)]
+         (96, 32, [33, 1, 16, 0, 140, 64, 17, 63, 65, 2] * 3), (24, 8, [40, 1, 17, 33, 16, 15, 65, 2])]
 
 
 @pytest.mark.parametrize("causal", [True, False])
 @pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
 @pytest.mark.parametrize("d_head", [32, 64, 128])
-@pytest.mark.parametrize("heads,kv_heads,lens", TILES, ids=["128", "64", "32", "16", "short"])
+@pytest.mark.parametrize("heads,kv_heads,lens", TILES, ids=["128", "64", "32", "16", "short", "pair"])
 def test_each_tile(heads, kv_heads, lens, d_head, dtype, causal):
     """Heads and rows enough for tiles of 128, 64, 32 and 16 rows and those of short sequences, which ends cut; behind the
     last sequence, and in its last token's value, stands no number."""

@@ -338,6 +338,19 @@ def test_a_graph_of_cut_lengths():
     assert int(full[0]) == 3000
 
 
+@pytest.mark.parametrize("dtype,fp8", CONFIGS)
+@pytest.mark.parametrize("d_head", [32, 64, 128])
+def test_many_short_sequences(d_head, dtype, fp8):
+    """More tasks of few rows than fit the GPU at once; lengths around a tile's 32 and 64 keys."""
+    n = 130
+    new = [(i * 37) % 6 for i in range(n)]
+    lens = [max(new[i], (i * 7919) % 140) for i in range(n)]
+    pages = Pages(lens, 8, d_head, 16, dtype, fp8, seed=3).fill(4)
+    q = queries(sum(new), 8, d_head, dtype)
+    masks = trees(new, 8)
+    check(run(pages, q, new, masks, 0.18), pages, q, new, masks, 0.18)
+
+
 def test_two_streams():
     """Cut lengths on two streams at once, each with a workspace and outputs of its own."""
     import torch

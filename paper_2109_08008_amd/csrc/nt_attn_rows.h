@@ -15,7 +15,7 @@
 //
 // Roundings.  16-bit probabilities are rounded once to the type, for the second product and their sum
 // alike (the sum is a product with ones), which costs at most a quarter of the output's own
-// rounding beside it: 2.0e-4 .. 2.5e-4 from 64 bits (fp16), 1.7e-3 .. 1.9e-3 (bf16), where fp32 throughout
+// rounding beside it: 2.0e-4 .. 2.6e-4 from 64 bits (fp16), 1.7e-3 .. 1.9e-3 (bf16), where fp32 throughout
 // has 2.0e-4 and 1.6e-3.  Two terms of P, as nt_op_attn_paged has them, would be half the products again.
 //
 // What bounds it, one MI355X.  Long rows: the issue of a SIMD's two waves, of which the matrix cores have

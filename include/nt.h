@@ -504,8 +504,9 @@ nt_status nt_op_attn_paged_workspace(const nt_kv_pages* cache, int32_t n_heads, 
  * d_off[b+1] - 1, any number of them, none included; n_rows: rows of the buffers.  Rows of no
  * sequence are not written, and what they hold is never part of a result; nor is what a row
  * does not see, whatever it is (infinities and NaN stay with the rows that see them; a wave's rows
- * where one came out as no number, or has scores past 2^24, are formed again key by key, at a small
- * part of the speed).
+ * where one came out as no number, has scores past 2^24, or weighted values whose sum passes fp32's
+ * largest number, are formed again key by key, at a small part of the speed).  Finite values have a finite
+ * average (but in fp32 for one within its roundings of the largest number).
  * Scores, softmax and sums are fp32; with 16-bit values each probability is rounded once to dtype
  * for the second product (half a step of it), and their sum is that of the rounded ones.  Results
  * do not depend on the other sequences except through where tiles of keys begin (a matter of

@@ -701,10 +701,17 @@ __global__ __launch_bounds__(64 * RW * KW) __attribute__((amdgpu_waves_per_eu(2)
     }
   }
 
+  // From here on o is the average of the values, which l weighs in a join: a sum of finite values may pass
+  // fp32's largest number, an average of them does not.
+  float inv[QB];
+#pragma unroll
+  for (int q = 0; q < QB; ++q) inv[q] = l[q] == 0.f ? 0.f : 1.0f / l[q];
+
   // Where a row came out as no number, its wave's rows are formed again key by key, so that a key or
   // value that is none (or a product that overflows) reaches the rows that see it and no others.  So are
   // scores past 2^24: a row's largest product and its reference, the same product rounded, differ by
-  // steps of 1 and more, so that its probability is not 1 but may be any, 0 among them.
+  // steps of 1 and more, so that its probability is not 1 but may be any, 0 among them.  So are sums of values
+  // that overflow: here o is the sum times the power of two that brings l into [1/4, 1/2), `down`.
   {
     float bad = 0.f;
 #pragma unroll
@@ -718,10 +725,12 @@ __global__ __launch_bounds__(64 * RW * KW) __attribute__((amdgpu_waves_per_eu(2)
       if (live[q]) bad += x;
     }
     if (__ballot(bad != 0.f)) {
+      float up[QB];                                     // 1 / down
 #pragma unroll
       for (int q = 0; q < QB; ++q) {
         m[q] = -INFINITY;
         l[q] = 0.f;
+        up[q] = 1.f;
 #pragma unroll
         for (int c = 0; c < CB; ++c) o[c][q] = floatx4{0.f, 0.f, 0.f, 0.f};
       }
@@ -761,25 +770,24 @@ __global__ __launch_bounds__(64 * RW * KW) __attribute__((amdgpu_waves_per_eu(2)
               const float alpha = __builtin_amdgcn_exp2f(m[q] - ref), p = __builtin_amdgcn_exp2f(s - ref);
               m[q] = mn;
               l[q] = l[q] * alpha + p;
+              const int e = __builtin_bit_cast(int, fmaxf(l[q], 1.f)) >> 23;   // (NaN counts as 1)
+              const float down = __builtin_bit_cast(float, (252 - e) << 23), f = alpha * (down * up[q]);
+              up[q] = __builtin_bit_cast(float, (e + 2) << 23);
 #pragma unroll
               for (int c = 0; c < CB; ++c) {
                 float v[4];
                 four_values<KV>(vp + (c * 16 + 4 * grp) * EC, v);
 #pragma unroll
-                for (int r = 0; r < 4; ++r) o[c][q][r] = fmaf(p, v[r], o[c][q][r] * alpha);
+                for (int r = 0; r < 4; ++r) o[c][q][r] = fmaf(p, v[r] * down, o[c][q][r] * f);
               }
             }
           }
         }
       }
-      // to the scale of the others
-      if constexpr (PSH != 0.f) {
 #pragma unroll
-        for (int q = 0; q < QB; ++q) {
-          l[q] *= P1;
-#pragma unroll
-          for (int c = 0; c < CB; ++c) o[c][q] *= P1;
-        }
+      for (int q = 0; q < QB; ++q) {
+        inv[q] = l[q] == 0.f ? 0.f : up[q] / l[q];
+        l[q] *= P1;                                     // to the scale of the others
       }
     }
   }
@@ -798,8 +806,8 @@ __global__ __launch_bounds__(64 * RW * KW) __attribute__((amdgpu_waves_per_eu(2)
     const int i = (r0 + r) / a.group, h = hk * a.group + (r0 + r) - i * a.group;
     return ((size_t)part * a.n_rows + row_first + i) * a.n_heads + h;
   };
-  auto store4 = [&](int r, int x, floatx4 s, float inv) {
-    alignas(16) T t4[4] = {from_f32<T>(s.x * inv), from_f32<T>(s.y * inv), from_f32<T>(s.z * inv), from_f32<T>(s.w * inv)};
+  auto store4 = [&](int r, int x, floatx4 s) {
+    alignas(16) T t4[4] = {from_f32<T>(s.x), from_f32<T>(s.y), from_f32<T>(s.z), from_f32<T>(s.w)};
     T* p = out_row(r) + x;
     if constexpr (EB == 2) *reinterpret_cast<uint2*>(p) = *reinterpret_cast<const uint2*>(t4);
     else *reinterpret_cast<uint4*>(p) = *reinterpret_cast<const uint4*>(t4);
@@ -810,13 +818,12 @@ __global__ __launch_bounds__(64 * RW * KW) __attribute__((amdgpu_waves_per_eu(2)
       const int r = (rw * QB + q) * 16 + ln;
       if (!live[q]) continue;
       if (!PAGED || whole_length) {
-        const float inv = l[q] == 0.f ? 0.f : 1.0f / l[q];
 #pragma unroll
-        for (int c = 0; c < CB; ++c) store4(r, c * 16 + 4 * grp, o[c][q], inv);
+        for (int c = 0; c < CB; ++c) store4(r, c * 16 + 4 * grp, o[c][q] * inv[q]);
       } else {
         const size_t pr = part_row(r);
 #pragma unroll
-        for (int c = 0; c < CB; ++c) *reinterpret_cast<floatx4*>(a.part_o + pr * DH + c * 16 + 4 * grp) = o[c][q];
+        for (int c = 0; c < CB; ++c) *reinterpret_cast<floatx4*>(a.part_o + pr * DH + c * 16 + 4 * grp) = o[c][q] * inv[q];
         if (grp == 0) *reinterpret_cast<float2*>(a.part_ml + pr * 2) = make_float2(m[q], l[q]);
       }
     }
@@ -832,7 +839,7 @@ __global__ __launch_bounds__(64 * RW * KW) __attribute__((amdgpu_waves_per_eu(2)
       }
 #pragma unroll
       for (int c = 0; c < CB; ++c)
-        *reinterpret_cast<floatx4*>(jo + ((wave * QB + q) * 16 + ln) * DH + (((c * 4 + grp) ^ (ln & 7)) << 2)) = o[c][q];
+        *reinterpret_cast<floatx4*>(jo + ((wave * QB + q) * 16 + ln) * DH + (((c * 4 + grp) ^ (ln & 7)) << 2)) = o[c][q] * inv[q];
     }
     __syncthreads();
     for (int e = threadIdx.x; e < BM * (DH / 4); e += 64 * W) {
@@ -843,16 +850,19 @@ __global__ __launch_bounds__(64 * RW * KW) __attribute__((amdgpu_waves_per_eu(2)
 #pragma unroll
       for (int w = 1; w < KW; ++w) mm = fmaxf(mm, jm[w0 + w][i]);
       const float ref = mm == -INFINITY ? 0.f : mm;
-      float z = 0.f;
-      floatx4 s = floatx4{0.f, 0.f, 0.f, 0.f};
+      float f[KW], z = 0.f;
 #pragma unroll
       for (int w = 0; w < KW; ++w) {
-        const float f = __builtin_amdgcn_exp2f(jm[w0 + w][i] - ref);
-        z += f * jl[w0 + w][i];
-        s += f * *reinterpret_cast<const floatx4*>(jo + ((w0 + w) * QB * 16 + i) * DH + ((x ^ (i & 7)) << 2));
+        f[w] = __builtin_amdgcn_exp2f(jm[w0 + w][i] - ref) * jl[w0 + w][i];
+        z += f[w];
       }
+      const float iz = z == 0.f ? 0.f : 1.0f / z;
+      floatx4 s = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int w = 0; w < KW; ++w)
+        s += f[w] * iz * *reinterpret_cast<const floatx4*>(jo + ((w0 + w) * QB * 16 + i) * DH + ((x ^ (i & 7)) << 2));
       if (!PAGED || whole_length) {
-        store4(r, x * 4, s, z == 0.f ? 0.f : 1.0f / z);
+        store4(r, x * 4, s);
       } else {
         const size_t pr = part_row(r);
         *reinterpret_cast<floatx4*>(a.part_o + pr * DH + x * 4) = s;
@@ -861,7 +871,7 @@ __global__ __launch_bounds__(64 * RW * KW) __attribute__((amdgpu_waves_per_eu(2)
     }
   }
 }
-// Merges the parts of ITEMS heads of a new row: a wave, DH / 4 lanes four channels each of every
+// Merges the parts of ITEMS heads of a new row (averages of values and what weighs them): a wave, DH / 4 lanes four channels each of every
 // (256 / DH)-th part, ITEMS * U parts' loads in flight.  Bound by HBM and a launch: 64 rows of 16 heads in 64
 // parts (34 MB) 9 us, 4100 rows in 2..3 parts 14 us.
 template <typename T, int DH, int ITEMS>
@@ -915,15 +925,19 @@ __global__ __launch_bounds__(256) void rows_join_kernel(RowsAttnArgs a) {
         if (p + u * ROWS >= n) w[i][u] = make_float2(-INFINITY, 0.f);
         mn = fmaxf(mn, w[i][u].x);
       }
-      const float ref = mn == -INFINITY ? 0.f : mn, f0 = __builtin_amdgcn_exp2f(m[i] - ref);
-      l[i] *= f0;
-      s[i] *= f0;
+      const float ref = mn == -INFINITY ? 0.f : mn, l0 = l[i] * __builtin_amdgcn_exp2f(m[i] - ref);
+      float f[U];
+      l[i] = l0;
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const float f = __builtin_amdgcn_exp2f(w[i][u].x - ref);
-        l[i] += f * w[i][u].y;
-        if (p + u * ROWS < n) s[i] += f * v[i][u];      // (a part past the last is the last one's again)
+        f[u] = __builtin_amdgcn_exp2f(w[i][u].x - ref) * w[i][u].y;
+        l[i] += f[u];
       }
+      const float inv = l[i] == 0.f ? 0.f : 1.0f / l[i];
+      s[i] *= l0 * inv;
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (p + u * ROWS < n) s[i] += f[u] * inv * v[i][u];   // (a part past the last is the last one's again)
       m[i] = mn;
     }
   }
@@ -933,16 +947,15 @@ __global__ __launch_bounds__(256) void rows_join_kernel(RowsAttnArgs a) {
     for (int d = COLS; d < kWave; d *= 2) {
       const float mo = __shfl_xor(m[i], d, kWave), lo = __shfl_xor(l[i], d, kWave);
       const float mn = fmaxf(m[i], mo), ref = mn == -INFINITY ? 0.f : mn;
-      const float f = __builtin_amdgcn_exp2f(m[i] - ref), g = __builtin_amdgcn_exp2f(mo - ref);
-      l[i] = l[i] * f + lo * g;
+      const float f = l[i] * __builtin_amdgcn_exp2f(m[i] - ref), g = lo * __builtin_amdgcn_exp2f(mo - ref);
+      l[i] = f + g;
+      const float inv = l[i] == 0.f ? 0.f : 1.0f / l[i];
 #pragma unroll
-      for (int r = 0; r < 4; ++r) s[i][r] = s[i][r] * f + __shfl_xor(s[i][r], d, kWave) * g;
+      for (int r = 0; r < 4; ++r) s[i][r] = s[i][r] * (f * inv) + __shfl_xor(s[i][r], d, kWave) * (g * inv);
       m[i] = mn;
     }
     if (lane >= COLS) continue;
-    const float inv = l[i] == 0.f ? 0.f : 1.0f / l[i];
-    alignas(16) T t4[4] = {from_f32<T>(s[i].x * inv), from_f32<T>(s[i].y * inv), from_f32<T>(s[i].z * inv),
-                           from_f32<T>(s[i].w * inv)};
+    alignas(16) T t4[4] = {from_f32<T>(s[i].x), from_f32<T>(s[i].y), from_f32<T>(s[i].z), from_f32<T>(s[i].w)};
     T* out = static_cast<T*>(a.out) + (size_t)row * a.out_ld + (size_t)(h0 + i) * DH + x;
     if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(out) = *reinterpret_cast<const uint2*>(t4);
     else *reinterpret_cast<uint4*>(out) = *reinterpret_cast<const uint4*>(t4);

@@ -360,7 +360,7 @@ struct RowsAttnArgs {
   // the call's cut (attn_prompt_plan, attn_tree_plan): a RowsTile; blocks of query rows (a key
   // head's, or the packed rows'); parts of `chunk` keys
   int tile, rblocks, parts, chunk;
-  float* part_o;              // parts > 1: [parts][n_rows][n_heads][d_head] and (max, sum) of each
+  float* part_o;              // parts > 1: [parts][n_rows][n_heads][d_head] averages and (max, sum) of each
   float* part_ml;
 };
 // Fill the cut from the sizes.  Host only.

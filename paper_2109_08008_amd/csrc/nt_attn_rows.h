@@ -124,6 +124,14 @@ constexpr float p_shift() {
   return std::is_same<T, f16>::value ? 7.f : 0.f;
 }
 
+// The weight of a wave's or part's sums, whose largest score is m, beside those of largest score top.  A row whose
+// scores are all -inf has a sum that is not 0 and no average; it comes out as no number unless another
+// part has a score above.
+__device__ __forceinline__ float share_of(float m, float top) {
+  return top == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - top);
+}
+__device__ __forceinline__ bool no_average(float m, float l) { return m == -INFINITY && l != 0.f; }
+
 // 16 bytes a lane, 1024 consecutive ones of LDS from dst on.  The compiler does not see the load: it
 // would wait for all of them before the next read of LDS, whatever that reads.
 __device__ __forceinline__ void load_to_lds(const char* base, unsigned at, unsigned dst) {
@@ -711,9 +719,11 @@ __global__ __launch_bounds__(64 * RW * KW) __attribute__((amdgpu_waves_per_eu(2)
   // value that is none (or a product that overflows) reaches the rows that see it and no others.  So are
   // scores past 2^24: a row's largest product and its reference, the same product rounded, differ by
   // steps of 1 and more, so that its probability is not 1 but may be any, 0 among them.  So are sums of values
-  // that overflow: here o is the sum times the power of two that brings l into [1/4, 1/2), `down`.
+  // that overflow: here o is the sum times the power of two that brings l into [1/4, 1/2), `down`.  And so are
+  // rows that came out with nothing though they see some of the wave's keys: with scores of -inf.
   {
     float bad = 0.f;
+    bool nothing = false;
 #pragma unroll
     for (int q = 0; q < QB; ++q) {
       float x = l[q] * 0.f;
@@ -723,6 +733,21 @@ __global__ __launch_bounds__(64 * RW * KW) __attribute__((amdgpu_waves_per_eu(2)
         for (int r = 0; r < 4; ++r) x = fmaf(o[c][q][r], 0.f, x);
       if (m[q] > -INFINITY && l[q] < 0.5f * P1) x = 1.f;
       if (live[q]) bad += x;
+      nothing |= live[q] & (m[q] == -INFINITY);
+    }
+    if (__ballot(nothing)) {
+      auto below = [&](int x) {                         // the wave's keys below x
+        const int d = max(x, k0) - k0;
+        return d / BK * TK + min(max(d % BK - kw * TK, 0), TK);
+      };
+      unsigned long long mine = 0;                      // of a tree's new tokens
+      if (PAGED && a.mask) {
+        const int key = (int)((unsigned)base + lane);
+        mine = __ballot(key >= k0 && key < k1 && below(key + 1) > below(key));
+      }
+#pragma unroll
+      for (int q = 0; q < QB; ++q)
+        if (live[q] && m[q] == -INFINITY && ((bits[q] & mine) || below(min(hi[q], k1)) > below(lo[q]))) bad += 1.f;
     }
     if (__ballot(bad != 0.f)) {
       float up[QB];                                     // 1 / down
@@ -741,7 +766,10 @@ __global__ __launch_bounds__(64 * RW * KW) __attribute__((amdgpu_waves_per_eu(2)
           const char *kp, *vp;
           if constexpr (PAGED) {
             const int id = table[min(key >> sh, a.c.max_pages - 1)];
-            if ((unsigned)id >= (unsigned)a.c.n_pages) continue;
+            if ((unsigned)id >= (unsigned)a.c.n_pages) {
+              key |= 15;                                // (the rest of the block has none either)
+              continue;
+            }
             const size_t at = (size_t)id * page_bytes + (size_t)(key & (slots - 1)) * RB;
             kp = Kp + at;
             vp = Vp + at;
@@ -770,6 +798,7 @@ __global__ __launch_bounds__(64 * RW * KW) __attribute__((amdgpu_waves_per_eu(2)
               const float alpha = __builtin_amdgcn_exp2f(m[q] - ref), p = __builtin_amdgcn_exp2f(s - ref);
               m[q] = mn;
               l[q] = l[q] * alpha + p;
+              if (mn == -INFINITY && l[q] == 0.f) l[q] = 1.f;   // it sees a key
               const int e = __builtin_bit_cast(int, fmaxf(l[q], 1.f)) >> 23;   // (NaN counts as 1)
               const float down = __builtin_bit_cast(float, (252 - e) << 23), f = alpha * (down * up[q]);
               up[q] = __builtin_bit_cast(float, (e + 2) << 23);
@@ -818,6 +847,7 @@ __global__ __launch_bounds__(64 * RW * KW) __attribute__((amdgpu_waves_per_eu(2)
       const int r = (rw * QB + q) * 16 + ln;
       if (!live[q]) continue;
       if (!PAGED || whole_length) {
+        if (no_average(m[q], l[q])) inv[q] = NAN;
 #pragma unroll
         for (int c = 0; c < CB; ++c) store4(r, c * 16 + 4 * grp, o[c][q] * inv[q]);
       } else {
@@ -849,11 +879,10 @@ __global__ __launch_bounds__(64 * RW * KW) __attribute__((amdgpu_waves_per_eu(2)
       float mm = jm[w0][i];
 #pragma unroll
       for (int w = 1; w < KW; ++w) mm = fmaxf(mm, jm[w0 + w][i]);
-      const float ref = mm == -INFINITY ? 0.f : mm;
       float f[KW], z = 0.f;
 #pragma unroll
       for (int w = 0; w < KW; ++w) {
-        f[w] = __builtin_amdgcn_exp2f(jm[w0 + w][i] - ref) * jl[w0 + w][i];
+        f[w] = share_of(jm[w0 + w][i], mm) * jl[w0 + w][i];
         z += f[w];
       }
       const float iz = z == 0.f ? 0.f : 1.0f / z;
@@ -862,6 +891,7 @@ __global__ __launch_bounds__(64 * RW * KW) __attribute__((amdgpu_waves_per_eu(2)
       for (int w = 0; w < KW; ++w)
         s += f[w] * iz * *reinterpret_cast<const floatx4*>(jo + ((w0 + w) * QB * 16 + i) * DH + ((x ^ (i & 7)) << 2));
       if (!PAGED || whole_length) {
+        if (no_average(mm, z)) s = floatx4{NAN, NAN, NAN, NAN};
         store4(r, x * 4, s);
       } else {
         const size_t pr = part_row(r);
@@ -925,12 +955,12 @@ __global__ __launch_bounds__(256) void rows_join_kernel(RowsAttnArgs a) {
         if (p + u * ROWS >= n) w[i][u] = make_float2(-INFINITY, 0.f);
         mn = fmaxf(mn, w[i][u].x);
       }
-      const float ref = mn == -INFINITY ? 0.f : mn, l0 = l[i] * __builtin_amdgcn_exp2f(m[i] - ref);
+      const float l0 = l[i] * share_of(m[i], mn);
       float f[U];
       l[i] = l0;
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        f[u] = __builtin_amdgcn_exp2f(w[i][u].x - ref) * w[i][u].y;
+        f[u] = share_of(w[i][u].x, mn) * w[i][u].y;
         l[i] += f[u];
       }
       const float inv = l[i] == 0.f ? 0.f : 1.0f / l[i];
@@ -946,8 +976,7 @@ __global__ __launch_bounds__(256) void rows_join_kernel(RowsAttnArgs a) {
 #pragma unroll
     for (int d = COLS; d < kWave; d *= 2) {
       const float mo = __shfl_xor(m[i], d, kWave), lo = __shfl_xor(l[i], d, kWave);
-      const float mn = fmaxf(m[i], mo), ref = mn == -INFINITY ? 0.f : mn;
-      const float f = l[i] * __builtin_amdgcn_exp2f(m[i] - ref), g = lo * __builtin_amdgcn_exp2f(mo - ref);
+      const float mn = fmaxf(m[i], mo), f = l[i] * share_of(m[i], mn), g = lo * share_of(mo, mn);
       l[i] = f + g;
       const float inv = l[i] == 0.f ? 0.f : 1.0f / l[i];
 #pragma unroll
@@ -955,6 +984,7 @@ __global__ __launch_bounds__(256) void rows_join_kernel(RowsAttnArgs a) {
       m[i] = mn;
     }
     if (lane >= COLS) continue;
+    if (no_average(m[i], l[i])) s[i] = floatx4{NAN, NAN, NAN, NAN};
     alignas(16) T t4[4] = {from_f32<T>(s[i].x), from_f32<T>(s[i].y), from_f32<T>(s[i].z), from_f32<T>(s[i].w)};
     T* out = static_cast<T*>(a.out) + (size_t)row * a.out_ld + (size_t)(h0 + i) * DH + x;
     if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(out) = *reinterpret_cast<const uint2*>(t4);

@@ -3,8 +3,9 @@ shared out: over a tile's waves, over parts of a length, over neither."""
 import pytest
 
 from tests.paged_util import Pages, torch_dtype
-from tests.test_gpu_prompt import check as check_prompt, make, run as run_prompt
-from tests.test_gpu_tree import check as check_tree, queries, run as run_tree, trees
+from tests.rows_util import assert_rows, attention
+from tests.test_gpu_prompt import check as check_prompt, make, run as run_prompt, split
+from tests.test_gpu_tree import cells, check as check_tree, queries, run as run_tree, trees
 
 pytestmark = pytest.mark.gpu
 
@@ -70,3 +71,104 @@ def test_large_values_over_a_cache(size, lens, group, new, dtype):
         check_tree(run_tree(pages, q, news, masks, 0.125, n_rows=2 * new), pages, q, news, masks, 0.125)
     pages.v.abs_()
     check_tree(run_tree(pages, q, news, None, 0.125, n_rows=2 * new), pages, q, news, None, 0.125)
+
+
+# ---- scores of -inf -------------------------------------------------------------------
+# A softmax over scores of -inf alone is no number; beside one finite score they weigh nothing.
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
+@pytest.mark.parametrize("heads,lens", PROMPTS, ids=PROMPT_IDS)
+def test_nothing_but_scores_of_minus_infinity(heads, lens, dtype, causal):
+    """Every second sequence has keys of -inf: all of them, or (the third, seventh ..) all but the last."""
+    import torch
+    dh, hkv = 128 if heads == 24 else 64, heads // 8 or 1
+    heads = hkv * 8 if heads > 8 else heads
+    x, off, rows = make(lens, heads, hkv, dh, dtype, seed=heads)
+    x[:, :heads * dh:dh] = x[:, :heads * dh:dh].abs() + 0.5          # channel 0 of every query is positive
+    for b in range(0, len(lens), 2):
+        end = off[b + 1] - (1 if b % 4 == 2 else 0)
+        x[off[b]:end, heads * dh:(heads + hkv) * dh:dh] = float("-inf")
+    got = run_prompt(x, off, rows, heads, hkv, dh, dtype, causal, 0.1)
+    q, k, v = split(torch.where(torch.isinf(x), torch.zeros_like(x), x), heads, hkv, dh)
+    for b, n in enumerate(lens):
+        lo, hi = off[b], off[b + 1]
+        seen = torch.ones(n, n, dtype=torch.bool, device="cuda")
+        seen = seen.tril() if causal else seen
+        if b % 2 == 0:
+            seen[:, :n - (1 if b % 4 == 2 else 0)] = False
+        want, bound = attention(q[lo:hi], k[lo:hi], v[lo:hi], seen, 0.1, dtype)
+        some = seen.any(1)
+        mine = got[lo:hi].reshape(n, heads, dh)
+        assert bool(torch.isnan(mine[~some]).all()), (b, n)
+        if bool(some.any()):
+            assert_rows(mine[some], want[some], bound[some], (b, n))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_scores_that_overflow_downwards(dtype):
+    """Finite queries and keys whose product is below fp32's range: no number, as above it."""
+    import torch
+    lens, dh = [20, 70], 64
+    for sign in (1, -1):
+        x, off, rows = make(lens, 1, 1, dh, dtype, seed=2)
+        x[:20, :dh] = 1e25
+        x[:20, dh:2 * dh] = sign * 1e25
+        got = run_prompt(x, off, rows, 1, 1, dh, dtype, True, 0.1)
+        assert bool(torch.isnan(got[:20]).all())
+        q, k, v = split(x[20:], 1, 1, dh)
+        seen = torch.ones(70, 70, dtype=torch.bool, device="cuda").tril()
+        want, bound = attention(q, k, v, seen, 0.1, dtype)
+        assert_rows(got[20:].reshape(70, 1, dh), want, bound)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
+@pytest.mark.parametrize("group,new", [(1, 3), (4, 4), (4, 16), (4, 40)])
+@pytest.mark.parametrize("length", [50, 250, 5003])
+@pytest.mark.parametrize("tree", [True, False])
+def test_scores_of_minus_infinity_over_a_cache(tree, length, group, new, dtype):
+    """Keys of -inf in the whole context, in most of it (parts that hold nothing else), and in new tokens."""
+    import torch
+    base = length - new
+    masks = [[1 << i for i in range(new)]] if tree else None        # tokens that see the context and themselves
+    q = queries(new, group, 64, dtype, behind=0)
+    q[:, :, 0] = q[:, :, 0].abs() + 0.5
+    for finite in ([], [0], [base - 1], [base + 1], [base // 2, base]):
+        pages = Pages([length], 1, 64, 16, dtype, seed=3).fill(4)
+        clean = pages.k.clone()
+        for p in range(length):
+            if p not in finite:
+                pages.k[int(pages.table_np[0, p // 16]), 0, p % 16, 0] = float("-inf")
+        got = run_tree(pages, q, [new], masks, 0.125)
+        pages.k.copy_(clean)
+        k, _ = cells(pages, pages.k, 0, length)
+        v, _ = cells(pages, pages.v, 0, length)
+        seen = torch.zeros(new, length, dtype=torch.bool, device="cuda")
+        for p in finite:
+            for i in range(new):
+                seen[i, p] = p < base or (p - base == i if tree else p - base <= i)
+        want, bound = attention(q.double(), k, v, seen, 0.125, dtype)
+        some = seen.any(1)
+        assert bool(torch.isnan(got[~some]).all()), finite
+        if bool(some.any()):
+            assert_rows(got[some], want[some], bound[some], finite)
+
+
+@pytest.mark.parametrize("length", [6, 100, 3000])
+def test_holes_and_empty_masks_beside_minus_infinity(length):
+    """Rows without a key that they see are zero, whatever stands in holes and in keys that others see."""
+    import torch
+    new = 6
+    pages = Pages([length, length], 1, 64, 16, "f16", seed=3).fill(4)
+    pages.k[:, :, :, 0] = float("-inf")
+    table = pages.table_np.copy()
+    table[0, :] = -1                                 # the first sequence has no page
+    pages.retable(table)
+    q = queries(2 * new, 4, 64, "f16")
+    q[:, :, 0] = 1.0
+    for masks in ([[0] * new, [0] * new], None):
+        got = run_tree(pages, q, [new, new], masks, 0.125)
+        assert bool((got[:new] == 0).all())
+        if masks is not None and length == new:
+            assert bool((got[new:2 * new] == 0).all())
+        else:
+            assert bool(torch.isnan(got[new:2 * new]).all())

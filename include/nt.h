@@ -507,7 +507,7 @@ nt_status nt_op_attn_paged_workspace(const nt_kv_pages* cache, int32_t n_heads, 
  * where one came out as no number, has scores past 2^24, or weighted values whose sum passes fp32's
  * largest number, are formed again key by key, at a small part of the speed).  Finite values have a finite
  * average (but in fp32 for one within its roundings of the largest number).  A row whose scores are all -inf
- * is no number, as one with a score of +inf or NaN is.
+ * is no number, as one with a score of +inf or NaN is; a scale of 0 makes no number of a query that is none.
  * Scores, softmax and sums are fp32; with 16-bit values each probability is rounded once to dtype
  * for the second product (half a step of it), and their sum is that of the rounded ones.  Results
  * do not depend on the other sequences except through where tiles of keys begin (a matter of

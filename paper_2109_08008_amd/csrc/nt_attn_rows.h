@@ -102,6 +102,14 @@ __device__ __forceinline__ void settle(floatx4* c) {
   }
 }
 
+// 0 times a word's values of T: NaN where one is no number.
+template <typename T>
+__device__ __forceinline__ unsigned times_zero(unsigned x) {
+  constexpr unsigned E = sizeof(T) == 4 ? 0x7f800000u : std::is_same<T, f16>::value ? 0x7c00u : 0x7f80u;
+  if constexpr (sizeof(T) == 4) return (x & E) == E ? 0x7fffffffu : 0u;
+  else return ((x & E) == E ? 0x7fffu : 0u) | ((x & E << 16) == E << 16 ? 0x7fff0000u : 0u);
+}
+
 // Four consecutive values (uint8_t: E4M3) as fp32.
 template <typename E>
 __device__ __forceinline__ void four_values(const char* p, float (&x)[4]) {
@@ -428,7 +436,10 @@ __global__ __launch_bounds__(64 * RW * KW) __attribute__((amdgpu_waves_per_eu(2)
 #pragma unroll
       for (int st = 0; st < QK; ++st)
 #pragma unroll
-        for (int w = 0; w < 4; ++w) qf[q][st][w] = (qf[q][st][w] & a.q_and) ^ a.q_xor;
+        for (int w = 0; w < 4; ++w) {
+          const unsigned x = qf[q][st][w];
+          qf[q][st][w] = ((x & a.q_and) ^ a.q_xor) | (times_zero<T>(x) & ~a.q_and);
+        }
   }
 
   // What lies behind the last key, or on no page, may be anything: its values become zeros (no 0 * NaN).
@@ -787,7 +798,7 @@ __global__ __launch_bounds__(64 * RW * KW) __attribute__((amdgpu_waves_per_eu(2)
               four_values<KV>(kp + (c * 16 + 4 * grp) * EC, x);
               four_values<T>(qrow[q] + (c * 16 + 4 * grp) * EB, y);
 #pragma unroll
-              for (int r = 0; r < 4; ++r) s = fmaf(x[r], y[r], s);
+              for (int r = 0; r < 4; ++r) s = fmaf(x[r], a.q_and ? y[r] : y[r] * 0.f, s);
             }
             s += __shfl_xor(s, 16, kWave);
             s += __shfl_xor(s, 32, kWave);

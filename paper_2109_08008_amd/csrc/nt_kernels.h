@@ -353,8 +353,8 @@ struct RowsAttnArgs {
   int out_ld;
   int n_seqs, n_rows, n_heads, group;   // group: query heads of a key head
   int max_new, max_len, causal;
-  // |scale| log2(e), and what the queries' words are masked and xored with for the rest of it;
-  // scale log2(e) itself
+  // |scale| log2(e), and what the queries' words are masked and xored with for the rest of it (masked with
+  // none, for a scale of 0, a word that is no number stays one); scale log2(e) itself
   float scale_log2, scale_signed;
   unsigned q_and, q_xor;
   // the call's cut (attn_prompt_plan, attn_tree_plan): a RowsTile; blocks of query rows (a key

@@ -172,3 +172,52 @@ def test_holes_and_empty_masks_beside_minus_infinity(length):
             assert bool((got[new:2 * new] == 0).all())
         else:
             assert bool(torch.isnan(got[new:2 * new]).all())
+
+
+# ---- a scale of 0 -----------------------------------------------------------------------
+@pytest.mark.parametrize("scale", [0.0, -0.0, 1e-40, -1e-40])
+@pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
+@pytest.mark.parametrize("bad", ["nan", "inf", "-inf"])
+def test_queries_that_are_no_numbers_at_scale_0(bad, dtype, scale):
+    """0 times what is no number is none, whether or not another row of the wave is formed again; the others
+    are means of their values."""
+    import torch
+    lens, h, hkv, dh = [40, 100], 2, 1, 64
+    for broken_value in (False, True):
+        x, off, rows = make(lens, h, hkv, dh, dtype, seed=4)
+        x[17, 3] = float(bad)                        # head 0 of a row of either sequence
+        x[60, dh + 5] = float(bad)                   # head 1
+        if broken_value:
+            x[39, (h + hkv) * dh:] = float("nan")    # seen by the first one's last row alone
+        got = run_prompt(x, off, rows, h, hkv, dh, dtype, True, scale).reshape(rows, h, dh)
+        hit = torch.zeros(rows, h, dtype=torch.bool, device="cuda")
+        hit[17, 0] = hit[60, 1] = True
+        hit[39] = broken_value
+        assert bool(torch.isnan(got[hit]).all())
+        q, k, v = split(torch.nan_to_num(x, posinf=0.0, neginf=0.0), h, hkv, dh)
+        for b, n in enumerate(lens):
+            lo, hi = off[b], off[b + 1]
+            seen = torch.ones(n, n, dtype=torch.bool, device="cuda").tril()
+            want, bound = attention(q[lo:hi], k[lo:hi], v[lo:hi], seen, 0.0, dtype)
+            ok = ~hit[lo:hi]
+            assert_rows(got[lo:hi][ok], want[ok], bound[ok], (b, broken_value))
+
+
+@pytest.mark.parametrize("dtype,fp8", [("f16", False), ("f16", True), ("bf16", False), ("f32", False)])
+def test_scale_0_over_a_cache(dtype, fp8):
+    """The same for new tokens over a cache, alone and in a tree."""
+    import torch
+    new = [3, 20]
+    pages = Pages([60, 700], 1, 64, 16, dtype, fp8, seed=2).fill(3)
+    q = queries(23, 4, 64, dtype, behind=0)
+    q[1, 2, 7] = float("nan")
+    q[9, 0, 0] = float("inf")
+    hit = torch.isnan(q).any(2) | torch.isinf(q).any(2)
+    clean = torch.nan_to_num(q, posinf=0.0)
+    for masks in (trees(new, 4), None):
+        got = run_tree(pages, q, new, masks, 0.0)
+        assert bool(torch.isnan(got[hit]).all())
+        want = run_tree(pages, clean, new, masks, 0.0)
+        check_tree(want, pages, clean, new, masks, 0.0)
+        got[hit] = want[hit]
+        check_tree(got, pages, clean, new, masks, 0.0)

@@ -756,9 +756,15 @@ __global__ __launch_bounds__(64 * RW * KW) __attribute__((amdgpu_waves_per_eu(2)
         const int key = (int)((unsigned)base + lane);
         mine = __ballot(key >= k0 && key < k1 && below(key + 1) > below(key));
       }
+      bool sees_some = false;
 #pragma unroll
       for (int q = 0; q < QB; ++q)
-        if (live[q] && m[q] == -INFINITY && ((bits[q] & mine) || below(min(hi[q], k1)) > below(lo[q]))) bad += 1.f;
+        sees_some |= live[q] && m[q] == -INFINITY && ((bits[q] & mine) || below(min(hi[q], k1)) > below(lo[q]));
+      if (__ballot(sees_some)) {
+        bool there = !PAGED;                            // (not where a sequence has no pages at all)
+        for (int t = k0; t < k1 && !there; t += SPAN) there = __ballot(pages_from(t) >= 0) != 0;
+        if (there && sees_some) bad += 1.f;
+      }
     }
     if (__ballot(bad != 0.f)) {
       float up[QB];                                     // 1 / down

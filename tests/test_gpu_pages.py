@@ -137,6 +137,29 @@ def test_all_or_nothing():
     step(plain, device, [30, -60, 0, 0, 40], 70)
 
 
+@pytest.mark.parametrize("n", [5, 1500])
+def test_more_pages_given_up_than_the_ring_has_room_for(n):
+    """Lengths and ring that do not match: nothing is done.  With the room, to the page, it is."""
+    import torch
+    for count, fits in ((100 * n, False), (100 * n - n // 5 + 1, False), (100 * n - n // 5, True)):
+        plain = Plain(n, 16, 100 * n, 4, seed=1, head=9)
+        plain.lens[:] = np.where(np.arange(n) % 5 == 2, 17, 16)
+        plain.table[:, :2] = np.arange(2 * n).reshape(n, 2)
+        plain.state[1] = count
+        device = Device(plain)
+        add = np.where(np.arange(n) % 5 == 2, -1, 0)           # every fifth sequence gives a page up
+        add[0] = 0
+        if fits:
+            step(plain, device, add, 7)
+            assert device.state.tolist() == [9, 100 * n, 0, 0]
+            continue
+        before = [x.clone() for x in (device.table, device.lens, device.ring)]
+        off, pos, slot = device.resize(add, 7)
+        assert device.state.tolist() == [9, count, -1, 0]
+        assert all(torch.equal(a, b) for a, b in zip(before, (device.table, device.lens, device.ring)))
+        assert not off.any() and (pos == -1).all() and (slot == -1).all()
+
+
 @pytest.mark.parametrize("outputs", [(), ("off",), ("pos",), ("slot",)])
 def test_outputs_are_optional(outputs):
     for n in (3, 1500):

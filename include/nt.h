@@ -509,7 +509,9 @@ nt_status nt_op_attn_paged_workspace(const nt_kv_pages* cache, int32_t n_heads, 
  * average (but in fp32 for one within its roundings of the largest number).  A row whose scores are all -inf
  * is no number, as one with a score of +inf or NaN is; a scale of 0 makes no number of a query that is none.
  * Scores, softmax and sums are fp32; with 16-bit values each probability is rounded once to dtype
- * for the second product (half a step of it), and their sum is that of the rounded ones.  Results
+ * for the second product (half a step of it), and their sum is that of the rounded ones: with u half a
+ * step and A = sum_j p_j |v_j| an output o is off by u (A + |o|) at most for it, beside its own rounding
+ * u |o| (fp16: and 2^-32 of the largest value a key).  Results
  * do not depend on the other sequences except through where tiles of keys begin (a matter of
  * rounding).  d_head in {32, 64, 128}.  out overlaps no input.  Asynchronous, one launch, no workspace,
  * on the current device.  NT_E_INVALID for a null pointer, a negative size, a d_head or heads that
@@ -521,7 +523,7 @@ nt_status nt_op_attn_prompt(int32_t dtype, const void* d_q, int32_t q_ld, int32_
                             int32_t n_seqs, int32_t n_rows, int32_t causal, float scale, void* d_out, int32_t out_ld,
                             void* stream);
 
-/* Attention of several new tokens a sequence over a paged cache, as nt_op_attn_paged for each:
+/* Attention of several new tokens a sequence over a paged cache, by nt_op_attn_paged's formula for each:
  * a tree of drafted tokens, a chain of them, or the next piece of a prompt.  Sequence b's new
  * tokens are rows d_off[b] .. d_off[b+1] - 1 of d_q and d_out (d_off: [n_seqs + 1] non-decreasing;
  * NULL: row b alone, n_rows == n_seqs) and its last positions of d_lens[b], in order, where
@@ -533,7 +535,8 @@ nt_status nt_op_attn_prompt(int32_t dtype, const void* d_q, int32_t q_ld, int32_
  * divided by): a sequence's rows past max_new are not written, positions past max_len not read.  A row that sees
  * nothing is zero; holes, what lies behind a length and what a row does not see are never part of
  * a result, as for nt_op_attn_prompt; rows of no sequence are not written.  Scores, softmax, sums
- * and roundings as there; into how many parts a length is cut follows from n_seqs, max_new and max_len
+ * and roundings as there (so with 16 bits a token's result may differ in its last bits from nt_op_attn_paged's, whose
+ * probabilities have two terms); into how many parts a length is cut follows from n_seqs, max_new and max_len
  * (a matter of rounding).  d_out overlaps no input.  fp8 caches as for nt_op_attn_paged.
  * d_ws: workspace of at least nt_op_attn_tree_workspace bytes (256-byte aligned; may be NULL
  * when that is 0), in use until the call's work is done: calls that may overlap need their own.

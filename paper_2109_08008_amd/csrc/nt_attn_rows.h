@@ -14,16 +14,18 @@
 // each has rows of its own, with few some of the tile's keys, and they join in LDS.
 //
 // Roundings.  16-bit probabilities are rounded once to the type, for the second product and their sum
-// alike (the sum is a product with ones), which costs at most a quarter of the output's own
-// rounding beside it: 2.0e-4 .. 2.6e-4 from 64 bits (fp16), 1.7e-3 .. 1.9e-3 (bf16), where fp32 throughout
-// has 2.0e-4 and 1.6e-3.  Two terms of P, as nt_op_attn_paged has them, would be half the products again.
+// alike (the sum is a product with ones).  With u half a step of the type and A = sum_j p_j |V_j| that adds at
+// most u (A + |o|) to the output's own u |o|, and in fp16, where probabilities below 2^-14 of the scaled ones
+// have fewer bits, 2^-32 of the largest value a key.  Measured on normal inputs: 2.0e-4 .. 2.6e-4 from 64 bits (fp16),
+// 1.7e-3 .. 1.9e-3 (bf16), where fp32 throughout has 2.0e-4 and 1.6e-3.  Two terms of P, as nt_op_attn_paged
+// has them, would be half the products again.
 //
 // What bounds it, one MI355X.  Long rows: the issue of a SIMD's two waves, of which the matrix cores have
 // 58 % and the softmax (a fused multiply-add, an exponential, half a conversion, a maximum an element) most of the
-// rest: 16383 tokens, 16 heads of 128 channels, causal, 0.97 ms = 1.13 PFLOP/s, above what a large fp16
+// rest: 16383 tokens, 16 heads of 128 channels, causal, 0.98 .. 1.0 ms = 1.1 PFLOP/s, above what a large fp16
 // product reaches (1.05).  Few rows over a cache: HBM, 5.1 TB/s (64 requests of 100..4000 positions, 8 key
 // heads).  Short sequences: a workgroup's reads in series (offsets, queries, tiles) with five workgroups a CU:
-// 540 of 1..150 tokens, 16 heads of 64: 107 us, 3.1 TB/s.
+// 540 of 1..150 tokens, 16 heads of 64: 104 us, 3.2 TB/s.
 #pragma once
 #include <algorithm>
 
@@ -180,7 +182,7 @@ struct Offsets {
     mine = n > 0 ? off[min(first + lane, n)] : 0;
   }
   // A lane's row: the last b in [0, n_seqs] with off[b] <= row (0 if there is none; n_seqs: behind the
-  // last sequence) and its first and last-but-one rows.
+  // last sequence), its first row and the row behind its last one.
   __device__ __forceinline__ int find(int row, int& start, int& end) const {
     int at = 0;
 #pragma unroll

@@ -38,19 +38,31 @@ void attn_prompt_plan(RowsAttnArgs* a) {
 // positions, 8 key heads of 128 channels (597 MB), 8 rows 110 / 108 / 126, 32 rows 176 / 109 / 117, 1..96 rows
 // - / 157 / 121, 256 rows - / 245 / 200.
 // Lengths are cut into parts of about chunk keys, a multiple of 512, alike within a sequence (its length
-// decides how many), so that two workgroups a CU have work; with more than two blocks of rows, where matrix
-// products bound it and a workgroup's own time is long, so that six have (the ends of ragged batches even
-// out), but into 8 parts at most, whose join costs less.  Measured, us, uncut / 4096 / 2048 / 1024
+// decides how many): the longest into 512 / tasks parts, rounded down, which is up to two workgroups a CU
+// (nothing is cut from 257 tasks on); with more than two blocks of rows, where matrix products bound it and a
+// workgroup's own time is long, into 3200 / tasks, though no more than 8 unless 512 / tasks is.  That is
+// twelve workgroups a CU by the largest sizes; ragged batches leave many of them empty or short, and their ends even
+// out.  Measured, us, uncut / 4096 / 2048 / 1024
 // keys: 12 requests of 1000..8000 positions and 200..500 new tokens, 4 key heads of four 228 / 174 / 164 /
 // 184, forty 498 / 498 / 498 / 511; three such in 3 / 4 / 8 parts 68 / 61 / 51; six of 2000..16000 positions and
 // 500..1000 new, 8 key heads of four, in 1 / 2 / 4 parts 576 / 492 / 507; one of 30000 positions, 512 new, in
 // 8 / 12 / 18 / 25 parts 269 / 279 / 290 / 300; one of 131001 E4M3 positions, 64 new, uncut / 4096 / 2048 /
 // 1024 keys 3150 / 119 / 90 / 106.  With parts of exactly chunk keys and a rest: 187 for the first's 174.
+// 1600 / 3200 / 6400 for tasks of more than two blocks, fp16, us: 16 heads on 4, 12 requests of 1000..8000 and
+// 200..500 new 174 / 165 / 185, 24 of them 364 / 340 / 352, 40 508 / 507 / 526; 32 heads on 8, 6 of 2000..16000 and
+// 500..1000 new (bf16) 579 / 497 / 514, 16 of 1000..3000 and 100..300 new 149 / 160 / 172; 8 on 8, 30 of
+// 500..4000 and 150..300 new 126 / 126 / 151; 8 on 2, 100 of 300..3000 and 70..300 new 167 / 166 / 199; one to three
+// requests within 1.5 % of each other.
+// One sequence much longer than the others is cut as they are: 64 requests, 8 key heads of 128 bf16 channels, 8
+// new tokens each, all of 4000 positions 161, one of them of 131001 2365, that one alone 92.
 // Never more than 32768 parts in all, however far max_len is above the lengths.
 // 16 rows by two waves instead of four, for the same reason as prompts, and for many short sequences: 8 key heads
 // of 128, up to 8 new tokens, 500 requests of 5..100 bf16 positions 88 / 53, of E4M3 44 / 29; 8 of 500..3000 29 / 25,
 // 64 of 100..4000 110 / 108, one of 16000 20.2 / 21.3; of 64 channels 500 of 5..100 37 / 24, 300 of 100..300 33 / 27,
 // 160 of 100..1000 37.8 / 38.1, 256 of 100..4000 174 / 182, 64 of 100..4000 54 / 66, 4 of 13..68 5.8 / 6.9.
+// fp32 goes by its bytes too, four waves / two: 8 key heads of 128, 500 of 5..100 121 / 80, 300 of 100..300 140 / 114, 8 of
+// 500..3000 56 / 48, 64 of 100..4000 274 / 280, 40 of 50..900 62 / 67; of 64 channels, 500 of 5..100 54 / 39, but 64 of
+// 100..4000 125 / 200.
 void attn_tree_plan(RowsAttnArgs* a) {
   const long long rows = (long long)std::max(a->max_new, 1) * a->group;
   a->tile = rows <= 16 ? ROWS_16 : rows <= 64 ? ROWS_64 : ROWS_128;
